@@ -89,6 +89,7 @@ extern "C" {
 #define ADAPLD_OP_SEMANTIC_TOPK_EMBED 5
 #define ADAPLD_OP_BUILD_DRAFT_TREE_PAPER 6
 #define ADAPLD_OP_STEP 7
+#define ADAPLD_OP_TREE_VERIFY_ATTN_KV4 8
 
 /* Limits of this implementation (larger values return ADAPLD_ERR_UNSUPPORTED). */
 #define ADAPLD_MAX_NMAX 64
@@ -522,6 +523,160 @@ int adapld_accept_greedy(const int32_t* node_token, const int32_t* node_parent,
                          int T_max, int Hkv, int D, int32_t* accept_len, int32_t* accept_nodes,
                          int32_t* out_tokens, uint16_t* k_ctx, uint16_t* v_ctx,
                          hipStream_t stream);
+
+/*
+ * Paged 4-bit K/V cache -- the context's K/V of the verify attention
+ * (Sec. 3.6) in pages of a pool, at 136 bytes per token and kv head instead of
+ * bf16's 512.
+ *
+ * A row is one token of one kv head, for K and for V: 128 codes of 4 bits
+ * (E2M1: sign, then 0 .5 1 1.5 2 3 4 6; dimension 2i in the low half of byte
+ * i, 2i + 1 in the high half) and one scale byte e for every
+ * ADAPLD_KV4_GROUP dimensions; a value is E2M1 * 2^(e - 127), exact in bf16.
+ *
+ *   k_codes, v_codes    uint8 [n_pages, Hkv, page_size, D / 2]
+ *   k_scales, v_scales  uint8 [n_pages, Hkv, page_size, D / ADAPLD_KV4_GROUP]
+ *   page_table          int32 [B, max_pages]: page i of sequence b holds its
+ *                       positions [i * page_size, (i + 1) * page_size)
+ *   page_size           16, 32, 64, 128 or 256 tokens
+ *   slot                page * page_size + offset in the page, a token's place
+ * Codes are 16-byte aligned, scales 4-byte aligned.  The arrays are the
+ * caller's, like every other buffer; pages need no initial contents.
+ * n_pages * page_size and max_pages * page_size must not exceed INT32_MAX
+ * (offsets into the arrays are 64-bit).
+ *
+ * An iteration of a decoding loop: adapld_kv4_page_map for the tokens to come
+ * (their slots), adapld_kv4_append of their K/V, adapld_tree_verify_attn_kv4,
+ * adapld_accept_greedy without K/V, then page_map and append again for the
+ * accepted nodes (rows = accept_nodes).
+ */
+#define ADAPLD_KV4_GROUP 32
+
+/*
+ * adapld_kv4_page_map -- page tables and slot maps from sequence lengths.
+ *
+ * Sequence b goes from lens_old[b] to lens_new[b] tokens (each clamped on the
+ * device to [0, max_pages * page_size]).  The pool's free pages are a stack:
+ * free_pages[0 .. free_count - 1], the next one to hand out on top.
+ *   1. A sequence that needs fewer pages than before gives its last ones
+ *      back: they are pushed in order of b, then of page index.  (lens_new = 0
+ *      ends a sequence.)  Their table entries are left as they are.
+ *   2. A sequence that needs more gets them from the top of the stack, in
+ *      order of b, then of page index, and they are written to its table
+ *      row.  Sequence b is served if the pages asked for by sequences 0..b
+ *      fit the stack; if not it gets none, and granted[b] = 0.
+ *   3. slot_map[b, i], i < N, is the slot of position lens_old[b] + i where
+ *      that is below lens_new[b], granted[b] is 1 and the table entry is a
+ *      page of the pool; otherwise -1.
+ * Table entries outside those ranges and stack entries above the pushed ones
+ * are untouched.  The same inputs give the same pages.
+ *
+ *   lens_old, lens_new  int32 [B]
+ *   page_table          int32 [B, max_pages]   (in, out)
+ *   free_pages          int32 [n_pages]        (in, out)
+ *   free_count          int32 [1]              pages on the stack
+ *   free_count_out      int32 [1]       (out)  the count after the call; may be
+ *                       free_count itself.  With another buffer the call can
+ *                       be made again on the same inputs.
+ *   N                   >= 0 slots per sequence; slot_map may be NULL if 0
+ *   slot_map            int32 [B, N]    (out)
+ *   granted             int32 [B]       (out)  1, or 0 where pages ran out
+ * No two buffers overlap, except free_count and free_count_out.
+ *
+ * Errors: NULL_ARG; INVALID_ARG for B < 0, max_pages, n_pages < 1, N < 0 or a
+ * page_size other than the five; UNSUPPORTED for n_pages * page_size,
+ * max_pages * page_size, B * max_pages or B * N > INT32_MAX, or B > 65535.
+ */
+int adapld_kv4_page_map(const int32_t* lens_old, const int32_t* lens_new, int B, int page_size, int max_pages,
+                        int n_pages, int N, int32_t* page_table, int32_t* free_pages, const int32_t* free_count,
+                        int32_t* free_count_out, int32_t* slot_map, int32_t* granted, hipStream_t stream);
+
+/*
+ * adapld_kv4_append -- quantises rows of K/V into the cache.
+ *
+ * For every b and i < N with a slot slot_map[b, i] in [0, n_pages * page_size)
+ * and a source row r = rows[b, i] (i itself if `rows` is NULL) in [0, n_src):
+ * the Hkv rows k_new[b, r], v_new[b, r] are stored at the slot.  Other entries
+ * are skipped (so -1 marks padding, and `rows` is not read there).  Per group
+ * of ADAPLD_KV4_GROUP values with largest magnitude amax, the scale X = 2^(e -
+ * 127) is the smallest power of two with amax < 7 X, e limited to 1..252; a
+ * code is |x| / X rounded to the nearest E2M1 (ties to the even code, 6 at
+ * most) with the sign of x.  Infinities are stored as 6 * 2^125; a NaN makes
+ * the values of its group unspecified, and no others.
+ *
+ *   k_new, v_new  bf16 [B, n_src, Hkv, D]   the layout of k_tree, v_tree
+ *   rows          int32 [B, N] or NULL      e.g. accept_nodes (NULL: N <= n_src)
+ *   slot_map      int32 [B, N]              slots of one call are distinct: of
+ *                 two equal ones the stored row is a mix of both
+ *
+ * Errors: NULL_ARG; INVALID_ARG for B < 0, n_src, N, Hkv, n_pages < 1, a
+ * page_size other than the five, N > n_src without rows or misaligned
+ * pointers; UNSUPPORTED for D != 128, n_pages * page_size > INT32_MAX or
+ * B * N * Hkv > 2^28 - 16.
+ */
+int adapld_kv4_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* slot_map,
+                      int B, int n_src, int N, int Hkv, int D, int page_size, int n_pages, uint8_t* k_codes,
+                      uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream);
+
+/*
+ * adapld_kv4_gather -- reads rows of the cache back as bf16 (exact values).
+ *
+ * k_out[b, i], v_out[b, i] (bf16 [B, N, Hkv, D]) are the rows at
+ * slot_map[b, i]; rows of slots outside [0, n_pages * page_size) are left as
+ * they are.  Arguments and errors as for adapld_kv4_append.
+ */
+int adapld_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                      const uint8_t* v_scales, const int32_t* slot_map, int B, int N, int Hkv, int D, int page_size,
+                      int n_pages, uint16_t* k_out, uint16_t* v_out, hipStream_t stream);
+
+/*
+ * adapld_tree_verify_attn_kv4 -- adapld_tree_verify_attn with the context's
+ * K/V in the paged 4-bit cache.
+ *
+ * For node u < T = node_count[b] and query head h (kv head g = h / (Hq/Hkv)):
+ * the keys are the cache rows of positions 0..L-1 of sequence b and kv head g,
+ * as the bf16 values they stand for, followed by k_tree[b, v, g] for every v <
+ * T with bit v of tree_mask[b, u] set; values likewise; out and lse as in
+ * adapld_tree_verify_attn.  k_tree, v_tree and tree_mask may all be NULL: then
+ * every row attends to the context alone (decoding of single tokens, whose own
+ * K/V are in the cache already).  A row without any key has out = 0 and lse =
+ * -inf.  L = lens[b] clamped to [0, L_max]; T is clamped to [0, T_max].
+ *
+ *   q           bf16 [B, T_max, Hq, D]
+ *   k_codes, k_scales, v_codes, v_scales, page_table   the cache; a table entry
+ *               of a page that holds a position below L must be a page of the
+ *               pool (with any other the sequence's results are unspecified;
+ *               nothing outside the cache is read); other entries and rows at
+ *               or behind L are not read
+ *   k_tree, v_tree  bf16 [B, T_max, Hkv, D] or NULL
+ *   lens, node_count, tree_mask   as in adapld_tree_verify_attn
+ *   L_max       an upper bound of the lengths, at most max_pages * page_size;
+ *               with the other sizes it decides how contexts are cut, so a
+ *               bound near the lengths serves them best
+ *   out         bf16 [B, T_max, Hq, D] (out) rows u >= T are not written
+ *   lse         fp32 [B, Hq, T_max]    (out, may be NULL) entries u >= T not written
+ *   ws          workspace of adapld_workspace_bytes(
+ *               ADAPLD_OP_TREE_VERIFY_ATTN_KV4, B, L_max, 0, 0, T_max, Hq, Hkv,
+ *               D) bytes (may be NULL if 0), 16-byte aligned
+ * A sequence's results depend on its own inputs and the sizes alone, not on
+ * its batch-mates, page ids or page size.
+ * q, the cache's values and the tree's K/V must be finite; scale must be
+ * finite and > 0.
+ *
+ * Errors: NULL_ARG (also for some but not all of k_tree, v_tree, tree_mask);
+ * INVALID_ARG for Hq % Hkv != 0, non-positive sizes, L_max > max_pages *
+ * page_size, a page_size other than the five, scale not finite and > 0, or
+ * misaligned pointers; UNSUPPORTED for D != 128, T_max >
+ * ADAPLD_MAX_TREE_NODES, n_pages * page_size or max_pages * page_size >
+ * INT32_MAX, L_max > 2^30, or more work than one launch holds (B * Hkv * T_max * Hq / Hkv
+ * times the number of context splits up to 2^23 - 8); WORKSPACE_TOO_SMALL.
+ */
+int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,
+                                const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* page_table,
+                                const uint16_t* k_tree, const uint16_t* v_tree, const int32_t* lens,
+                                const int32_t* node_count, const uint64_t* tree_mask, int B, int L_max, int T_max,
+                                int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, float scale,
+                                uint16_t* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

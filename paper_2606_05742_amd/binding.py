@@ -21,8 +21,10 @@ OP_LEXICAL_MATCH, OP_SEMANTIC_TOPK, OP_BUILD_DRAFT_TREE, OP_TREE_VERIFY_ATTN = 1
 OP_SEMANTIC_TOPK_EMBED = 5
 OP_BUILD_DRAFT_TREE_PAPER = 6
 OP_STEP = 7
+OP_TREE_VERIFY_ATTN_KV4 = 8
 SUCC_EVERY_BRANCH, SUCC_SEMANTIC_ONLY = 0, 1
 HEAD_DIM = 128
+KV4_GROUP = 32   # dimensions that share a scale of the 4-bit cache
 
 # ADAPLD_LIB names another build of the library (the sanitized host test
 # build); by default the in-tree libadapld.so.
@@ -86,6 +88,11 @@ SIGNATURES = {
         ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
         ctypes.c_float, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
         ctypes.c_void_p]),
+    "adapld_kv4_page_map": (ctypes.c_int, [ctypes.c_void_p] * 2 + [ctypes.c_int] * 5 + [ctypes.c_void_p] * 7),
+    "adapld_kv4_append": (ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int] * 7 + [ctypes.c_void_p] * 5),
+    "adapld_kv4_gather": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int] * 6 + [ctypes.c_void_p] * 3),
+    "adapld_tree_verify_attn_kv4": (ctypes.c_int, [ctypes.c_void_p] * 11 + [ctypes.c_int] * 9 + [ctypes.c_float]
+                                    + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
 }
 
 
@@ -153,6 +160,23 @@ def _stream(stream):
     if stream is not None:
         return stream.cuda_stream
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(_current_device())
+
+
+def _same_device(**tensors):
+    """The calls on the 4-bit cache launch on the current device: every tensor
+    must live there."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, _Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        at = t.get_device()
+        if at < 0:
+            raise AdapldError(-2, f"{name} must live on the GPU (got {t.device})")
+        dev = _current_device() if dev is None else dev
+        if at != dev:
+            raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
 
 
 def workspace_bytes(op, B, L_stride, d=0, k=0, T_max=0, Hq=0, Hkv=0, D=0) -> int:
@@ -432,6 +456,148 @@ class NgramIndex:
                                                             _stream(stream))
         _check(st, "adapld_ngram_index_append_match")
         return outs
+
+
+@dataclass
+class Kv4Cache:
+    """The paged 4-bit K/V cache of B sequences: a pool of pages, the page
+    table of each sequence and the stack of free pages (adapld_kv4_*).  The
+    buffers may be the caller's own, and those that no call uses None: page_map
+    takes the table and the stack, the other calls the pool and (the attention)
+    the table.  allocate() makes an empty cache."""
+    k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
+    k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    page_table: torch.Tensor    # int32 [B, max_pages]
+    free_pages: torch.Tensor    # int32 [n_pages], the stack
+    free_count: torch.Tensor    # int32 [1]
+    page_size: int
+
+    @staticmethod
+    def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
+        u8 = lambda n: torch.empty((n_pages, Hkv, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
+        return Kv4Cache(
+            k_codes=u8(D // 2), k_scales=u8(D // KV4_GROUP), v_codes=u8(D // 2), v_scales=u8(D // KV4_GROUP),
+            page_table=torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+            free_pages=torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+            free_count=torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size=page_size)
+
+    @property
+    def n_pages(self):
+        return self.k_codes.shape[0]
+
+    @property
+    def Hkv(self):
+        return self.k_codes.shape[1]
+
+    def _arrays(self):
+        """Pointers of the pool's four arrays."""
+        _same_device(k_codes=self.k_codes, k_scales=self.k_scales, v_codes=self.v_codes, v_scales=self.v_scales)
+        u8 = (torch.uint8,)
+        D = 2 * self.k_codes.shape[-1]
+        codes = (self.n_pages, self.Hkv, self.page_size, D // 2)
+        scales = (self.n_pages, self.Hkv, self.page_size, D // KV4_GROUP)
+        return (_ptr(self.k_codes, "k_codes", u8, codes), _ptr(self.k_scales, "k_scales", u8, scales),
+                _ptr(self.v_codes, "v_codes", u8, codes), _ptr(self.v_scales, "v_scales", u8, scales))
+
+
+def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, granted=None, free_count_out=None,
+             stream=None):
+    """Pages for sequences that go from lens_old to lens_new tokens, and the
+    slots of their first N new ones (N from slot_map if it is given); returns
+    (slot_map, granted).  The cache's page_table and stack are updated; the
+    stack's count goes to free_count_out (default: in place)."""
+    B, max_pages = cache.page_table.shape
+    n_pages = cache.free_pages.shape[0]
+    dev = cache.page_table.device
+    i32 = (torch.int32,)
+    if slot_map is None:
+        slot_map = torch.empty((B, 0 if N is None else N), dtype=torch.int32, device=dev)
+    N = slot_map.shape[1] if N is None else N
+    granted = _i32(B, dev) if granted is None else granted
+    free_count_out = cache.free_count if free_count_out is None else free_count_out
+    _same_device(page_table=cache.page_table, free_pages=cache.free_pages, free_count=cache.free_count,
+                 free_count_out=free_count_out, lens_old=lens_old, lens_new=lens_new, slot_map=slot_map, granted=granted)
+    st = load_library().adapld_kv4_page_map(
+        _ptr(lens_old, "lens_old", i32, (B,)), _ptr(lens_new, "lens_new", i32, (B,)), B, cache.page_size, max_pages,
+        n_pages, N, _ptr(cache.page_table, "page_table", i32), _ptr(cache.free_pages, "free_pages", i32), _ptr(cache.free_count, "free_count", i32, (1,)),
+        _ptr(free_count_out, "free_count_out", i32, (1,)), _ptr(slot_map, "slot_map", i32, (B, N)),
+        _ptr(granted, "granted", i32, (B,)), _stream(stream))
+    _check(st, "adapld_kv4_page_map")
+    return slot_map, granted
+
+
+def kv4_append(cache: Kv4Cache, k_new, v_new, slot_map, *, rows=None, stream=None):
+    """Quantises K/V rows (bf16 [B, n_src, Hkv, D]) into the cache: row
+    rows[b, i] (row i without rows) of sequence b at slot_map[b, i]; slots of
+    -1 are padding."""
+    B, n_src, Hkv, D = k_new.shape
+    N = slot_map.shape[1]
+    if Hkv != cache.Hkv:
+        raise AdapldError(-2, f"k_new has {Hkv} kv heads, the cache {cache.Hkv}")
+    _same_device(k_new=k_new, v_new=v_new, rows=rows, slot_map=slot_map)
+    st = load_library().adapld_kv4_append(
+        _ptr(k_new, "k_new", _BF16_DTYPES), _ptr(v_new, "v_new", _BF16_DTYPES, (B, n_src, Hkv, D)),
+        _ptr(rows, "rows", (torch.int32,), (B, N), nullable=True), _ptr(slot_map, "slot_map", (torch.int32,), (B, N)),
+        B, n_src, N, Hkv, D, cache.page_size, cache.n_pages, *cache._arrays(), _stream(stream))
+    _check(st, "adapld_kv4_append")
+
+
+def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None):
+    """The cache's rows at slot_map (int32 [B, N]) as bf16 [B, N, Hkv, D];
+    returns (k_out, v_out).  Rows of slots outside the pool are left as they
+    are (zero in new outputs)."""
+    B, N = slot_map.shape
+    D = 2 * cache.k_codes.shape[-1]
+    shape = (B, N, cache.Hkv, D)
+    new = lambda: torch.zeros(shape, dtype=torch.bfloat16, device=slot_map.device)  # noqa: E731
+    k_out = new() if k_out is None else k_out
+    v_out = new() if v_out is None else v_out
+    _same_device(slot_map=slot_map, k_out=k_out, v_out=v_out)
+    st = load_library().adapld_kv4_gather(
+        *cache._arrays(), _ptr(slot_map, "slot_map", (torch.int32,)), B, N, cache.Hkv, D, cache.page_size,
+        cache.n_pages, _ptr(k_out, "k_out", _BF16_DTYPES, shape), _ptr(v_out, "v_out", _BF16_DTYPES, shape),
+        _stream(stream))
+    _check(st, "adapld_kv4_gather")
+    return k_out, v_out
+
+
+def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None,
+                         L_max=None, scale=None, out=None, lse=None, ws=None, with_lse=True, stream=None):
+    """tree_verify_attn with the context in the 4-bit cache; without k_tree,
+    v_tree and tree_mask every row attends to the context alone.  L_max bounds
+    the lengths (default: what the page table holds).  Returns (out, lse)."""
+    lib = load_library()
+    B, T_max, Hq, D = q.shape
+    Hkv, max_pages = cache.Hkv, cache.page_table.shape[1]
+    dev = q.device
+    L_max = max_pages * cache.page_size if L_max is None else L_max
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    out = torch.empty((B, T_max, Hq, D), dtype=torch.bfloat16, device=dev) if out is None else out
+    if lse is None and with_lse:
+        lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=dev)
+    if ws is None:
+        need = workspace_bytes(OP_TREE_VERIFY_ATTN_KV4, B, L_max, 0, 0, T_max, Hq, Hkv, D)
+        ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    nw = (T_max + 63) // 64
+    if D != 2 * cache.k_codes.shape[-1]:
+        raise AdapldError(-2, f"q has head dimension {D}, the cache {2 * cache.k_codes.shape[-1]}")
+    _same_device(q=q, page_table=cache.page_table, lens=lens, node_count=node_count, k_tree=k_tree, v_tree=v_tree,
+                 tree_mask=tree_mask, out=out, lse=lse, ws=ws)
+    st = lib.adapld_tree_verify_attn_kv4(
+        _ptr(q, "q", _BF16_DTYPES), *cache._arrays(),
+        _ptr(cache.page_table, "page_table", (torch.int32,), (B, max_pages)),
+        _ptr(k_tree, "k_tree", _BF16_DTYPES, (B, T_max, Hkv, D), nullable=True),
+        _ptr(v_tree, "v_tree", _BF16_DTYPES, (B, T_max, Hkv, D), nullable=True),
+        _ptr(lens, "lens", (torch.int32,), (B,)), _ptr(node_count, "node_count", (torch.int32,), (B,)),
+        _ptr(tree_mask, "tree_mask", (torch.int64, torch.uint64), (B, T_max, nw), nullable=True),
+        B, L_max, T_max, Hq, Hkv, D, cache.page_size, cache.n_pages, max_pages, float(scale),
+        _ptr(out, "out", _BF16_DTYPES, (B, T_max, Hq, D)),
+        _ptr(lse, "lse", (torch.float32,), (B, Hq, T_max), nullable=True),
+        _ptr(ws, "ws", (torch.uint8,)), ws.numel(), _stream(stream))
+    _check(st, "adapld_tree_verify_attn_kv4")
+    return out, lse
 
 
 @dataclass

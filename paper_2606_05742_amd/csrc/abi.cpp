@@ -1,5 +1,6 @@
 // C ABI of libadapld: argument validation, workspace sizing, status reporting.
 // Every check runs on the host before anything is enqueued.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -150,6 +151,10 @@ size_t adapld_workspace_bytes(int op, int B, int L_stride, int d, int k, int T_m
       if (T_max < 1 || T_max > ADAPLD_MAX_TREE_NODES || Hq < 1 || Hkv < 1 || Hq % Hkv) return 0;
       const adapld::VerifyPlan p = adapld::plan_verify(B, L_stride, T_max, Hq, Hkv);
       return adapld::verify_ws_bytes(p, B, Hkv);
+    }
+    case ADAPLD_OP_TREE_VERIFY_ATTN_KV4: {
+      if (T_max < 1 || T_max > ADAPLD_MAX_TREE_NODES || Hq < 1 || Hkv < 1 || Hq % Hkv || L_stride > (1 << 30)) return 0;
+      return adapld::verify_kv4_ws_bytes(adapld::plan_verify_kv4(B, L_stride, T_max, Hq, Hkv), B, Hkv);
     }
     default:
       return 0;
@@ -421,6 +426,128 @@ int adapld_accept_greedy(const int32_t* node_token, const int32_t* node_parent,
                                                  tree_mask, target_next, lens, k_tree, v_tree, B,
                                                  L_stride, T_max, n_kv ? Hkv : 0, accept_len,
                                                  accept_nodes, out_tokens, k_ctx, v_ctx, stream));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------ paged 4-bit K/V cache
+
+namespace {
+
+// Sizes of the pool that every call on it shares.
+int check_kv4_pool(int page_size, int n_pages) {
+  if (n_pages < 1 || page_size < 16 || page_size > 256 || (page_size & (page_size - 1))) return ADAPLD_ERR_INVALID_ARG;
+  if ((int64_t)n_pages * page_size > INT32_MAX) return ADAPLD_ERR_UNSUPPORTED;
+  return ADAPLD_OK;
+}
+
+// A launch holds less than 2^32 threads: 16 a row, 512 a verify workgroup.
+constexpr int64_t kKv4MaxRows = (1 << 28) - 16;
+constexpr int64_t kKv4MaxGroups = (1 << 23) - 8;
+
+bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+
+int check_kv4_arrays(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                     const uint8_t* v_scales) {
+  if (!k_codes || !k_scales || !v_codes || !v_scales) return ADAPLD_ERR_NULL_ARG;
+  if (misaligned16(k_codes) || misaligned16(v_codes) || misaligned4(k_scales) || misaligned4(v_scales))
+    return ADAPLD_ERR_INVALID_ARG;
+  return ADAPLD_OK;
+}
+
+// Checks that append and gather share; x and y are the bf16 rows.
+int check_kv4_rows(const uint16_t* x, const uint16_t* y, const int32_t* slot_map, int B, int N, int Hkv, int D,
+                   int page_size, int n_pages, const uint8_t* k_codes, const uint8_t* k_scales,
+                   const uint8_t* v_codes, const uint8_t* v_scales) {
+  if (!x || !y || !slot_map) return ADAPLD_ERR_NULL_ARG;
+  if (const int st = check_kv4_arrays(k_codes, k_scales, v_codes, v_scales); st != ADAPLD_OK) return st;
+  if (N < 1 || Hkv < 1 || misaligned16(x) || misaligned16(y)) return ADAPLD_ERR_INVALID_ARG;
+  if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
+  if (D != ADAPLD_HEAD_DIM || (int64_t)B * N > kKv4MaxRows || (int64_t)B * N * Hkv > kKv4MaxRows)
+    return ADAPLD_ERR_UNSUPPORTED;
+  return ADAPLD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adapld_kv4_page_map(const int32_t* lens_old, const int32_t* lens_new, int B, int page_size, int max_pages,
+                        int n_pages, int N, int32_t* page_table, int32_t* free_pages, const int32_t* free_count,
+                        int32_t* free_count_out, int32_t* slot_map, int32_t* granted, hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (!lens_old || !lens_new || !page_table || !free_pages || !free_count || !free_count_out || !granted ||
+      (N > 0 && !slot_map))
+    return ADAPLD_ERR_NULL_ARG;
+  if (N < 0 || max_pages < 1) return ADAPLD_ERR_INVALID_ARG;
+  if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
+  if (B > 65535 || (int64_t)max_pages * page_size > INT32_MAX || (int64_t)B * max_pages > INT32_MAX ||
+      (int64_t)B * N > INT32_MAX)
+    return ADAPLD_ERR_UNSUPPORTED;
+  return hip_status(adapld::launch_kv4_page_map(lens_old, lens_new, B, page_size, max_pages, n_pages, N, page_table,
+                                                free_pages, free_count, free_count_out, slot_map, granted, stream));
+}
+
+int adapld_kv4_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* slot_map,
+                      int B, int n_src, int N, int Hkv, int D, int page_size, int n_pages, uint8_t* k_codes,
+                      uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (const int st = check_kv4_rows(k_new, v_new, slot_map, B, N, Hkv, D, page_size, n_pages, k_codes, k_scales,
+                                    v_codes, v_scales);
+      st != ADAPLD_OK)
+    return st;
+  if (n_src < 1 || (!rows && N > n_src)) return ADAPLD_ERR_INVALID_ARG;
+  return hip_status(adapld::launch_kv4_append(k_new, v_new, rows, slot_map, B, n_src, N, Hkv, page_size, n_pages,
+                                              k_codes, k_scales, v_codes, v_scales, stream));
+}
+
+int adapld_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                      const uint8_t* v_scales, const int32_t* slot_map, int B, int N, int Hkv, int D, int page_size,
+                      int n_pages, uint16_t* k_out, uint16_t* v_out, hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (const int st = check_kv4_rows(k_out, v_out, slot_map, B, N, Hkv, D, page_size, n_pages, k_codes, k_scales,
+                                    v_codes, v_scales);
+      st != ADAPLD_OK)
+    return st;
+  return hip_status(adapld::launch_kv4_gather(k_codes, k_scales, v_codes, v_scales, slot_map, B, N, Hkv, page_size,
+                                              n_pages, k_out, v_out, stream));
+}
+
+int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,
+                                const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* page_table,
+                                const uint16_t* k_tree, const uint16_t* v_tree, const int32_t* lens,
+                                const int32_t* node_count, const uint64_t* tree_mask, int B, int L_max, int T_max,
+                                int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, float scale,
+                                uint16_t* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (!q || !page_table || !lens || !node_count || !out) return ADAPLD_ERR_NULL_ARG;
+  const int n_tree = (k_tree != nullptr) + (v_tree != nullptr) + (tree_mask != nullptr);
+  if (n_tree != 0 && n_tree != 3) return ADAPLD_ERR_NULL_ARG;
+  if (const int st = check_kv4_arrays(k_codes, k_scales, v_codes, v_scales); st != ADAPLD_OK) return st;
+  if (L_max < 1 || T_max < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || !std::isfinite(scale) ||
+      !(scale > 0.f))
+    return ADAPLD_ERR_INVALID_ARG;
+  if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
+  if (D != ADAPLD_HEAD_DIM || T_max > ADAPLD_MAX_TREE_NODES || (int64_t)max_pages * page_size > INT32_MAX ||
+      L_max > (1 << 30))
+    return ADAPLD_ERR_UNSUPPORTED;
+  if (L_max > max_pages * page_size || misaligned16(q) || misaligned16(out) || misaligned16(k_tree) ||
+      misaligned16(v_tree))
+    return ADAPLD_ERR_INVALID_ARG;
+  const adapld::VerifyKv4Plan p = adapld::plan_verify_kv4(B, L_max, T_max, Hq, Hkv);
+  if ((double)B * Hkv * p.nsplit * std::max(p.rowgroups, p.rows_max) > kKv4MaxGroups) return ADAPLD_ERR_UNSUPPORTED;
+  const size_t need = adapld::verify_kv4_ws_bytes(p, B, Hkv);
+  if (need > 0 && !ws) return ADAPLD_ERR_NULL_ARG;
+  if (ws_bytes < need) return ADAPLD_ERR_WORKSPACE_TOO_SMALL;
+  if (need > 0 && misaligned16(ws)) return ADAPLD_ERR_INVALID_ARG;
+  const adapld::VerifyKv4Call c{q,   k_codes, k_scales, v_codes, v_scales, page_table, k_tree,   v_tree,  lens,
+                                node_count, tree_mask, B,  L_max,   T_max,    Hq,      Hkv,      page_size,
+                                n_pages, max_pages, scale, out, lse, ws};
+  return hip_status(adapld::launch_tree_verify_attn_kv4(c, p, stream));
 }
 
 }  // extern "C"

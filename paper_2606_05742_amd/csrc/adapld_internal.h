@@ -161,4 +161,48 @@ hipError_t launch_accept_greedy(const int32_t* node_token, const int32_t* node_p
                                 int32_t* accept_nodes, int32_t* out_tokens, uint16_t* k_ctx,
                                 uint16_t* v_ctx, hipStream_t stream);
 
+// ------------------------------------------------------ paged 4-bit K/V cache
+hipError_t launch_kv4_page_map(const int32_t* lens_old, const int32_t* lens_new, int B, int page_size, int max_pages,
+                               int n_pages, int N, int32_t* page_table, int32_t* free_pages,
+                               const int32_t* free_count, int32_t* free_count_out, int32_t* slot_map,
+                               int32_t* granted, hipStream_t stream);
+hipError_t launch_kv4_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows,
+                             const int32_t* slot_map, int B, int n_src, int N, int Hkv, int page_size, int n_pages,
+                             uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales,
+                             hipStream_t stream);
+hipError_t launch_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                             const uint8_t* v_scales, const int32_t* slot_map, int B, int N, int Hkv, int page_size,
+                             int n_pages, uint16_t* k_out, uint16_t* v_out, hipStream_t stream);
+
+// How the verify attention over the 4-bit cache decomposes a problem.
+struct VerifyKv4Plan {
+  int rows_max;    // T_max * G stacked query rows per (sequence, kv head)
+  int blocks;      // 32-row blocks per workgroup
+  int rowgroups;   // workgroups along the rows
+  int nsplit;      // context splits
+  int chunk;       // context keys per split (multiple of kKeyTile)
+};
+VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv);
+size_t verify_kv4_ws_bytes(const VerifyKv4Plan& p, int B, int Hkv);
+
+struct VerifyKv4Call {
+  const uint16_t* q;
+  const uint8_t* k_codes;
+  const uint8_t* k_scales;
+  const uint8_t* v_codes;
+  const uint8_t* v_scales;
+  const int32_t* page_table;
+  const uint16_t* k_tree;   // k_tree, v_tree, tree_mask: all or none
+  const uint16_t* v_tree;
+  const int32_t* lens;
+  const int32_t* node_count;
+  const uint64_t* tree_mask;
+  int B, L_max, T_max, Hq, Hkv, page_size, n_pages, max_pages;
+  float scale;
+  uint16_t* out;
+  float* lse;
+  void* ws;
+};
+hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Plan& p, hipStream_t stream);
+
 }  // namespace adapld

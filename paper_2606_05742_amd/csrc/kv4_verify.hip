@@ -1,0 +1,434 @@
+// Tree-masked verify attention over the paged 4-bit K/V cache (Sec. 3.6: all
+// draft paths are scored in one target forward with tree attention).
+#include <algorithm>
+#include <type_traits>
+
+#include "adapld_internal.h"
+#include "device_utils.h"
+#include "kv4.h"
+
+namespace adapld {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) bf16x8_t lds_bf16x8_t;
+
+constexpr int kD = ADAPLD_HEAD_DIM;
+constexpr int kRowBytes = kD * 2;                 // one bf16 row in LDS
+constexpr int kTileBytes = kKeyTile * kRowBytes;  // 16 KiB for K (and for V)
+constexpr int kStageBytes = 2 * kTileBytes;
+constexpr int kStages = 2;
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kMaskWords = (ADAPLD_MAX_TREE_NODES + 63) / 64;
+constexpr int kMaxChunk = 32768;                  // context keys of one split
+constexpr int kMinPage = 16;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kRescaleSlack = 8.0f;             // log2 units the running max may lag
+
+struct Kv4Args {
+  VerifyKv4Call c;
+  int G, rows_max, nw, nsplit, chunk, rowgroups, page_shift;
+  float scale_log2;
+  float* ws_o;     // [B*Hkv][nsplit][rows_max][D]  partial outputs O/l
+  float2* ws_ml;   // [B*Hkv][nsplit][rows_max]     (running max in log2 units, sum)
+};
+
+// Physical 16-byte chunk of logical chunk c in key row r is c ^ swz(r): a
+// bijection on every 16 consecutive rows, so 16 lanes that read (K fragments)
+// or write (the loader) one chunk of 16 rows touch all 64 banks; and the rows
+// of a transposed V read fall into different quarters of the bank row.
+__device__ __forceinline__ int swz(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+
+__device__ __forceinline__ bf16x8_t as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8_t, v); }
+
+// 8 codes with their scale as 8 bf16 values.
+__device__ __forceinline__ uint4 dequant8(uint32_t c, float X) {
+  uint4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 3));
+  return r;
+}
+
+// R 32-row blocks per workgroup; 8 / R waves share one and take 32 * R / 4 keys
+// of every tile each.
+template <int R>
+__global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a) {
+  static_assert(R == 8 || R == 4, "one or two waves per row block");
+  constexpr int KH = kWaves / R;
+  constexpr int HP = 2 / KH;   // 32-key halves of a tile that one wave takes
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStageBytes];
+  __shared__ uint64_t s_mask[ADAPLD_MAX_TREE_NODES * kMaskWords];
+  __shared__ int s_pages[kMaxChunk / kMinPage + 1];
+  const VerifyKv4Call& c = a.c;
+
+  // ---- the workgroup's job: the row groups of one (sequence, kv head, split)
+  // have consecutive slots on one XCD, so its L2 serves the second reader.
+  const int slot = blockIdx.x >> 3;
+  const int unit = (slot / a.rowgroups) * 8 + (blockIdx.x & 7);   // = bg * nsplit + split
+  const int rg = slot % a.rowgroups;
+  const int bg = unit / a.nsplit, split = unit - bg * a.nsplit;
+  const int b = bg / c.Hkv, g = bg - b * c.Hkv;
+  if (b >= c.B) return;
+  const int G = a.G;
+  const int T = min(max(c.node_count[b], 0), c.T_max);
+  const int L = min(max(c.lens[b], 0), c.L_max);
+  const int rows = T * G;
+  const int row_base = rg * (R * 32);
+  if (row_base >= rows) return;
+  const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, L);
+  const bool do_tree = split == a.nsplit - 1 && c.k_tree;
+  const int n_ctx = c1 > c0 ? (c1 - c0 + kKeyTile - 1) / kKeyTile : 0;
+  const int n_tiles = n_ctx + (do_tree ? (T + kKeyTile - 1) / kKeyTile : 0);
+
+  const int tid = threadIdx.x;
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int wrow = wave % R, kh = wave / R;
+  const int col = lane & 31, half = lane >> 5;
+
+  // ---- page ids of the split and the tree's mask to LDS
+  const int p0 = c0 >> a.page_shift;
+  if (n_ctx > 0) {
+    const int np = ((c1 - 1) >> a.page_shift) - p0 + 1;
+    for (int i = tid; i < np; i += kThreads)
+      s_pages[i] = kv4_page_in_pool(c.page_table[(size_t)b * c.max_pages + p0 + i], c.n_pages);
+  }
+  if (do_tree)
+    for (int i = tid; i < T * a.nw; i += kThreads) s_mask[i] = c.tree_mask[(size_t)b * c.T_max * a.nw + i];
+
+  // ---- query fragments (B operand): lane holds dims [16*ds + 8*half, +8) of its row
+  const int qr = row_base + wrow * 32 + col;
+  const bool valid = qr < rows;
+  const int u = valid ? qr / G : 0;
+  const int h = g * G + (valid ? qr - u * G : 0);
+  bf16x8_t qf[kD / 16];
+  {
+    const uint16_t* qp = c.q + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 8 * half;
+#pragma unroll
+    for (int ds = 0; ds < kD / 16; ++ds)
+      qf[ds] = as_bf16x8(valid ? *reinterpret_cast<const uint4*>(qp + 16 * ds) : make_uint4(0, 0, 0, 0));
+  }
+
+  // ---- loader: waves 0-3 bring K, waves 4-7 V; a lane one group of 32
+  // dimensions (16 bytes of codes) of one key.
+  const bool is_v = wave >= 4;
+  const int lkey = 16 * (wave & 3) + (lane & 15), lgrp = lane >> 4;
+  const uint8_t* codes = is_v ? c.v_codes : c.k_codes;
+  const uint8_t* scales = is_v ? c.v_scales : c.k_scales;
+  uint8_t* const lrow = smem + (is_v ? kTileBytes : 0) + lkey * kRowBytes;
+  int lpos[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) lpos[j] = ((4 * lgrp + j) ^ swz(lkey)) << 4;
+
+  struct Codes {
+    uint4 c;
+    uint32_t e;
+  };
+  // Keys behind the last read the last one again; their logits are masked.
+  auto load = [&](int t, Codes& x) {
+    const int pos = min(c0 + t * kKeyTile + lkey, c1 - 1);
+    const int page = s_pages[(pos >> a.page_shift) - p0];
+    const size_t row = kv4_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
+    x.c = *reinterpret_cast<const uint4*>(codes + row * kKv4RowBytes + lgrp * 16);
+    x.e = scales[row * kKv4Scales + lgrp];
+  };
+  auto store = [&](int t, const Codes& x) {
+    uint8_t* p = lrow + (t % kStages) * kStageBytes;
+    const float X = __uint_as_float(x.e << 23);
+    const uint32_t w[4] = {x.c.x, x.c.y, x.c.z, x.c.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(p + lpos[j]) = dequant8(w[j], X);
+  };
+  auto store_tree = [&](int t) {
+    const int v = min((t - n_ctx) * kKeyTile + lkey, T - 1);
+    const uint4* src = reinterpret_cast<const uint4*>((is_v ? c.v_tree : c.k_tree) +
+                                                      (((size_t)b * c.T_max + v) * c.Hkv + g) * kD + lgrp * 32);
+    uint8_t* p = lrow + (t % kStages) * kStageBytes;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(p + lpos[j]) = src[j];
+  };
+
+  // ---- LDS offsets of the fragments within a stage (kh: the wave's half)
+  const int half_off = (KH == 2 ? kh : 0) * 32 * kRowBytes;
+  int kofs[kD / 16];
+#pragma unroll
+  for (int ds = 0; ds < kD / 16; ++ds)
+    kofs[ds] = half_off + col * kRowBytes + (((2 * ds + half) ^ swz(col)) << 4);
+  const int vkey = 4 * half + ((lane & 15) >> 2);
+  const int vdim = (lane & 16) + 4 * (lane & 3);
+  int vofs[2][kD / 32];
+#pragma unroll
+  for (int db = 0; db < kD / 32; ++db) {
+    const int cch = (db * 32 + vdim) >> 3;
+    vofs[0][db] = half_off + kTileBytes + vkey * kRowBytes + ((cch ^ swz(vkey)) << 4) + (vdim & 7) * 2;
+    vofs[1][db] = half_off + kTileBytes + (vkey + 8) * kRowBytes + ((cch ^ swz(vkey + 8)) << 4) + (vdim & 7) * 2;
+  }
+
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16_t o[kD / 32];
+#pragma unroll
+  for (int db = 0; db < kD / 32; ++db) o[db] = f32x16_t{};
+  const float sl2 = a.scale_log2;
+
+  auto compute = [&](int t, int hp) {
+    const lds_u8* base = (const lds_u8*)smem + (t % kStages) * kStageBytes + (HP == 2 ? hp : 0) * 32 * kRowBytes;
+    f32x16_t s = f32x16_t{};
+#pragma unroll
+    for (int ds = 0; ds < kD / 16; ++ds) {
+      const bf16x8_t ka = *reinterpret_cast<const lds_bf16x8_t*>(base + kofs[ds]);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[ds], s, 0, 0, 0);
+    }
+    const bool is_tree = t >= n_ctx;
+    const int k0 = is_tree ? (t - n_ctx) * kKeyTile : c0 + t * kKeyTile;
+    const int kend = is_tree ? T : c1;
+    if (is_tree || k0 + kKeyTile > kend) {
+      const int kb = HP == 2 ? hp : kh;
+      const uint64_t mword = is_tree && valid ? s_mask[u * a.nw + (k0 >> 6)] : 0ull;
+      const uint32_t mbits = (uint32_t)(mword >> (kb * 32 + 4 * half));
+      const int kbase = k0 + kb * 32 + 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int kr = 8 * (r >> 2) + (r & 3);   // key kbase + kr
+        const bool ok = kbase + kr < kend && (!is_tree || ((mbits >> kr) & 1u));
+        s[r] = ok ? s[r] : -INFINITY;
+      }
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
+    mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1]));
+    const float mt = mx * sl2;   // scale > 0, so the max commutes with scaling
+    if (__ballot(mt > m_run + kRescaleSlack)) {
+      const float m_new = fmaxf(m_run, mt);
+      const float alpha = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < kD / 32; ++db) o[db] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    bf16x8_t pb[2];
+    float psum = 0.f;
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i], sl2, -m_use));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i + 1], sl2, -m_use));
+        psum += e0 + e1;
+        const bf16x2_t pk = __builtin_convertvector((f32x2_t){e0, e1}, bf16x2_t);
+        pb[s2][i] = pk[0];
+        pb[s2][i + 1] = pk[1];
+      }
+    l_run += psum;
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < kD / 32; ++db) {
+        const lds_u8* vb = base + 16 * s2 * kRowBytes;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + vofs[0][db]));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + vofs[1][db]));
+        const s16x8_t vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), pb[s2], o[db], 0, 0, 0);
+      }
+  };
+
+  // ---- tiles: codes of tile t + 2 are in flight and tile t + 1 is written
+  // to its stage while tile t is computed; one barrier a tile.
+  __syncthreads();   // the page ids and the mask
+  Codes cur{}, nxt{};
+  if (n_ctx > 0) {
+    load(0, cur);
+    if (n_ctx > 1) load(1, nxt);
+    store(0, cur);
+  } else if (n_tiles > 0) {
+    store_tree(0);
+  }
+  __syncthreads();
+  for (int t = 0; t < n_tiles; ++t) {
+    cur = nxt;
+    if (t + 2 < n_ctx) load(t + 2, nxt);
+    if (t + 1 < n_ctx) store(t + 1, cur);
+    else if (t + 1 < n_tiles) store_tree(t + 1);
+#pragma unroll
+    for (int hp = 0; hp < HP; ++hp) compute(t, hp);
+    __syncthreads();
+  }
+
+  // ---- epilogue: lane holds dims db*32 + 8*(r/4) + 4*half + r%4 of its query row
+  float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
+  if constexpr (KH == 2) {
+    // The wave with the other half of the keys hands its state over; each
+    // state is relative to its own running max, the merged one to M.
+    float4* xo = reinterpret_cast<float4*>(smem);                        // [R][16][64]
+    float2* xml = reinterpret_cast<float2*>(s_mask);                     // [R][64]
+    static_assert(R * 16 * 64 * 16 <= kStages * kStageBytes && R * 64 <= ADAPLD_MAX_TREE_NODES * kMaskWords,
+                  "the handed-over states fit");
+    if (kh == 1) {
+#pragma unroll
+      for (int db = 0; db < kD / 32; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          xo[(wrow * 16 + db * 4 + r4) * 64 + lane] =
+              make_float4(o[db][4 * r4], o[db][4 * r4 + 1], o[db][4 * r4 + 2], o[db][4 * r4 + 3]);
+      xml[wrow * 64 + lane] = make_float2(m_run, l_tot);
+    }
+    __syncthreads();
+    if (kh == 1) return;
+    const float2 ml = xml[wrow * 64 + lane];
+    const float M = fmaxf(m_run, ml.x);
+    const float a0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - M);
+    const float a1 = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+#pragma unroll
+    for (int db = 0; db < kD / 32; ++db)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const float4 v = xo[(wrow * 16 + db * 4 + r4) * 64 + lane];
+        o[db][4 * r4 + 0] = fmaf(a1, v.x, a0 * o[db][4 * r4 + 0]);
+        o[db][4 * r4 + 1] = fmaf(a1, v.y, a0 * o[db][4 * r4 + 1]);
+        o[db][4 * r4 + 2] = fmaf(a1, v.z, a0 * o[db][4 * r4 + 2]);
+        o[db][4 * r4 + 3] = fmaf(a1, v.w, a0 * o[db][4 * r4 + 3]);
+      }
+    l_tot = fmaf(a0, l_tot, a1 * ml.y);
+    m_run = M;
+  }
+  if (!valid) return;
+  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;   // a row without any key: 0
+  if (a.nsplit == 1) {
+    uint16_t* op = c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD;
+#pragma unroll
+    for (int db = 0; db < kD / 32; ++db)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        uint2 pk;
+        pk.x = f32_to_bf16_bits(o[db][4 * r4 + 0] * inv) | (f32_to_bf16_bits(o[db][4 * r4 + 1] * inv) << 16);
+        pk.y = f32_to_bf16_bits(o[db][4 * r4 + 2] * inv) | (f32_to_bf16_bits(o[db][4 * r4 + 3] * inv) << 16);
+        *reinterpret_cast<uint2*>(op + db * 32 + 8 * r4 + 4 * half) = pk;
+      }
+    if (half == 0 && c.lse)
+      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : -INFINITY;
+  } else {
+    const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + qr;
+    float* wp = a.ws_o + at * kD;
+#pragma unroll
+    for (int db = 0; db < kD / 32; ++db)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<float4*>(wp + db * 32 + 8 * r4 + 4 * half) =
+            make_float4(o[db][4 * r4] * inv, o[db][4 * r4 + 1] * inv, o[db][4 * r4 + 2] * inv, o[db][4 * r4 + 3] * inv);
+    if (half == 0) a.ws_ml[at] = make_float2(m_run, l_tot);
+  }
+}
+
+// Merge the splits: a row is 32 lanes of four dimensions.  Split s carries
+// O_s/l_s with weight l_s 2^(m_s - M).
+constexpr int kCombineThreads = 256;
+constexpr int kCombineRows = kCombineThreads / 32;
+__global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4Args a) {
+  const VerifyKv4Call& c = a.c;
+  const uint32_t row = blockIdx.x * kCombineRows + threadIdx.x / 32;
+  const uint32_t bg = row / (uint32_t)a.rows_max;
+  const int qr = (int)(row - bg * (uint32_t)a.rows_max);
+  const int b = (int)(bg / (uint32_t)c.Hkv);
+  if (b >= c.B) return;
+  const int T = min(max(c.node_count[b], 0), c.T_max);
+  if (qr >= T * a.G) return;
+  const int dim = (threadIdx.x & 31) * 4;
+  const size_t row0 = (size_t)bg * a.nsplit * a.rows_max + qr;
+  float M = -INFINITY, den = 0.f;
+  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < a.nsplit; ++s) {
+    const size_t at = row0 + (size_t)s * a.rows_max;
+    const float2 ml = a.ws_ml[at];
+    const float4 v = *reinterpret_cast<const float4*>(a.ws_o + at * kD + dim);
+    if (ml.y > 0.f) {
+      const float m_new = fmaxf(M, ml.x);
+      const float keep = exp2f(M - m_new);   // 0 while nothing has been merged
+      const float w = ml.y * exp2f(ml.x - m_new);
+      num.x = fmaf(num.x, keep, w * v.x);
+      num.y = fmaf(num.y, keep, w * v.y);
+      num.z = fmaf(num.z, keep, w * v.z);
+      num.w = fmaf(num.w, keep, w * v.w);
+      den = fmaf(den, keep, w);
+      M = m_new;
+    }
+  }
+  const int g = (int)bg - b * c.Hkv;
+  const int u = qr / a.G;
+  const int h = g * a.G + (qr - u * a.G);
+  const float inv = den > 0.f ? 1.f / den : 0.f;
+  uint2 pk;
+  pk.x = f32_to_bf16_bits(num.x * inv) | (f32_to_bf16_bits(num.y * inv) << 16);
+  pk.y = f32_to_bf16_bits(num.z * inv) | (f32_to_bf16_bits(num.w * inv) << 16);
+  *reinterpret_cast<uint2*>(c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + dim) = pk;
+  if (dim == 0 && c.lse)
+    c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = den > 0.f ? (M + log2f(den)) * kLn2 : -INFINITY;
+}
+
+}  // namespace
+
+VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
+  VerifyKv4Plan best{};
+  const int G = Hq / Hkv;
+  const int rows_max = T_max * G;
+  const int tiles = (L_max + kKeyTile - 1) / kKeyTile;   // L_max is at most 2^30
+  double best_cost = 0.0;
+  for (const int blocks : {8, 4}) {
+    const int rowgroups = (rows_max + blocks * 32 - 1) / (blocks * 32);
+    const int least = (tiles * kKeyTile + kMaxChunk - 1) / kMaxChunk;
+    const int most = std::max(least, std::min(64, tiles));
+    for (int want = least; want <= most; ++want) {
+      const int chunk = (tiles + want - 1) / want * kKeyTile;
+      const int nsplit = (tiles * kKeyTile + chunk - 1) / chunk;
+      if (nsplit != want) continue;   // the same split as a smaller count
+      const double rounds = (double)(((long)B * Hkv * rowgroups * nsplit + 255) / 256);
+      const double per_tile = blocks == 8 ? 2.0 : 1.0;
+      const double cost = rounds * (per_tile * (chunk / kKeyTile + (T_max + kKeyTile - 1) / kKeyTile) + 12.0) +
+                          (nsplit > 1 ? 6.0 : 0.0);
+      if (best.blocks == 0 || cost < best_cost) {
+        best_cost = cost;
+        best = VerifyKv4Plan{rows_max, blocks, rowgroups, nsplit, chunk};
+      }
+    }
+  }
+  return best;
+}
+
+size_t verify_kv4_ws_bytes(const VerifyKv4Plan& p, int B, int Hkv) {
+  if (p.nsplit <= 1) return 0;
+  return (size_t)B * Hkv * p.nsplit * p.rows_max * (kD * sizeof(float) + sizeof(float2));
+}
+
+hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Plan& p, hipStream_t stream) {
+  Kv4Args a{};
+  a.c = c;
+  a.G = c.Hq / c.Hkv; a.rows_max = p.rows_max; a.nw = (c.T_max + 63) / 64;
+  a.nsplit = p.nsplit; a.chunk = p.chunk; a.rowgroups = p.rowgroups; a.page_shift = log2_pow2(c.page_size);
+  a.scale_log2 = c.scale * kLog2e;
+  const size_t slots = (size_t)c.B * c.Hkv * p.nsplit * p.rows_max;
+  a.ws_o = static_cast<float*>(c.ws);
+  a.ws_ml = c.ws ? reinterpret_cast<float2*>(static_cast<float*>(c.ws) + slots * kD) : nullptr;
+  const int units = c.B * c.Hkv * p.nsplit;
+  const dim3 grid((unsigned)((units + 7) / 8 * 8 * p.rowgroups));
+  if (p.blocks == 8) hipLaunchKernelGGL(kv4_verify_kernel<8>, grid, dim3(kThreads), 0, stream, a);
+  else hipLaunchKernelGGL(kv4_verify_kernel<4>, grid, dim3(kThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.nsplit == 1) return e;
+  const unsigned n_rows = (unsigned)c.B * c.Hkv * p.rows_max;
+  hipLaunchKernelGGL(kv4_combine_kernel, dim3((n_rows + kCombineRows - 1) / kCombineRows), dim3(kCombineThreads), 0,
+                     stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace adapld
