@@ -59,6 +59,94 @@ __device__ __forceinline__ uint4 dequant8(uint32_t c, float X) {
   return r;
 }
 
+// ------------------------------------------------- one 32-row block's softmax
+//
+// S^T = K Q^T on v_mfma_f32_32x32x16_bf16 (A = 32 keys, B = 32 query rows)
+// leaves a lane one query row (lane & 31) and 16 keys of it: value r is key
+// 8*(r/4) + 4*(lane/32) + r%4.  So the online softmax is lane-local but for
+// one exchange with the other half of the wave, and P^T goes straight back as
+// the B operand of O^T = V^T P^T.
+struct Block {
+  float m, l;              // running max (log2 units) and this lane's share of the sum
+  f32x16_t o[kD / 32];     // O^T: value r is dim 32*db + 8*(r/4) + 4*(lane/32) + r%4
+};
+
+__device__ __forceinline__ void block_init(Block& x) {
+  x.m = -INFINITY;
+  x.l = 0.f;
+#pragma unroll
+  for (int db = 0; db < kD / 32; ++db) x.o[db] = f32x16_t{};
+}
+
+// Keys at or past n (of 32) out, and with TREE those whose mask bit is 0.
+template <bool TREE>
+__device__ __forceinline__ void mask_keys(f32x16_t& s, int n, uint32_t bits) {
+  const int k0 = 4 * (lane_id() >> 5);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int key = 8 * (r >> 2) + (r & 3) + k0;
+    s[r] = key < n && (!TREE || ((bits >> key) & 1u)) ? s[r] : -INFINITY;
+  }
+}
+
+// Max, lazy rescale and the exponentials of 32 keys: P^T packed to bf16 in the
+// order of the B operand.  The running max moves only when it grows by more
+// than kRescaleSlack (a factor 256), which keeps the rescale of the output off
+// the common path; the weights are rounded to bf16 once for the product and
+// summed before that in fp32.
+__device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, Block& x, bf16x8_t (&pb)[2]) {
+  float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+  for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
+  mx = fmaxf(mx, s[15]);
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
+  mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1]));
+  const float mt = mx * sl2;   // scale > 0, so the max commutes with scaling
+  if (__ballot(mt > x.m + kRescaleSlack)) {
+    const float m_new = fmaxf(x.m, mt);
+    const float alpha = m_new == x.m ? 1.f : __builtin_amdgcn_exp2f(x.m - m_new);
+    x.m = m_new;
+    x.l *= alpha;
+#pragma unroll
+    for (int db = 0; db < kD / 32; ++db) x.o[db] *= alpha;
+  }
+  const float m_use = x.m == -INFINITY ? 0.f : x.m;
+  float psum = 0.f;
+#pragma unroll
+  for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i], sl2, -m_use));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i + 1], sl2, -m_use));
+      psum += e0 + e1;
+      const bf16x2_t pk = __builtin_convertvector((f32x2_t){e0, e1}, bf16x2_t);
+      pb[s2][i] = pk[0];
+      pb[s2][i + 1] = pk[1];
+    }
+  x.l += psum;
+}
+
+// V^T fragment of 16 keys x 32 dims from row-major bf16 rows: each 16-lane
+// group reads 4 keys x 16 dims transposed, in the key order of P^T.
+__device__ __forceinline__ bf16x8_t v_fragment(const lds_u8* rows, int lo_ofs, int hi_ofs) {
+  const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(rows + lo_ofs));
+  const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(rows + hi_ofs));
+  const s16x8_t vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return __builtin_bit_cast(bf16x8_t, vv);
+}
+// Byte offsets of a lane's two reads for dims [32*db, +32): keys vkey and vkey + 8.
+__device__ __forceinline__ void v_offsets(int (&vofs)[2][kD / 32]) {
+  const int lane = lane_id();
+  const int vkey = 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const int vdim = (lane & 16) + 4 * (lane & 3);
+#pragma unroll
+  for (int db = 0; db < kD / 32; ++db) {
+    const int c = (db * 32 + vdim) >> 3;
+    vofs[0][db] = vkey * kRowBytes + ((c ^ swz(vkey)) << 4) + (vdim & 7) * 2;
+    vofs[1][db] = (vkey + 8) * kRowBytes + ((c ^ swz(vkey + 8)) << 4) + (vdim & 7) * 2;
+  }
+}
+
 // R 32-row blocks per workgroup; 8 / R waves share one and take 32 * R / 4 keys
 // of every tile each.
 template <int R>
@@ -163,85 +251,39 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   int kofs[kD / 16];
 #pragma unroll
   for (int ds = 0; ds < kD / 16; ++ds)
-    kofs[ds] = half_off + col * kRowBytes + (((2 * ds + half) ^ swz(col)) << 4);
-  const int vkey = 4 * half + ((lane & 15) >> 2);
-  const int vdim = (lane & 16) + 4 * (lane & 3);
+    kofs[ds] = col * kRowBytes + (((2 * ds + half) ^ swz(col)) << 4);
   int vofs[2][kD / 32];
-#pragma unroll
-  for (int db = 0; db < kD / 32; ++db) {
-    const int cch = (db * 32 + vdim) >> 3;
-    vofs[0][db] = half_off + kTileBytes + vkey * kRowBytes + ((cch ^ swz(vkey)) << 4) + (vdim & 7) * 2;
-    vofs[1][db] = half_off + kTileBytes + (vkey + 8) * kRowBytes + ((cch ^ swz(vkey + 8)) << 4) + (vdim & 7) * 2;
-  }
+  v_offsets(vofs);
 
-  float m_run = -INFINITY, l_run = 0.f;
-  f32x16_t o[kD / 32];
-#pragma unroll
-  for (int db = 0; db < kD / 32; ++db) o[db] = f32x16_t{};
+  Block x;
+  block_init(x);
   const float sl2 = a.scale_log2;
 
   auto compute = [&](int t, int hp) {
-    const lds_u8* base = (const lds_u8*)smem + (t % kStages) * kStageBytes + (HP == 2 ? hp : 0) * 32 * kRowBytes;
+    const lds_u8* base =
+        (const lds_u8*)smem + (t % kStages) * kStageBytes + half_off + (HP == 2 ? hp : 0) * 32 * kRowBytes;
     f32x16_t s = f32x16_t{};
 #pragma unroll
     for (int ds = 0; ds < kD / 16; ++ds) {
       const bf16x8_t ka = *reinterpret_cast<const lds_bf16x8_t*>(base + kofs[ds]);
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[ds], s, 0, 0, 0);
     }
-    const bool is_tree = t >= n_ctx;
-    const int k0 = is_tree ? (t - n_ctx) * kKeyTile : c0 + t * kKeyTile;
-    const int kend = is_tree ? T : c1;
-    if (is_tree || k0 + kKeyTile > kend) {
-      const int kb = HP == 2 ? hp : kh;
-      const uint64_t mword = is_tree && valid ? s_mask[u * a.nw + (k0 >> 6)] : 0ull;
-      const uint32_t mbits = (uint32_t)(mword >> (kb * 32 + 4 * half));
-      const int kbase = k0 + kb * 32 + 4 * half;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int kr = 8 * (r >> 2) + (r & 3);   // key kbase + kr
-        const bool ok = kbase + kr < kend && (!is_tree || ((mbits >> kr) & 1u));
-        s[r] = ok ? s[r] : -INFINITY;
-      }
+    const int kb = 32 * (HP == 2 ? hp : kh);   // first key of the half
+    if (t >= n_ctx) {
+      const int k0 = (t - n_ctx) * kKeyTile;
+      const uint64_t mword = valid ? s_mask[u * a.nw + (k0 >> 6)] : 0ull;
+      mask_keys<true>(s, T - k0 - kb, (uint32_t)(mword >> kb));
+    } else if (c0 + (t + 1) * kKeyTile > c1) {
+      mask_keys<false>(s, c1 - c0 - t * kKeyTile - kb, 0u);
     }
-    float mx = s[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
-    mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1]));
-    const float mt = mx * sl2;   // scale > 0, so the max commutes with scaling
-    if (__ballot(mt > m_run + kRescaleSlack)) {
-      const float m_new = fmaxf(m_run, mt);
-      const float alpha = m_new == m_run ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-      m_run = m_new;
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < kD / 32; ++db) o[db] *= alpha;
-    }
-    const float m_use = m_run == -INFINITY ? 0.f : m_run;
     bf16x8_t pb[2];
-    float psum = 0.f;
+    softmax_step(s, sl2, x, pb);
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float e0 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i], sl2, -m_use));
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i + 1], sl2, -m_use));
-        psum += e0 + e1;
-        const bf16x2_t pk = __builtin_convertvector((f32x2_t){e0, e1}, bf16x2_t);
-        pb[s2][i] = pk[0];
-        pb[s2][i + 1] = pk[1];
-      }
-    l_run += psum;
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-      for (int db = 0; db < kD / 32; ++db) {
-        const lds_u8* vb = base + 16 * s2 * kRowBytes;
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + vofs[0][db]));
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vb + vofs[1][db]));
-        const s16x8_t vv = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, vv), pb[s2], o[db], 0, 0, 0);
-      }
+      for (int db = 0; db < kD / 32; ++db)
+        x.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            v_fragment(base + kTileBytes + 16 * s2 * kRowBytes, vofs[0][db], vofs[1][db]), pb[s2], x.o[db], 0, 0, 0);
   };
 
   // ---- tiles: codes of tile t + 2 are in flight and tile t + 1 is written
@@ -267,7 +309,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   }
 
   // ---- epilogue: lane holds dims db*32 + 8*(r/4) + 4*half + r%4 of its query row
-  float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
+  float l_tot = x.l + __shfl_xor(x.l, 32, kWave);
   if constexpr (KH == 2) {
     // The wave with the other half of the keys hands its state over; each
     // state is relative to its own running max, the merged one to M.
@@ -281,27 +323,27 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4)
           xo[(wrow * 16 + db * 4 + r4) * 64 + lane] =
-              make_float4(o[db][4 * r4], o[db][4 * r4 + 1], o[db][4 * r4 + 2], o[db][4 * r4 + 3]);
-      xml[wrow * 64 + lane] = make_float2(m_run, l_tot);
+              make_float4(x.o[db][4 * r4], x.o[db][4 * r4 + 1], x.o[db][4 * r4 + 2], x.o[db][4 * r4 + 3]);
+      xml[wrow * 64 + lane] = make_float2(x.m, l_tot);
     }
     __syncthreads();
     if (kh == 1) return;
     const float2 ml = xml[wrow * 64 + lane];
-    const float M = fmaxf(m_run, ml.x);
-    const float a0 = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - M);
+    const float M = fmaxf(x.m, ml.x);
+    const float a0 = x.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x.m - M);
     const float a1 = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
 #pragma unroll
     for (int db = 0; db < kD / 32; ++db)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const float4 v = xo[(wrow * 16 + db * 4 + r4) * 64 + lane];
-        o[db][4 * r4 + 0] = fmaf(a1, v.x, a0 * o[db][4 * r4 + 0]);
-        o[db][4 * r4 + 1] = fmaf(a1, v.y, a0 * o[db][4 * r4 + 1]);
-        o[db][4 * r4 + 2] = fmaf(a1, v.z, a0 * o[db][4 * r4 + 2]);
-        o[db][4 * r4 + 3] = fmaf(a1, v.w, a0 * o[db][4 * r4 + 3]);
+        x.o[db][4 * r4 + 0] = fmaf(a1, v.x, a0 * x.o[db][4 * r4 + 0]);
+        x.o[db][4 * r4 + 1] = fmaf(a1, v.y, a0 * x.o[db][4 * r4 + 1]);
+        x.o[db][4 * r4 + 2] = fmaf(a1, v.z, a0 * x.o[db][4 * r4 + 2]);
+        x.o[db][4 * r4 + 3] = fmaf(a1, v.w, a0 * x.o[db][4 * r4 + 3]);
       }
     l_tot = fmaf(a0, l_tot, a1 * ml.y);
-    m_run = M;
+    x.m = M;
   }
   if (!valid) return;
   const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;   // a row without any key: 0
@@ -312,12 +354,12 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         uint2 pk;
-        pk.x = f32_to_bf16_bits(o[db][4 * r4 + 0] * inv) | (f32_to_bf16_bits(o[db][4 * r4 + 1] * inv) << 16);
-        pk.y = f32_to_bf16_bits(o[db][4 * r4 + 2] * inv) | (f32_to_bf16_bits(o[db][4 * r4 + 3] * inv) << 16);
+        pk.x = f32_to_bf16_bits(x.o[db][4 * r4 + 0] * inv) | (f32_to_bf16_bits(x.o[db][4 * r4 + 1] * inv) << 16);
+        pk.y = f32_to_bf16_bits(x.o[db][4 * r4 + 2] * inv) | (f32_to_bf16_bits(x.o[db][4 * r4 + 3] * inv) << 16);
         *reinterpret_cast<uint2*>(op + db * 32 + 8 * r4 + 4 * half) = pk;
       }
     if (half == 0 && c.lse)
-      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l_tot > 0.f ? (m_run + log2f(l_tot)) * kLn2 : -INFINITY;
+      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l_tot > 0.f ? (x.m + log2f(l_tot)) * kLn2 : -INFINITY;
   } else {
     const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + qr;
     float* wp = a.ws_o + at * kD;
@@ -326,8 +368,276 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4)
         *reinterpret_cast<float4*>(wp + db * 32 + 8 * r4 + 4 * half) =
-            make_float4(o[db][4 * r4] * inv, o[db][4 * r4 + 1] * inv, o[db][4 * r4 + 2] * inv, o[db][4 * r4 + 3] * inv);
-    if (half == 0) a.ws_ml[at] = make_float2(m_run, l_tot);
+            make_float4(x.o[db][4 * r4] * inv, x.o[db][4 * r4 + 1] * inv, x.o[db][4 * r4 + 2] * inv, x.o[db][4 * r4 + 3] * inv);
+    if (half == 0) a.ws_ml[at] = make_float2(x.m, l_tot);
+  }
+}
+
+// ------------------------------------------------------------- up to 64 rows
+//
+// With one or two 32-row blocks (single tokens, one copied chain) the call is
+// one pass over the cache, so no two waves share keys: wave w of 8 takes the
+// 32-key steps w, w + 8, ... of the split, alone, without a barrier.  K codes
+// go from memory straight to the A fragments: the order of the dimensions in
+// the products is free, so a lane's 16 bytes (one group of 32 dimensions of one
+// key, one scale) are four fragments, and Q is loaded in the same order.  V
+// codes become bf16 rows in 8 KiB of LDS that the wave has for itself, from
+// which they are read transposed.  Codes of two steps are in flight.  At the
+// end the waves' states are merged through LDS.
+constexpr int kStep = 32;
+constexpr int kWaveLds = kStep * kRowBytes;   // 8 KiB
+
+template <int NB>
+__global__ __launch_bounds__(kThreads, 1) void kv4_narrow_kernel(const Kv4Args a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * kWaveLds];
+  __shared__ float2 s_ml[kWaves][NB * 32];
+  __shared__ int s_pages[kMaxChunk / kMinPage + 1];
+  // Two blocks' query fragments do not fit the registers beside their outputs:
+  // all waves read them from here, 16 bytes a lane.
+  constexpr bool kQInLds = NB == 2;
+  constexpr int kDepth = NB == 2 ? 1 : 2;   // steps whose codes are in flight
+  __shared__ uint4 s_q[kQInLds ? NB * 8 * kWave : 1];
+  const VerifyKv4Call& c = a.c;
+  const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
+  const int b = bg / c.Hkv, g = bg - b * c.Hkv;
+  const int G = a.G;
+  const int T = min(max(c.node_count[b], 0), c.T_max);
+  const int L = min(max(c.lens[b], 0), c.L_max);
+  const int rows = T * G;
+  if (rows == 0) return;
+  const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, L);
+  const bool do_tree = split == a.nsplit - 1 && c.k_tree;
+  const int n_ctx = c1 > c0 ? (c1 - c0 + kStep - 1) / kStep : 0;
+  const int n_steps = n_ctx + (do_tree ? (T + kStep - 1) / kStep : 0);
+
+  const int tid = threadIdx.x;
+  const int lane = lane_id();
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int col = lane & 31, half = lane >> 5;
+
+  const int p0 = c0 >> a.page_shift;
+  if (n_ctx > 0) {
+    const int np = ((c1 - 1) >> a.page_shift) - p0 + 1;
+    for (int i = tid; i < np; i += kThreads)
+      s_pages[i] = kv4_page_in_pool(c.page_table[(size_t)b * c.max_pages + p0 + i], c.n_pages);
+  }
+
+  // Query fragment (i, j): dims [32 * (2i + half) + 8j, +8) of the lane's row.
+  bf16x8_t qf[kQInLds ? 1 : NB][2][4];
+  uint64_t sees[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const int qr = nb * 32 + col;
+    const bool valid = qr < rows;
+    const int u = valid ? qr / G : 0;
+    const int h = g * G + (valid ? qr - u * G : 0);
+    const uint16_t* qp = c.q + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 32 * half;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (!kQInLds || wave == nb * 4 + i * 2 + j / 2) {
+          const uint4 w = valid ? *reinterpret_cast<const uint4*>(qp + 64 * i + 8 * j) : make_uint4(0, 0, 0, 0);
+          if constexpr (kQInLds) s_q[((nb * 2 + i) * 4 + j) * kWave + lane] = w;
+          else qf[nb][i][j] = as_bf16x8(w);
+        }
+    // at most 64 rows, so at most 64 nodes and one mask word
+    sees[nb] = do_tree && valid ? c.tree_mask[(size_t)b * c.T_max + u] : 0ull;
+  }
+
+  Block x[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) block_init(x[nb]);
+  const float sl2 = a.scale_log2;
+  uint8_t* const vrows = smem + wave * kWaveLds;
+  const lds_u8* const vbase = (const lds_u8*)vrows;
+  const int vkey = lane & 15, vgrp = lane >> 4;   // loader: keys vkey, vkey + 16, one group
+  int vpos[4], vofs[2][kD / 32];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) vpos[j] = vkey * kRowBytes + (((4 * vgrp + j) ^ swz(vkey)) << 4);
+  v_offsets(vofs);
+
+  struct Raw {
+    uint4 k[2], v[2];
+    uint32_t ke, ve[2];
+  };
+  auto row_of = [&](int pos) {
+    pos = min(pos, c1 - 1);   // keys behind the last read the last one again; they are masked
+    const int page = s_pages[(pos >> a.page_shift) - p0];
+    return kv4_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
+  };
+  auto load = [&](int s, Raw& r) {
+    const int k0 = c0 + s * kStep;
+    const size_t row = row_of(k0 + col);
+    const uint8_t* kc = c.k_codes + row * kKv4RowBytes + 16 * half;
+    r.k[0] = *reinterpret_cast<const uint4*>(kc);
+    r.k[1] = *reinterpret_cast<const uint4*>(kc + 32);
+    r.ke = *reinterpret_cast<const uint32_t*>(c.k_scales + row * kKv4Scales);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const size_t vr = row_of(k0 + vkey + 16 * i);
+      r.v[i] = *reinterpret_cast<const uint4*>(c.v_codes + vr * kKv4RowBytes + 16 * vgrp);
+      r.ve[i] = c.v_scales[vr * kKv4Scales + vgrp];
+    }
+  };
+  // S, softmax and O of one step whose V rows are in LDS; ka(i, j) are its K fragments.
+  auto attend = [&](auto&& ka, auto tree, int n, int k0) {
+    // keeps the queries' reads in the loop: hoisted, they spill
+    if constexpr (kQInLds) asm volatile("" ::: "memory");
+    f32x16_t s[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) s[nb] = f32x16_t{};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8_t f = ka(i, j);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              f, kQInLds ? as_bf16x8(s_q[((nb * 2 + i) * 4 + j) * kWave + lane]) : qf[kQInLds ? 0 : nb][i][j], s[nb], 0,
+              0, 0);
+      }
+    bf16x8_t pb[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if constexpr (decltype(tree)::value) mask_keys<true>(s[nb], n, (uint32_t)(sees[nb] >> k0));
+      else if (n < kStep) mask_keys<false>(s[nb], n, 0u);
+      softmax_step(s[nb], sl2, x[nb], pb[nb]);
+    }
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < kD / 32; ++db) {
+        const bf16x8_t f = v_fragment(vbase + 16 * s2 * kRowBytes, vofs[0][db], vofs[1][db]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+          x[nb].o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[nb][s2], x[nb].o[db], 0, 0, 0);
+      }
+  };
+  auto ctx_step = [&](int s, Raw& r) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float X = __uint_as_float(r.ve[i] << 23);
+      const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)   // keys 16 apart have the same swizzle
+        *reinterpret_cast<uint4*>(vrows + 16 * i * kRowBytes + vpos[j]) = dequant8(w[j], X);
+    }
+    bf16x8_t f[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float X = __uint_as_float(((r.ke >> (8 * (2 * i + half))) & 0xffu) << 23);
+      const uint32_t w[4] = {r.k[i].x, r.k[i].y, r.k[i].z, r.k[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[i][j] = as_bf16x8(dequant8(w[j], X));
+    }
+    if (s + kDepth * kWaves < n_ctx) load(s + kDepth * kWaves, r);
+    attend([&](int i, int j) { return f[i][j]; }, std::false_type{}, c1 - c0 - s * kStep, 0);
+  };
+  auto tree_step = [&](int s) {
+    const int k0 = (s - n_ctx) * kStep;
+    const size_t node0 = (size_t)b * c.T_max;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4* src = reinterpret_cast<const uint4*>(
+          c.v_tree + ((node0 + min(k0 + vkey + 16 * i, T - 1)) * c.Hkv + g) * kD + 32 * vgrp);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(vrows + 16 * i * kRowBytes + vpos[j]) = src[j];
+    }
+    const uint16_t* kp = c.k_tree + ((node0 + min(k0 + col, T - 1)) * c.Hkv + g) * kD + 32 * half;
+    attend([&](int i, int j) { return as_bf16x8(*reinterpret_cast<const uint4*>(kp + 64 * i + 8 * j)); },
+           std::true_type{}, T - k0, k0);
+  };
+
+  __syncthreads();   // the page ids and the queries
+  {
+    Raw r[kDepth];
+    int s = wave;
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d)
+      if (s + d * kWaves < n_ctx) load(s + d * kWaves, r[d]);
+    for (; s + (kDepth - 1) * kWaves < n_ctx; s += kDepth * kWaves)
+#pragma unroll
+      for (int d = 0; d < kDepth; ++d) ctx_step(s + d * kWaves, r[d]);
+#pragma unroll
+    for (int d = 0; d + 1 < kDepth; ++d)
+      if (s < n_ctx) {
+        ctx_step(s, r[d]);
+        s += kWaves;
+      }
+    for (; s < n_steps; s += kWaves) tree_step(s);
+  }
+
+  // ---- merge: every wave's output relative to the common max, 16 rows at a
+  // time: [wave][row][dim], 16-byte chunks swizzled by the row.
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    const float l = x[nb].l + __shfl_xor(x[nb].l, 32, kWave);
+    if (half == 0) s_ml[wave][nb * 32 + col] = make_float2(x[nb].m, l);
+  }
+  __syncthreads();
+  float scale[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][nb * 32 + col].x);
+    scale[nb] = x[nb].m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[nb].m - M);
+  }
+  float4* const xo = reinterpret_cast<float4*>(smem);   // [kWaves][16][32]
+  static_assert(kWaves * 16 * 32 * 16 <= kWaves * kWaveLds, "16 rows of every wave fit");
+#pragma unroll
+  for (int ph = 0; ph < 2 * NB; ++ph) {
+    if (ph * 16 >= rows) break;
+    const int nb = ph / 2;
+    if (ph > 0) __syncthreads();
+    if ((col >> 4) == (ph & 1) && nb * 32 + col < rows) {
+      const int r16 = col & 15;
+#pragma unroll
+      for (int db = 0; db < kD / 32; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          xo[(wave * 16 + r16) * 32 + ((db * 8 + 2 * r4 + half) ^ r16)] =
+              make_float4(x[nb].o[db][4 * r4] * scale[nb], x[nb].o[db][4 * r4 + 1] * scale[nb],
+                          x[nb].o[db][4 * r4 + 2] * scale[nb], x[nb].o[db][4 * r4 + 3] * scale[nb]);
+    }
+    __syncthreads();
+    const int r16 = tid >> 5, ch = tid & 31, qr = ph * 16 + r16;
+    if (qr < rows) {
+      float M = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][qr].x);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 ml = s_ml[w][qr];
+        l += ml.x == -INFINITY ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - M);
+        const float4 y = xo[(w * 16 + r16) * 32 + (ch ^ r16)];
+        v.x += y.x;
+        v.y += y.y;
+        v.z += y.z;
+        v.w += y.w;
+      }
+      const float inv = l > 0.f ? 1.f / l : 0.f;   // a row without any key: 0
+      v.x *= inv;
+      v.y *= inv;
+      v.z *= inv;
+      v.w *= inv;
+      if (a.nsplit == 1) {
+        const int u = qr / G, h = g * G + (qr - u * G);
+        uint2 pk;
+        pk.x = f32_to_bf16_bits(v.x) | (f32_to_bf16_bits(v.y) << 16);
+        pk.y = f32_to_bf16_bits(v.z) | (f32_to_bf16_bits(v.w) << 16);
+        *reinterpret_cast<uint2*>(c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 4 * ch) = pk;
+        if (ch == 0 && c.lse)
+          c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l > 0.f ? (M + log2f(l)) * kLn2 : -INFINITY;
+      } else {
+        const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + qr;
+        *reinterpret_cast<float4*>(a.ws_o + at * kD + 4 * ch) = v;
+        if (ch == 0) a.ws_ml[at] = make_float2(M, l);
+      }
+    }
   }
 }
 
@@ -379,26 +689,35 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
 }  // namespace
 
 VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
+  // The estimated time is the number of rounds of workgroups over the CUs (one
+  // a CU) times a workgroup's steps and start-up, plus the combine launch of
+  // a split context.  The constants are in units of a SIMD's time for 32 rows
+  // x 64 keys with two waves per SIMD.
+  struct Shape { int blocks; bool narrow; int unit; double per_unit, start; };
+  const Shape shapes[] = {{1, true, kWaves * kStep, 2.0, 12.0},
+                          {2, true, kWaves * kStep, 4.0, 12.0},
+                          {4, false, kKeyTile, 1.0, 12.0},
+                          {8, false, kKeyTile, 2.0, 12.0}};
+  const int rows_max = T_max * (Hq / Hkv);
   VerifyKv4Plan best{};
-  const int G = Hq / Hkv;
-  const int rows_max = T_max * G;
-  const int tiles = (L_max + kKeyTile - 1) / kKeyTile;   // L_max is at most 2^30
   double best_cost = 0.0;
-  for (const int blocks : {8, 4}) {
-    const int rowgroups = (rows_max + blocks * 32 - 1) / (blocks * 32);
-    const int least = (tiles * kKeyTile + kMaxChunk - 1) / kMaxChunk;
-    const int most = std::max(least, std::min(64, tiles));
+  for (const Shape& s : shapes) {
+    const int rowgroups = (rows_max + s.blocks * 32 - 1) / (s.blocks * 32);
+    if (s.narrow && rowgroups > 1) continue;
+    if (!s.narrow && rows_max <= 64) continue;
+    const int units = (L_max + s.unit - 1) / s.unit;   // L_max is at most 2^30
+    const int least = (int)(((long)units * s.unit + kMaxChunk - 1) / kMaxChunk);
+    const int most = std::max(least, std::min(64, units));
     for (int want = least; want <= most; ++want) {
-      const int chunk = (tiles + want - 1) / want * kKeyTile;
-      const int nsplit = (tiles * kKeyTile + chunk - 1) / chunk;
+      const int chunk = (units + want - 1) / want * s.unit;
+      const int nsplit = (int)(((long)units * s.unit + chunk - 1) / chunk);
       if (nsplit != want) continue;   // the same split as a smaller count
       const double rounds = (double)(((long)B * Hkv * rowgroups * nsplit + 255) / 256);
-      const double per_tile = blocks == 8 ? 2.0 : 1.0;
-      const double cost = rounds * (per_tile * (chunk / kKeyTile + (T_max + kKeyTile - 1) / kKeyTile) + 12.0) +
-                          (nsplit > 1 ? 6.0 : 0.0);
+      const double tree = (double)((T_max + s.unit - 1) / s.unit);
+      const double cost = rounds * (s.per_unit * (chunk / s.unit + tree) + s.start) + (nsplit > 1 ? 6.0 : 0.0);
       if (best.blocks == 0 || cost < best_cost) {
         best_cost = cost;
-        best = VerifyKv4Plan{rows_max, blocks, rowgroups, nsplit, chunk};
+        best = VerifyKv4Plan{rows_max, s.blocks, rowgroups, nsplit, chunk};
       }
     }
   }
@@ -421,7 +740,11 @@ hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Pl
   a.ws_ml = c.ws ? reinterpret_cast<float2*>(static_cast<float*>(c.ws) + slots * kD) : nullptr;
   const int units = c.B * c.Hkv * p.nsplit;
   const dim3 grid((unsigned)((units + 7) / 8 * 8 * p.rowgroups));
-  if (p.blocks == 8) hipLaunchKernelGGL(kv4_verify_kernel<8>, grid, dim3(kThreads), 0, stream, a);
+  if (p.blocks == 1)
+    hipLaunchKernelGGL(kv4_narrow_kernel<1>, dim3((unsigned)units), dim3(kThreads), 0, stream, a);
+  else if (p.blocks == 2)
+    hipLaunchKernelGGL(kv4_narrow_kernel<2>, dim3((unsigned)units), dim3(kThreads), 0, stream, a);
+  else if (p.blocks == 8) hipLaunchKernelGGL(kv4_verify_kernel<8>, grid, dim3(kThreads), 0, stream, a);
   else hipLaunchKernelGGL(kv4_verify_kernel<4>, grid, dim3(kThreads), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
