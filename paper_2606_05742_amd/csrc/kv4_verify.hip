@@ -22,8 +22,8 @@ typedef __attribute__((address_space(3))) bf16x8_t lds_bf16x8_t;
 constexpr int kD = ADAPLD_HEAD_DIM;
 constexpr int kRowBytes = kD * 2;                 // one bf16 row in LDS
 constexpr int kTileBytes = kKeyTile * kRowBytes;  // 16 KiB for K (and for V)
-constexpr int kStageBytes = 2 * kTileBytes;
-constexpr int kStages = 2;
+constexpr int kStages = 4;                        // ring of tiles, a power of two
+constexpr int kVRegion = kStages * kTileBytes;    // the V tiles behind the K tiles
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kMaskWords = (ADAPLD_MAX_TREE_NODES + 63) / 64;
@@ -94,35 +94,41 @@ __device__ __forceinline__ void mask_keys(f32x16_t& s, int n, uint32_t bits) {
 // than kRescaleSlack (a factor 256), which keeps the rescale of the output off
 // the common path; the weights are rounded to bf16 once for the product and
 // summed before that in fp32.
-__device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, Block& x, bf16x8_t (&pb)[2]) {
+__device__ __forceinline__ float row_max(const f32x16_t& s) {
   float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
   for (int r = 3; r < 15; r += 2) mx = fmaxf(fmaxf(mx, s[r]), s[r + 1]);
   mx = fmaxf(mx, s[15]);
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
-  mx = fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1]));
-  const float mt = mx * sl2;   // scale > 0, so the max commutes with scaling
-  if (__ballot(mt > x.m + kRescaleSlack)) {
-    const float m_new = fmaxf(x.m, mt);
-    const float alpha = m_new == x.m ? 1.f : __builtin_amdgcn_exp2f(x.m - m_new);
-    x.m = m_new;
-    x.l *= alpha;
+  return fmaxf(__int_as_float(sw[0]), __int_as_float(sw[1]));
+}
+__device__ __forceinline__ void rescale_to(Block& x, float mt) {
+  const float m_new = fmaxf(x.m, mt);
+  const float alpha = m_new == x.m ? 1.f : __builtin_amdgcn_exp2f(x.m - m_new);
+  x.m = m_new;
+  x.l *= alpha;
 #pragma unroll
-    for (int db = 0; db < kD / 32; ++db) x.o[db] *= alpha;
+  for (int db = 0; db < kD / 32; ++db) x.o[db] *= alpha;
+}
+// The exponentials of values [8*s2, +8), added to psum.
+__device__ __forceinline__ void exp_part(const f32x16_t& s, int s2, float sl2, float m_use, bf16x8_t& pb, float& psum) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i], sl2, -m_use));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i + 1], sl2, -m_use));
+    psum += e0 + e1;
+    const bf16x2_t pk = __builtin_convertvector((f32x2_t){e0, e1}, bf16x2_t);
+    pb[i] = pk[0];
+    pb[i + 1] = pk[1];
   }
+}
+__device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, Block& x, bf16x8_t (&pb)[2]) {
+  const float mt = row_max(s) * sl2;   // scale > 0, so the max commutes with scaling
+  if (__ballot(mt > x.m + kRescaleSlack)) rescale_to(x, mt);
   const float m_use = x.m == -INFINITY ? 0.f : x.m;
   float psum = 0.f;
-#pragma unroll
-  for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i], sl2, -m_use));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(s[8 * s2 + i + 1], sl2, -m_use));
-      psum += e0 + e1;
-      const bf16x2_t pk = __builtin_convertvector((f32x2_t){e0, e1}, bf16x2_t);
-      pb[s2][i] = pk[0];
-      pb[s2][i + 1] = pk[1];
-    }
+  exp_part(s, 0, sl2, m_use, pb[0], psum);
+  exp_part(s, 1, sl2, m_use, pb[1], psum);
   x.l += psum;
 }
 
@@ -154,7 +160,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   static_assert(R == 8 || R == 4, "one or two waves per row block");
   constexpr int KH = kWaves / R;
   constexpr int HP = 2 / KH;   // 32-key halves of a tile that one wave takes
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kStages * kStageBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kVRegion];
   __shared__ uint64_t s_mask[ADAPLD_MAX_TREE_NODES * kMaskWords];
   __shared__ int s_pages[kMaxChunk / kMinPage + 1];
   const VerifyKv4Call& c = a.c;
@@ -213,7 +219,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   const int lkey = 16 * (wave & 3) + (lane & 15), lgrp = lane >> 4;
   const uint8_t* codes = is_v ? c.v_codes : c.k_codes;
   const uint8_t* scales = is_v ? c.v_scales : c.k_scales;
-  uint8_t* const lrow = smem + (is_v ? kTileBytes : 0) + lkey * kRowBytes;
+  uint8_t* const lrow = smem + (is_v ? kVRegion : 0) + lkey * kRowBytes;
   int lpos[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) lpos[j] = ((4 * lgrp + j) ^ swz(lkey)) << 4;
@@ -231,7 +237,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     x.e = scales[row * kKv4Scales + lgrp];
   };
   auto store = [&](int t, const Codes& x) {
-    uint8_t* p = lrow + (t % kStages) * kStageBytes;
+    uint8_t* p = lrow + (t % kStages) * kTileBytes;
     const float X = __uint_as_float(x.e << 23);
     const uint32_t w[4] = {x.c.x, x.c.y, x.c.z, x.c.w};
 #pragma unroll
@@ -241,9 +247,24 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     const int v = min((t - n_ctx) * kKeyTile + lkey, T - 1);
     const uint4* src = reinterpret_cast<const uint4*>((is_v ? c.v_tree : c.k_tree) +
                                                       (((size_t)b * c.T_max + v) * c.Hkv + g) * kD + lgrp * 32);
-    uint8_t* p = lrow + (t % kStages) * kStageBytes;
+    uint8_t* p = lrow + (t % kStages) * kTileBytes;
 #pragma unroll
     for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(p + lpos[j]) = src[j];
+  };
+  // Tile t + 1 to its stage while tile t is computed; the codes of tiles t + 2
+  // and t + 3 are in flight, those of even tiles in `even`.
+  Codes even{}, odd{};
+  auto advance = [&](int t, Codes& x) {
+    if (t + 1 < n_ctx) {
+      store(t + 1, x);
+      if (t + 3 < n_ctx) load(t + 3, x);
+    } else if (t + 1 < n_tiles) {
+      store_tree(t + 1);
+    }
+  };
+  auto advance_any = [&](int t) {
+    if (t & 1) advance(t, even);
+    else advance(t, odd);
   };
 
   // ---- LDS offsets of the fragments within a stage (kh: the wave's half)
@@ -251,61 +272,157 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   int kofs[kD / 16];
 #pragma unroll
   for (int ds = 0; ds < kD / 16; ++ds)
-    kofs[ds] = col * kRowBytes + (((2 * ds + half) ^ swz(col)) << 4);
+    kofs[ds] = half_off + col * kRowBytes + (((2 * ds + half) ^ swz(col)) << 4);
   int vofs[2][kD / 32];
   v_offsets(vofs);
+#pragma unroll
+  for (int db = 0; db < kD / 32; ++db) {
+    vofs[0][db] += half_off + kVRegion;
+    vofs[1][db] += half_off + kVRegion;
+  }
 
   Block x;
   block_init(x);
   const float sl2 = a.scale_log2;
 
-  auto compute = [&](int t, int hp) {
-    const lds_u8* base =
-        (const lds_u8*)smem + (t % kStages) * kStageBytes + half_off + (HP == 2 ? hp : 0) * 32 * kRowBytes;
-    f32x16_t s = f32x16_t{};
+  // The wave's half h lies in tile h / HP; with KH = 1 it covers keys
+  // [32*(h&1), +32) of that tile, with KH = 2 the wave's own half.  hs is h,
+  // or in the unrolled loop h modulo the ring's period, a constant: every LDS
+  // address is then a lane offset plus an immediate.
+  constexpr int kPeriod = HP * kStages;
+  auto base_of = [&](int hs) {
+    return (const lds_u8*)smem + ((hs / HP) % kStages) * kTileBytes + (HP == 2 ? (hs & 1) : 0) * 32 * kRowBytes;
+  };
+  auto qk = [&](int hs, f32x16_t& s) {
+    const lds_u8* base = base_of(hs);
+    s = f32x16_t{};
 #pragma unroll
     for (int ds = 0; ds < kD / 16; ++ds) {
       const bf16x8_t ka = *reinterpret_cast<const lds_bf16x8_t*>(base + kofs[ds]);
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[ds], s, 0, 0, 0);
     }
-    const int kb = 32 * (HP == 2 ? hp : kh);   // first key of the half
-    if (t >= n_ctx) {
-      const int k0 = (t - n_ctx) * kKeyTile;
-      const uint64_t mword = valid ? s_mask[u * a.nw + (k0 >> 6)] : 0ull;
-      mask_keys<true>(s, T - k0 - kb, (uint32_t)(mword >> kb));
-    } else if (c0 + (t + 1) * kKeyTile > c1) {
-      mask_keys<false>(s, c1 - c0 - t * kKeyTile - kb, 0u);
-    }
-    bf16x8_t pb[2];
-    softmax_step(s, sl2, x, pb);
+  };
+  auto pv = [&](int hs, const bf16x8_t (&pb)[2]) {
+    const lds_u8* base = base_of(hs);
 #pragma unroll
     for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
       for (int db = 0; db < kD / 32; ++db)
         x.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            v_fragment(base + kTileBytes + 16 * s2 * kRowBytes, vofs[0][db], vofs[1][db]), pb[s2], x.o[db], 0, 0, 0);
+            v_fragment(base + 16 * s2 * kRowBytes, vofs[0][db], vofs[1][db]), pb[s2], x.o[db], 0, 0, 0);
   };
+  auto mask = [&](int h, f32x16_t& s) {
+    const int t = h / HP, kb = 32 * (HP == 2 ? (h & 1) : kh);   // first key of the half
+    if (t >= n_ctx) {
+      const int k0 = (t - n_ctx) * kKeyTile;
+      const uint64_t mword = valid ? s_mask[u * a.nw + (k0 >> 6)] : 0ull;
+      mask_keys<true>(s, T - k0 - kb, (uint32_t)(mword >> kb));
+    } else {
+      mask_keys<false>(s, c1 - c0 - t * kKeyTile - kb, 0u);
+    }
+  };
+  // Publishes the tile that was written since the last one; the stage of the
+  // tile before the current one is free after it.  Loads stay in flight.
+  auto tile_barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-  // ---- tiles: codes of tile t + 2 are in flight and tile t + 1 is written
-  // to its stage while tile t is computed; one barrier a tile.
   __syncthreads();   // the page ids and the mask
-  Codes cur{}, nxt{};
   if (n_ctx > 0) {
-    load(0, cur);
-    if (n_ctx > 1) load(1, nxt);
-    store(0, cur);
+    load(0, even);
+    if (n_ctx > 1) load(1, odd);
+    store(0, even);
+    if (n_ctx > 2) load(2, even);
   } else if (n_tiles > 0) {
     store_tree(0);
   }
-  __syncthreads();
-  for (int t = 0; t < n_tiles; ++t) {
-    cur = nxt;
-    if (t + 2 < n_ctx) load(t + 2, nxt);
-    if (t + 1 < n_ctx) store(t + 1, cur);
-    else if (t + 1 < n_tiles) store_tree(t + 1);
-#pragma unroll
-    for (int hp = 0; hp < HP; ++hp) compute(t, hp);
-    __syncthreads();
+  tile_barrier();
+
+  const int H = HP * n_tiles;
+  const int n_plain = max(c1 - c0, 0) / kKeyTile;   // leading context tiles with no masked key
+  const int H_plain = HP * n_plain;
+  // A wave whose row block holds no valid row brings its share of every tile,
+  // takes every barrier, and does no math.
+  if (row_base + wrow * 32 >= rows) {
+    for (int t = 0; t + 1 < n_tiles; ++t) {
+      advance_any(t);
+      tile_barrier();
+    }
+  } else if (H > 0) {
+    f32x16_t s_cur, s_nxt;
+    bf16x8_t pb[2];
+    qk(0, s_cur);
+    if (H_plain == 0) mask(0, s_cur);
+    advance_any(0);
+    if (HP == 1 && H > 1) tile_barrier();   // half 1 is in tile 1
+    qk(1, s_nxt);
+    softmax_step(s_cur, sl2, x, pb);
+    s_cur = s_nxt;
+    // Half h: its softmax runs beside the products of P V of half h - 1 and of
+    // S of half h + 1.  (Past the last half qk reads a stale stage; unused.)
+    auto body = [&](int h, bool masked) {
+      if (h % HP == 0) advance_any(h / HP);
+      pv(h - 1, pb);
+      if (masked) mask(h, s_cur);
+      if (h % HP == HP - 1 && h + 1 < H) tile_barrier();
+      qk(h + 1, s_nxt);
+      softmax_step(s_cur, sl2, x, pb);
+      s_cur = s_nxt;
+    };
+    auto body_c = [&](auto J, int h) {
+      constexpr int j = decltype(J)::value;
+      pv((j + kPeriod - 1) % kPeriod, pb);
+      if constexpr (j % HP == 0) {
+        if constexpr ((j / HP) & 1) advance(h / HP, even);
+        else advance(h / HP, odd);
+      }
+      // The exponentials use the running max as it stands, eight products on
+      // either side of the tile barrier beside half of them each; the rare half
+      // whose max outgrows it by more than kRescaleSlack is done again.
+      const float mt = row_max(s_cur) * sl2;
+      const float m_use = x.m == -INFINITY ? 0.f : x.m;
+      float psum = 0.f;
+      bf16x8_t pn[2];
+      exp_part(s_cur, 0, sl2, m_use, pn[0], psum);
+      // Empty asm statements that consume the values pin each part to its side
+      // of the barrier; otherwise both sink below the check.
+      asm volatile("" ::"v"(pn[0]), "v"(psum));
+      if (j % HP == HP - 1 && h + 1 < H) tile_barrier();
+      qk((j + 1) % kPeriod, s_nxt);
+      exp_part(s_cur, 1, sl2, m_use, pn[1], psum);
+      asm volatile("" ::"v"(pn[1]), "v"(psum));
+      if (__ballot(mt > x.m + kRescaleSlack)) {
+        rescale_to(x, mt);
+        psum = 0.f;
+        exp_part(s_cur, 0, sl2, x.m, pn[0], psum);
+        exp_part(s_cur, 1, sl2, x.m, pn[1], psum);
+      }
+      x.l += psum;
+      pb[0] = pn[0];
+      pb[1] = pn[1];
+      s_cur = s_nxt;
+    };
+    int h = 1;
+    if constexpr (kPeriod == 8) {
+      for (; h + 8 <= H_plain; h += 8) {   // h = 1 (mod 8) here
+        body_c(std::integral_constant<int, 1>{}, h);
+        body_c(std::integral_constant<int, 2>{}, h + 1);
+        body_c(std::integral_constant<int, 3>{}, h + 2);
+        body_c(std::integral_constant<int, 4>{}, h + 3);
+        body_c(std::integral_constant<int, 5>{}, h + 4);
+        body_c(std::integral_constant<int, 6>{}, h + 5);
+        body_c(std::integral_constant<int, 7>{}, h + 6);
+        body_c(std::integral_constant<int, 0>{}, h + 7);
+      }
+    } else {
+      static_assert(kPeriod == 4, "one or two halves per tile, four stages");
+      for (; h + 4 <= H_plain; h += 4) {   // h = 1 (mod 4) here
+        body_c(std::integral_constant<int, 1>{}, h);
+        body_c(std::integral_constant<int, 2>{}, h + 1);
+        body_c(std::integral_constant<int, 3>{}, h + 2);
+        body_c(std::integral_constant<int, 0>{}, h + 3);
+      }
+    }
+    for (; h < H; ++h) body(h, h >= H_plain);
+    pv(H - 1, pb);
   }
 
   // ---- epilogue: lane holds dims db*32 + 8*(r/4) + 4*half + r%4 of its query row
@@ -315,8 +432,9 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     // state is relative to its own running max, the merged one to M.
     float4* xo = reinterpret_cast<float4*>(smem);                        // [R][16][64]
     float2* xml = reinterpret_cast<float2*>(s_mask);                     // [R][64]
-    static_assert(R * 16 * 64 * 16 <= kStages * kStageBytes && R * 64 <= ADAPLD_MAX_TREE_NODES * kMaskWords,
+    static_assert(R * 16 * 64 * 16 <= 2 * kVRegion && R * 64 <= ADAPLD_MAX_TREE_NODES * kMaskWords,
                   "the handed-over states fit");
+    __syncthreads();   // no wave reads the ring or the mask any more
     if (kh == 1) {
 #pragma unroll
       for (int db = 0; db < kD / 32; ++db)
