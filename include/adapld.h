@@ -646,8 +646,8 @@ int adapld_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uin
  *   k_codes, k_scales, v_codes, v_scales, page_table   the cache; a table entry
  *               of a page that holds a position below L must be a page of the
  *               pool (with any other the sequence's results are unspecified;
- *               nothing outside the cache is read); other entries and rows at
- *               or behind L are not read
+ *               nothing outside the cache is read); other entries, rows at or
+ *               behind L and queries at or behind T may hold anything
  *   k_tree, v_tree  bf16 [B, T_max, Hkv, D] or NULL
  *   lens, node_count, tree_mask   as in adapld_tree_verify_attn
  *   L_max       an upper bound of the lengths, at most max_pages * page_size;

@@ -162,21 +162,30 @@ def _stream(stream):
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(_current_device())
 
 
-def _same_device(**tensors):
-    """The calls on the 4-bit cache launch on the current device: every tensor
-    must live there."""
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not isinstance(t, _Tensor):
-            raise TypeError(f"{name} must be a torch.Tensor")
-        at = t.get_device()
-        if at < 0:
-            raise AdapldError(-2, f"{name} must live on the GPU (got {t.device})")
-        dev = _current_device() if dev is None else dev
-        if at != dev:
-            raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
+# The device that calls without a stream of another one launch on.
+_raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _dptr(t, name, dtypes, shape, dev, nullable=False):
+    """_ptr for the calls on the 4-bit cache, which launch on the current
+    device `dev`: the tensor must live there.  One that passes every check
+    takes one line of attribute reads."""
+    if (type(t) is _Tensor and t.get_device() == dev and t.dtype in dtypes and (shape is None or t.shape == shape)
+            and t.is_contiguous()):
+        return t.data_ptr()
+    p = _ptr(t, name, dtypes, shape, nullable)
+    if p is not None and t.get_device() != dev:
+        raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
+    return p
+
+
+def _device_of(t, name):
+    """The current device, for a call whose first tensor is t."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() < 0:
+        raise AdapldError(-2, f"{name} must live on the GPU (got {t.device})")
+    return _raw_device()
 
 
 def workspace_bytes(op, B, L_stride, d=0, k=0, T_max=0, Hq=0, Hkv=0, D=0) -> int:
@@ -464,7 +473,9 @@ class Kv4Cache:
     table of each sequence and the stack of free pages (adapld_kv4_*).  The
     buffers may be the caller's own, and those that no call uses None: page_map
     takes the table and the stack, the other calls the pool and (the attention)
-    the table.  allocate() makes an empty cache."""
+    the table.  allocate() makes an empty cache.  The buffers are checked and
+    their pointers marshalled at the first call, and again after one of the
+    fields is assigned."""
     k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
     k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
     v_codes: torch.Tensor
@@ -473,6 +484,11 @@ class Kv4Cache:
     free_pages: torch.Tensor    # int32 [n_pages], the stack
     free_count: torch.Tensor    # int32 [1]
     page_size: int
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_pool", None)
+        object.__setattr__(self, "_pages", None)
 
     @staticmethod
     def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
@@ -491,15 +507,34 @@ class Kv4Cache:
     def Hkv(self):
         return self.k_codes.shape[1]
 
-    def _arrays(self):
-        """Pointers of the pool's four arrays."""
-        _same_device(k_codes=self.k_codes, k_scales=self.k_scales, v_codes=self.v_codes, v_scales=self.v_scales)
-        u8 = (torch.uint8,)
-        D = 2 * self.k_codes.shape[-1]
-        codes = (self.n_pages, self.Hkv, self.page_size, D // 2)
-        scales = (self.n_pages, self.Hkv, self.page_size, D // KV4_GROUP)
-        return (_ptr(self.k_codes, "k_codes", u8, codes), _ptr(self.k_scales, "k_scales", u8, scales),
-                _ptr(self.v_codes, "v_codes", u8, codes), _ptr(self.v_scales, "v_scales", u8, scales))
+    def _marshal_pool(self, dev):
+        """(device, pointers of the four arrays, n_pages, Hkv, D)."""
+        if self._pool is None or self._pool[0] != dev:
+            u8 = (torch.uint8,)
+            _device_of(self.k_codes, "k_codes")
+            if self.k_codes.dim() != 4:
+                raise AdapldError(-2, f"k_codes has shape {tuple(self.k_codes.shape)}, expected 4 dimensions")
+            n_pages, Hkv, page_size, half = self.k_codes.shape
+            codes = (n_pages, Hkv, self.page_size, half)
+            scales = (n_pages, Hkv, self.page_size, 2 * half // KV4_GROUP)
+            ptrs = (_dptr(self.k_codes, "k_codes", u8, codes, dev), _dptr(self.k_scales, "k_scales", u8, scales, dev),
+                    _dptr(self.v_codes, "v_codes", u8, codes, dev), _dptr(self.v_scales, "v_scales", u8, scales, dev))
+            object.__setattr__(self, "_pool", (dev, ptrs, n_pages, Hkv, 2 * half))
+        return self._pool
+
+    def _marshal_pages(self, dev):
+        """(device, pointer of the page table, B, max_pages)."""
+        if self._pages is None or self._pages[0] != dev:
+            _device_of(self.page_table, "page_table")
+            B, max_pages = self.page_table.shape
+            object.__setattr__(self, "_pages", (dev, _dptr(self.page_table, "page_table", _I32, (B, max_pages), dev), B, max_pages))
+        return self._pages
+
+
+_I32 = (torch.int32,)
+_F32 = (torch.float32,)
+_U8 = (torch.uint8,)
+_MASK = (torch.int64, torch.uint64)
 
 
 def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, granted=None, free_count_out=None,
@@ -508,23 +543,23 @@ def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, gran
     slots of their first N new ones (N from slot_map if it is given); returns
     (slot_map, granted).  The cache's page_table and stack are updated; the
     stack's count goes to free_count_out (default: in place)."""
-    B, max_pages = cache.page_table.shape
-    n_pages = cache.free_pages.shape[0]
-    dev = cache.page_table.device
-    i32 = (torch.int32,)
+    dev = _device_of(lens_old, "lens_old")
+    _, table, B, max_pages = cache._marshal_pages(dev)
     if slot_map is None:
-        slot_map = torch.empty((B, 0 if N is None else N), dtype=torch.int32, device=dev)
+        slot_map = torch.empty((B, 0 if N is None else N), dtype=torch.int32, device=lens_old.device)
     N = slot_map.shape[1] if N is None else N
-    granted = _i32(B, dev) if granted is None else granted
-    free_count_out = cache.free_count if free_count_out is None else free_count_out
-    _same_device(page_table=cache.page_table, free_pages=cache.free_pages, free_count=cache.free_count,
-                 free_count_out=free_count_out, lens_old=lens_old, lens_new=lens_new, slot_map=slot_map, granted=granted)
+    granted = _i32(B, lens_old.device) if granted is None else granted
+    free_count = cache.free_count
+    count = _dptr(free_count, "free_count", _I32, (1,), dev)
+    count_out = count if free_count_out is None else _dptr(free_count_out, "free_count_out", _I32, (1,), dev)
+    n_pages = cache.free_pages.shape[0]
     st = load_library().adapld_kv4_page_map(
-        _ptr(lens_old, "lens_old", i32, (B,)), _ptr(lens_new, "lens_new", i32, (B,)), B, cache.page_size, max_pages,
-        n_pages, N, _ptr(cache.page_table, "page_table", i32), _ptr(cache.free_pages, "free_pages", i32), _ptr(cache.free_count, "free_count", i32, (1,)),
-        _ptr(free_count_out, "free_count_out", i32, (1,)), _ptr(slot_map, "slot_map", i32, (B, N)),
-        _ptr(granted, "granted", i32, (B,)), _stream(stream))
-    _check(st, "adapld_kv4_page_map")
+        _dptr(lens_old, "lens_old", _I32, (B,), dev), _dptr(lens_new, "lens_new", _I32, (B,), dev), B,
+        cache.page_size, max_pages, n_pages, N, table, _dptr(cache.free_pages, "free_pages", _I32, (n_pages,), dev),
+        count, count_out, _dptr(slot_map, "slot_map", _I32, (B, N), dev), _dptr(granted, "granted", _I32, (B,), dev),
+        _stream(stream))
+    if st:
+        _check(st, "adapld_kv4_page_map")
     return slot_map, granted
 
 
@@ -532,34 +567,39 @@ def kv4_append(cache: Kv4Cache, k_new, v_new, slot_map, *, rows=None, stream=Non
     """Quantises K/V rows (bf16 [B, n_src, Hkv, D]) into the cache: row
     rows[b, i] (row i without rows) of sequence b at slot_map[b, i]; slots of
     -1 are padding."""
-    B, n_src, Hkv, D = k_new.shape
+    dev = _device_of(k_new, "k_new")
+    _, pool, n_pages, Hkv, _ = cache._marshal_pool(dev)
+    shape = k_new.shape
+    B, n_src, heads, D = shape
     N = slot_map.shape[1]
-    if Hkv != cache.Hkv:
-        raise AdapldError(-2, f"k_new has {Hkv} kv heads, the cache {cache.Hkv}")
-    _same_device(k_new=k_new, v_new=v_new, rows=rows, slot_map=slot_map)
+    if heads != Hkv:
+        raise AdapldError(-2, f"k_new has {heads} kv heads, the cache {Hkv}")
     st = load_library().adapld_kv4_append(
-        _ptr(k_new, "k_new", _BF16_DTYPES), _ptr(v_new, "v_new", _BF16_DTYPES, (B, n_src, Hkv, D)),
-        _ptr(rows, "rows", (torch.int32,), (B, N), nullable=True), _ptr(slot_map, "slot_map", (torch.int32,), (B, N)),
-        B, n_src, N, Hkv, D, cache.page_size, cache.n_pages, *cache._arrays(), _stream(stream))
-    _check(st, "adapld_kv4_append")
+        _dptr(k_new, "k_new", _BF16_DTYPES, None, dev), _dptr(v_new, "v_new", _BF16_DTYPES, shape, dev),
+        None if rows is None else _dptr(rows, "rows", _I32, (B, N), dev),
+        _dptr(slot_map, "slot_map", _I32, (B, N), dev), B, n_src, N, Hkv, D, cache.page_size, n_pages, *pool,
+        _stream(stream))
+    if st:
+        _check(st, "adapld_kv4_append")
 
 
 def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None):
     """The cache's rows at slot_map (int32 [B, N]) as bf16 [B, N, Hkv, D];
     returns (k_out, v_out).  Rows of slots outside the pool are left as they
     are (zero in new outputs)."""
+    dev = _device_of(slot_map, "slot_map")
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
     B, N = slot_map.shape
-    D = 2 * cache.k_codes.shape[-1]
-    shape = (B, N, cache.Hkv, D)
+    shape = (B, N, Hkv, D)
     new = lambda: torch.zeros(shape, dtype=torch.bfloat16, device=slot_map.device)  # noqa: E731
     k_out = new() if k_out is None else k_out
     v_out = new() if v_out is None else v_out
-    _same_device(slot_map=slot_map, k_out=k_out, v_out=v_out)
     st = load_library().adapld_kv4_gather(
-        *cache._arrays(), _ptr(slot_map, "slot_map", (torch.int32,)), B, N, cache.Hkv, D, cache.page_size,
-        cache.n_pages, _ptr(k_out, "k_out", _BF16_DTYPES, shape), _ptr(v_out, "v_out", _BF16_DTYPES, shape),
+        *pool, _dptr(slot_map, "slot_map", _I32, None, dev), B, N, Hkv, D, cache.page_size, n_pages,
+        _dptr(k_out, "k_out", _BF16_DTYPES, shape, dev), _dptr(v_out, "v_out", _BF16_DTYPES, shape, dev),
         _stream(stream))
-    _check(st, "adapld_kv4_gather")
+    if st:
+        _check(st, "adapld_kv4_gather")
     return k_out, v_out
 
 
@@ -569,34 +609,35 @@ def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v
     v_tree and tree_mask every row attends to the context alone.  L_max bounds
     the lengths (default: what the page table holds).  Returns (out, lse)."""
     lib = load_library()
-    B, T_max, Hq, D = q.shape
-    Hkv, max_pages = cache.Hkv, cache.page_table.shape[1]
-    dev = q.device
+    dev = _device_of(q, "q")
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
+    _, table, B, max_pages = cache._marshal_pages(dev)
+    shape = q.shape
+    if len(shape) != 4 or shape[0] != B or shape[3] != D:
+        raise AdapldError(-2, f"q has shape {tuple(shape)}, expected ({B}, T_max, Hq, {D})")
+    T_max, Hq = shape[1], shape[2]
     L_max = max_pages * cache.page_size if L_max is None else L_max
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    out = torch.empty((B, T_max, Hq, D), dtype=torch.bfloat16, device=dev) if out is None else out
+    out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if out is None else out
     if lse is None and with_lse:
-        lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=dev)
+        lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=q.device)
     if ws is None:
         need = workspace_bytes(OP_TREE_VERIFY_ATTN_KV4, B, L_max, 0, 0, T_max, Hq, Hkv, D)
-        ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
-    nw = (T_max + 63) // 64
-    if D != 2 * cache.k_codes.shape[-1]:
-        raise AdapldError(-2, f"q has head dimension {D}, the cache {2 * cache.k_codes.shape[-1]}")
-    _same_device(q=q, page_table=cache.page_table, lens=lens, node_count=node_count, k_tree=k_tree, v_tree=v_tree,
-                 tree_mask=tree_mask, out=out, lse=lse, ws=ws)
+        ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    kt = vt = mask = None
+    if k_tree is not None or v_tree is not None or tree_mask is not None:
+        tree = (B, T_max, Hkv, D)
+        kt = _dptr(k_tree, "k_tree", _BF16_DTYPES, tree, dev)
+        vt = _dptr(v_tree, "v_tree", _BF16_DTYPES, tree, dev)
+        mask = _dptr(tree_mask, "tree_mask", _MASK, (B, T_max, (T_max + 63) // 64), dev)
     st = lib.adapld_tree_verify_attn_kv4(
-        _ptr(q, "q", _BF16_DTYPES), *cache._arrays(),
-        _ptr(cache.page_table, "page_table", (torch.int32,), (B, max_pages)),
-        _ptr(k_tree, "k_tree", _BF16_DTYPES, (B, T_max, Hkv, D), nullable=True),
-        _ptr(v_tree, "v_tree", _BF16_DTYPES, (B, T_max, Hkv, D), nullable=True),
-        _ptr(lens, "lens", (torch.int32,), (B,)), _ptr(node_count, "node_count", (torch.int32,), (B,)),
-        _ptr(tree_mask, "tree_mask", (torch.int64, torch.uint64), (B, T_max, nw), nullable=True),
-        B, L_max, T_max, Hq, Hkv, D, cache.page_size, cache.n_pages, max_pages, float(scale),
-        _ptr(out, "out", _BF16_DTYPES, (B, T_max, Hq, D)),
-        _ptr(lse, "lse", (torch.float32,), (B, Hq, T_max), nullable=True),
-        _ptr(ws, "ws", (torch.uint8,)), ws.numel(), _stream(stream))
-    _check(st, "adapld_tree_verify_attn_kv4")
+        _dptr(q, "q", _BF16_DTYPES, None, dev), *pool, table, kt, vt, _dptr(lens, "lens", _I32, (B,), dev),
+        _dptr(node_count, "node_count", _I32, (B,), dev), mask, B, L_max, T_max, Hq, Hkv, D, cache.page_size, n_pages,
+        max_pages, scale, _dptr(out, "out", _BF16_DTYPES, shape, dev),
+        None if lse is None else _dptr(lse, "lse", _F32, (B, Hq, T_max), dev),
+        _dptr(ws, "ws", _U8, None, dev), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "adapld_tree_verify_attn_kv4")
     return out, lse
 
 

@@ -59,6 +59,25 @@ __device__ __forceinline__ uint4 dequant8(uint32_t c, float X) {
   return r;
 }
 
+// The page ids of a split's keys [c0, c0 + chunk) on their way to LDS (entries
+// of the sequence's table row only).  The first of each thread is requested by
+// begin(), before the queries: loads return in order, and the codes wait for
+// the page ids alone.
+struct PageLoad {
+  const int32_t* row;
+  int n, first;
+  __device__ __forceinline__ void begin(const Kv4Args& a, int b, int c0) {
+    const int p0 = c0 >> a.page_shift;
+    n = min(((c0 + a.chunk - 1) >> a.page_shift) - p0 + 1, a.c.max_pages - p0);
+    row = a.c.page_table + (size_t)b * a.c.max_pages + p0;
+    first = row[min((int)threadIdx.x, n - 1)];
+  }
+  __device__ __forceinline__ void finish(int n_pages, int* s_pages) {
+    if ((int)threadIdx.x < n) s_pages[threadIdx.x] = kv4_page_in_pool(first, n_pages);
+    for (int i = threadIdx.x + kThreads; i < n; i += kThreads) s_pages[i] = kv4_page_in_pool(row[i], n_pages);
+  }
+};
+
 // ------------------------------------------------- one 32-row block's softmax
 //
 // S^T = K Q^T on v_mfma_f32_32x32x16_bf16 (A = 32 keys, B = 32 query rows)
@@ -174,44 +193,46 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   const int b = bg / c.Hkv, g = bg - b * c.Hkv;
   if (b >= c.B) return;
   const int G = a.G;
-  const int T = min(max(c.node_count[b], 0), c.T_max);
-  const int L = min(max(c.lens[b], 0), c.L_max);
-  const int rows = T * G;
   const int row_base = rg * (R * 32);
-  if (row_base >= rows) return;
-  const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, L);
-  const bool do_tree = split == a.nsplit - 1 && c.k_tree;
-  const int n_ctx = c1 > c0 ? (c1 - c0 + kKeyTile - 1) / kKeyTile : 0;
-  const int n_tiles = n_ctx + (do_tree ? (T + kKeyTile - 1) / kKeyTile : 0);
-
   const int tid = threadIdx.x;
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int wrow = wave % R, kh = wave / R;
   const int col = lane & 31, half = lane >> 5;
 
-  // ---- page ids of the split and the tree's mask to LDS
-  const int p0 = c0 >> a.page_shift;
-  if (n_ctx > 0) {
-    const int np = ((c1 - 1) >> a.page_shift) - p0 + 1;
-    for (int i = tid; i < np; i += kThreads)
-      s_pages[i] = kv4_page_in_pool(c.page_table[(size_t)b * c.max_pages + p0 + i], c.n_pages);
-  }
-  if (do_tree)
-    for (int i = tid; i < T * a.nw; i += kThreads) s_mask[i] = c.tree_mask[(size_t)b * c.T_max * a.nw + i];
-
-  // ---- query fragments (B operand): lane holds dims [16*ds + 8*half, +8) of its row
+  // ---- one memory round trip for everything that no other load decides: the
+  // lengths, the page ids of a full split, the queries of a full tree and its
+  // mask (what lies behind the sequence's own length and nodes goes unused).
+  const int c0 = split * a.chunk;
+  PageLoad pages;
+  pages.begin(a, b, c0);
+  const int nodes = c.node_count[b], len = c.lens[b];
+  // Query fragments (B operand): lane holds dims [16*ds + 8*half, +8) of its row.
   const int qr = row_base + wrow * 32 + col;
-  const bool valid = qr < rows;
-  const int u = valid ? qr / G : 0;
-  const int h = g * G + (valid ? qr - u * G : 0);
+  const int u = qr < a.rows_max ? qr / G : 0;
+  const int h = g * G + (qr < a.rows_max ? qr - u * G : 0);
   bf16x8_t qf[kD / 16];
   {
     const uint16_t* qp = c.q + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 8 * half;
 #pragma unroll
-    for (int ds = 0; ds < kD / 16; ++ds)
-      qf[ds] = as_bf16x8(valid ? *reinterpret_cast<const uint4*>(qp + 16 * ds) : make_uint4(0, 0, 0, 0));
+    for (int ds = 0; ds < kD / 16; ++ds) qf[ds] = as_bf16x8(*reinterpret_cast<const uint4*>(qp + 16 * ds));
   }
+  pages.finish(c.n_pages, s_pages);
+  const bool do_tree = split == a.nsplit - 1 && c.k_tree;
+  if (do_tree)
+    for (int i = tid; i < c.T_max * a.nw; i += kThreads) s_mask[i] = c.tree_mask[(size_t)b * c.T_max * a.nw + i];
+  const int T = min(max(nodes, 0), c.T_max);
+  const int L = min(max(len, 0), c.L_max);
+  const int rows = T * G;
+  if (row_base >= rows) return;
+  const bool valid = qr < rows;
+#pragma unroll
+  for (int ds = 0; ds < kD / 16; ++ds)
+    if (!valid) qf[ds] = as_bf16x8(make_uint4(0, 0, 0, 0));
+  const int c1 = min(c0 + a.chunk, L);
+  const int n_ctx = c1 > c0 ? (c1 - c0 + kKeyTile - 1) / kKeyTile : 0;
+  const int n_tiles = n_ctx + (do_tree ? (T + kKeyTile - 1) / kKeyTile : 0);
+  const int p0 = c0 >> a.page_shift;
 
   // ---- loader: waves 0-3 bring K, waves 4-7 V; a lane one group of 32
   // dimensions (16 bytes of codes) of one key.
@@ -519,49 +540,47 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_narrow_kernel(const Kv4Args a
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
   const int b = bg / c.Hkv, g = bg - b * c.Hkv;
   const int G = a.G;
-  const int T = min(max(c.node_count[b], 0), c.T_max);
-  const int L = min(max(c.lens[b], 0), c.L_max);
-  const int rows = T * G;
-  if (rows == 0) return;
-  const int c0 = split * a.chunk, c1 = min(c0 + a.chunk, L);
-  const bool do_tree = split == a.nsplit - 1 && c.k_tree;
-  const int n_ctx = c1 > c0 ? (c1 - c0 + kStep - 1) / kStep : 0;
-  const int n_steps = n_ctx + (do_tree ? (T + kStep - 1) / kStep : 0);
-
   const int tid = threadIdx.x;
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane & 31, half = lane >> 5;
 
-  const int p0 = c0 >> a.page_shift;
-  if (n_ctx > 0) {
-    const int np = ((c1 - 1) >> a.page_shift) - p0 + 1;
-    for (int i = tid; i < np; i += kThreads)
-      s_pages[i] = kv4_page_in_pool(c.page_table[(size_t)b * c.max_pages + p0 + i], c.n_pages);
-  }
-
+  // One memory round trip, as in the tile kernel.
+  const int c0 = split * a.chunk;
+  const bool do_tree = split == a.nsplit - 1 && c.k_tree;
+  PageLoad pages;
+  pages.begin(a, b, c0);
+  const int T = min(max(c.node_count[b], 0), c.T_max);
+  const int L = min(max(c.lens[b], 0), c.L_max);
+  const int rows = T * G;
   // Query fragment (i, j): dims [32 * (2i + half) + 8j, +8) of the lane's row.
   bf16x8_t qf[kQInLds ? 1 : NB][2][4];
   uint64_t sees[NB];
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     const int qr = nb * 32 + col;
-    const bool valid = qr < rows;
-    const int u = valid ? qr / G : 0;
-    const int h = g * G + (valid ? qr - u * G : 0);
+    const int u = qr < a.rows_max ? qr / G : 0;
+    const int h = g * G + (qr < a.rows_max ? qr - u * G : 0);
     const uint16_t* qp = c.q + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 32 * half;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         if (!kQInLds || wave == nb * 4 + i * 2 + j / 2) {
-          const uint4 w = valid ? *reinterpret_cast<const uint4*>(qp + 64 * i + 8 * j) : make_uint4(0, 0, 0, 0);
+          uint4 w = *reinterpret_cast<const uint4*>(qp + 64 * i + 8 * j);
+          if (qr >= rows) w = make_uint4(0, 0, 0, 0);
           if constexpr (kQInLds) s_q[((nb * 2 + i) * 4 + j) * kWave + lane] = w;
           else qf[nb][i][j] = as_bf16x8(w);
         }
     // at most 64 rows, so at most 64 nodes and one mask word
-    sees[nb] = do_tree && valid ? c.tree_mask[(size_t)b * c.T_max + u] : 0ull;
+    sees[nb] = do_tree ? c.tree_mask[(size_t)b * c.T_max + u] : 0ull;
   }
+  pages.finish(c.n_pages, s_pages);
+  if (rows == 0) return;
+  const int c1 = min(c0 + a.chunk, L);
+  const int n_ctx = c1 > c0 ? (c1 - c0 + kStep - 1) / kStep : 0;
+  const int n_steps = n_ctx + (do_tree ? (T + kStep - 1) / kStep : 0);
+  const int p0 = c0 >> a.page_shift;
 
   Block x[NB];
 #pragma unroll
@@ -774,22 +793,33 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
   if (qr >= T * a.G) return;
   const int dim = (threadIdx.x & 31) * 4;
   const size_t row0 = (size_t)bg * a.nsplit * a.rows_max + qr;
+  // In index order, eight splits' loads in flight at a time.
   float M = -INFINITY, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < a.nsplit; ++s) {
-    const size_t at = row0 + (size_t)s * a.rows_max;
-    const float2 ml = a.ws_ml[at];
-    const float4 v = *reinterpret_cast<const float4*>(a.ws_o + at * kD + dim);
-    if (ml.y > 0.f) {
-      const float m_new = fmaxf(M, ml.x);
-      const float keep = exp2f(M - m_new);   // 0 while nothing has been merged
-      const float w = ml.y * exp2f(ml.x - m_new);
-      num.x = fmaf(num.x, keep, w * v.x);
-      num.y = fmaf(num.y, keep, w * v.y);
-      num.z = fmaf(num.z, keep, w * v.z);
-      num.w = fmaf(num.w, keep, w * v.w);
-      den = fmaf(den, keep, w);
-      M = m_new;
+  constexpr int kGroup = 8;
+  for (int s0 = 0; s0 < a.nsplit; s0 += kGroup) {
+    float2 ml[kGroup];
+    float4 v[kGroup];
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+      const bool in = s0 + j < a.nsplit;
+      const size_t at = row0 + (size_t)(s0 + j) * a.rows_max;
+      ml[j] = in ? a.ws_ml[at] : make_float2(-INFINITY, 0.f);
+      v[j] = in ? *reinterpret_cast<const float4*>(a.ws_o + at * kD + dim) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < kGroup; ++j) {
+      if (ml[j].y > 0.f) {
+        const float m_new = fmaxf(M, ml[j].x);
+        const float keep = exp2f(M - m_new);   // 0 while nothing has been merged
+        const float w = ml[j].y * exp2f(ml[j].x - m_new);
+        num.x = fmaf(num.x, keep, w * v[j].x);
+        num.y = fmaf(num.y, keep, w * v[j].y);
+        num.z = fmaf(num.z, keep, w * v[j].z);
+        num.w = fmaf(num.w, keep, w * v[j].w);
+        den = fmaf(den, keep, w);
+        M = m_new;
+      }
     }
   }
   const int g = (int)bg - b * c.Hkv;
