@@ -177,7 +177,7 @@ hipError_t launch_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, co
 // How the verify attention over the 4-bit cache decomposes a problem.
 struct VerifyKv4Plan {
   int rows_max;    // T_max * G stacked query rows per (sequence, kv head)
-  int blocks;      // 32-row blocks per workgroup
+  int rows;        // stacked rows per workgroup: 16, 32, 64 (narrow kernel), 128 or 256
   int rowgroups;   // workgroups along the rows
   int nsplit;      // context splits
   int chunk;       // context keys per split (multiple of kKeyTile)

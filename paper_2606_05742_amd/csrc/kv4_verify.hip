@@ -12,6 +12,7 @@ namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
@@ -32,6 +33,7 @@ constexpr int kMinPage = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleSlack = 8.0f;             // log2 units the running max may lag
+constexpr float kWeightLimit = 16777216.0f;       // sum of one lane's weights of a step that moves the max
 
 struct Kv4Args {
   VerifyKv4Call c;
@@ -41,11 +43,19 @@ struct Kv4Args {
   float2* ws_ml;   // [B*Hkv][nsplit][rows_max]     (running max in log2 units, sum)
 };
 
-// Physical 16-byte chunk of logical chunk c in key row r is c ^ swz(r): a
-// bijection on every 16 consecutive rows, so 16 lanes that read (K fragments)
-// or write (the loader) one chunk of 16 rows touch all 64 banks; and the rows
-// of a transposed V read fall into different quarters of the bank row.
-__device__ __forceinline__ int swz(int r) { return ((r & 3) << 2) | ((r >> 2) & 3); }
+// Physical 16-byte chunk of logical chunk c in key row r is c ^ swz(r).  LDS has 64
+// four-byte banks for reads (a 256-byte row once around); 16-byte writes go by
+// 8 lanes over 32 of them.  With r = r3 r2 r1 r0 the swizzle is (r1, r0, r1 ^ r3,
+// r2): a bijection on 16 rows (K fragments: 16 lanes read one chunk of 16 rows),
+// its low three bits one on every aligned 8 (the loader: 8 lanes write one chunk
+// of 8 rows), its high two on every aligned 4 (transposed V reads: 32 lanes cover
+// 64 bytes of 4 rows).  All three are free of bank conflicts.
+__device__ __forceinline__ int swz(int r) {
+  return ((r & 3) << 2) | ((((r >> 1) ^ (r >> 3)) & 1) << 1) | ((r >> 2) & 1);
+}
+// The same for transposed reads in which 32 lanes cover 32 bytes of 8 rows:
+// (r2, r1, r0, r2 ^ r3), its high three bits a bijection on every aligned 8.
+__device__ __forceinline__ int swz16(int r) { return ((r & 7) << 1) | (((r >> 2) ^ (r >> 3)) & 1); }
 
 __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8_t, v); }
 
@@ -57,6 +67,17 @@ __device__ __forceinline__ uint4 dequant8(uint32_t c, float X) {
   r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 2));
   r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 3));
   return r;
+}
+
+// 16 bytes of codes; STREAM for data that nothing reads again.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
+  const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p);
+  u32x4_t v;
+  if constexpr (STREAM) v = __builtin_nontemporal_load(q);
+  else v = *q;
+  return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // The page ids of a split's keys [c0, c0 + chunk) on their way to LDS (entries
@@ -396,22 +417,22 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
         else advance(h / HP, odd);
       }
       // The exponentials use the running max as it stands, eight products on
-      // either side of the tile barrier beside half of them each; the rare half
-      // whose max outgrows it by more than kRescaleSlack is done again.
-      const float mt = row_max(s_cur) * sl2;
-      const float m_use = x.m == -INFINITY ? 0.f : x.m;
+      // either side of the tile barrier beside half of them each.  A weight's
+      // scale costs no accuracy, so the max is not even looked for unless a lane's
+      // weights of the half sum up to kWeightLimit: then the half is done again
+      // with the max moved.
       float psum = 0.f;
       bf16x8_t pn[2];
-      exp_part(s_cur, 0, sl2, m_use, pn[0], psum);
+      exp_part(s_cur, 0, sl2, x.m, pn[0], psum);
       // Empty asm statements that consume the values pin each part to its side
       // of the barrier; otherwise both sink below the check.
       asm volatile("" ::"v"(pn[0]), "v"(psum));
       if (j % HP == HP - 1 && h + 1 < H) tile_barrier();
       qk((j + 1) % kPeriod, s_nxt);
-      exp_part(s_cur, 1, sl2, m_use, pn[1], psum);
+      exp_part(s_cur, 1, sl2, x.m, pn[1], psum);
       asm volatile("" ::"v"(pn[1]), "v"(psum));
-      if (__ballot(mt > x.m + kRescaleSlack)) {
-        rescale_to(x, mt);
+      if (__ballot(psum > kWeightLimit)) {
+        rescale_to(x, row_max(s_cur) * sl2);
         psum = 0.f;
         exp_part(s_cur, 0, sl2, x.m, pn[0], psum);
         exp_part(s_cur, 1, sl2, x.m, pn[1], psum);
@@ -514,28 +535,239 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
 
 // ------------------------------------------------------------- up to 64 rows
 //
-// With one or two 32-row blocks (single tokens, one copied chain) the call is
-// one pass over the cache, so no two waves share keys: wave w of 8 takes the
-// 32-key steps w, w + 8, ... of the split, alone, without a barrier.  K codes
-// go from memory straight to the A fragments: the order of the dimensions in
-// the products is free, so a lane's 16 bytes (one group of 32 dimensions of one
-// key, one scale) are four fragments, and Q is loaded in the same order.  V
-// codes become bf16 rows in 8 KiB of LDS that the wave has for itself, from
-// which they are read transposed.  Codes of two steps are in flight.  At the
-// end the waves' states are merged through LDS.
+// With few rows (single tokens, one copied chain) the call is one pass over the
+// cache, so waves share no keys: of the 8 waves, 8 / RB take the 32-key steps of
+// the split in turn for each of RB row blocks, alone, without a barrier.  16
+// rows run on 16x16x32 products, 32 and 64 in blocks of 32 on 32x32x16 ones.
+//
+// Lane (quad, col) brings group `quad` (16 bytes of codes, one scale) of keys col
+// and 16 + col.  K codes become A fragments in registers: the order of the
+// dimensions in the products is free, so a group is four fragments, and Q is
+// loaded in the same order.  V codes become bf16 rows in LDS that the wave has
+// for itself, from which they are read transposed.  16 keys never cross a page,
+// so their page id is a scalar (a lane of a register holds it for each of the
+// next 64 steps) and every address a scalar base plus a fixed lane offset.
+//
+// Codes of two steps are in flight, and the conversion and products S of one
+// step run beside the softmax and products O of the step before it (two V
+// buffers): the products then hide behind the conversions and exponentials of
+// the same wave.  At the end the waves' states are merged through LDS.
 constexpr int kStep = 32;
-constexpr int kWaveLds = kStep * kRowBytes;   // 8 KiB
+constexpr int kVBuffer = kStep * kRowBytes;   // 8 KiB
 
-template <int NB>
-__global__ __launch_bounds__(kThreads, 1) void kv4_narrow_kernel(const Kv4Args a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * kWaveLds];
-  __shared__ float2 s_ml[kWaves][NB * 32];
-  __shared__ int s_pages[kMaxChunk / kMinPage + 1];
-  // Two blocks' query fragments do not fit the registers beside their outputs:
-  // all waves read them from here, 16 bytes a lane.
-  constexpr bool kQInLds = NB == 2;
-  constexpr int kDepth = NB == 2 ? 1 : 2;   // steps whose codes are in flight
-  __shared__ uint4 s_q[kQInLds ? NB * 8 * kWave : 1];
+// A block of 16 rows on v_mfma_f32_16x16x32_bf16: a lane owns row `col` and the
+// keys 16*i + 4*quad + r (value r of tile i), again in the order of P's operand.
+struct Rows16 {
+  static constexpr int kRows = 16;
+  struct Logits {
+    f32x4_t v[2];
+  };
+  typedef bf16x8_t Weights;
+  float m, l;
+  f32x4_t o[kD / 16];   // value r is dim 16*db + 4*quad + r
+  bf16x8_t q[4];
+  int vofs[kD / 16];
+
+  __device__ __forceinline__ void init() {
+    m = -INFINITY;
+    l = 0.f;
+    const int col = lane_id() & 15, key = 4 * (lane_id() >> 4) + (col >> 2);
+#pragma unroll
+    for (int db = 0; db < kD / 16; ++db) {
+      o[db] = f32x4_t{};
+      // 4 keys x 16 dims by each 16 lanes; the next 16 keys lie 16 rows on,
+      // where the swizzle repeats
+      vofs[db] = key * kRowBytes + (((2 * db + ((col & 3) >> 1)) ^ swizzle(key)) << 4) + (col & 1) * 8;
+    }
+  }
+  static __device__ __forceinline__ int swizzle(int r) { return swz16(r); }
+  static __device__ __forceinline__ int row() { return lane_id() & 15; }
+  static __device__ __forceinline__ bool first_of_row() { return lane_id() < 16; }
+  __device__ __forceinline__ void load_q(const uint16_t* p, bool valid) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint4 w = *reinterpret_cast<const uint4*>(p + 32 * (lane_id() >> 4) + 8 * j);
+      if (!valid) w = make_uint4(0, 0, 0, 0);
+      q[j] = as_bf16x8(w);
+    }
+  }
+  // Codes as loaded are in order: part i is group quad of key 16*i + col.
+  static __device__ __forceinline__ void order_codes(uint4 (&)[2], uint32_t (&)[2]) {}
+  static __device__ __forceinline__ int key_of(int i) { return 16 * i + (lane_id() & 15); }
+  static __device__ __forceinline__ int dim_of(int) { return 32 * (lane_id() >> 4); }
+
+  template <class K>
+  __device__ __forceinline__ void products_s(K&& ka, Logits& s) const {
+    s.v[0] = s.v[1] = f32x4_t{};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s.v[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka(i, j), q[j], s.v[i], 0, 0, 0);
+  }
+  template <bool TREE>
+  static __device__ __forceinline__ void mask(Logits& s, int n, uint32_t bits) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int key = 16 * i + 4 * (lane_id() >> 4) + r;
+        s.v[i][r] = key < n && (!TREE || ((bits >> key) & 1u)) ? s.v[i][r] : -INFINITY;
+      }
+  }
+  __device__ __forceinline__ void move_max(const Logits& s, float sl2) {
+    float mx = fmaxf(fmaxf(s.v[0][0], s.v[0][1]), s.v[0][2]);
+    mx = fmaxf(fmaxf(mx, s.v[0][3]), s.v[1][0]);
+    mx = fmaxf(fmaxf(mx, s.v[1][1]), s.v[1][2]);
+    mx = fmaxf(mx, s.v[1][3]);
+    const auto w32 = __builtin_amdgcn_permlane32_swap(__float_as_int(mx), __float_as_int(mx), false, false);
+    mx = fmaxf(__int_as_float(w32[0]), __int_as_float(w32[1]));
+    const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_int(mx), __float_as_int(mx), false, false);
+    mx = fmaxf(__int_as_float(w16[0]), __int_as_float(w16[1]));
+    const float mt = mx * sl2;   // scale > 0, so the max commutes with scaling
+    if (__ballot(mt > m + kRescaleSlack)) {
+      const float m_new = fmaxf(m, mt);
+      const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < kD / 16; ++db) o[db] *= alpha;
+    }
+  }
+  // The weights of a step relative to m_use; returns the lane's sum.
+  static __device__ __forceinline__ float weights(const Logits& s, float sl2, float m_use, Weights& p) {
+    float psum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const float e0 = __builtin_amdgcn_exp2f(fmaf(s.v[i][r], sl2, -m_use));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s.v[i][r + 1], sl2, -m_use));
+        psum += e0 + e1;
+        const bf16x2_t pk = __builtin_convertvector((f32x2_t){e0, e1}, bf16x2_t);
+        p[4 * i + r] = pk[0];
+        p[4 * i + r + 1] = pk[1];
+      }
+    return psum;
+  }
+  __device__ __forceinline__ void add(float psum) { l += psum; }
+  __device__ __forceinline__ void products_o(const lds_u8* v, const Weights& p) {
+#pragma unroll
+    for (int db = 0; db < kD / 16; ++db)
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_fragment(v, vofs[db], vofs[db] + 16 * kRowBytes), p, o[db], 0,
+                                                      0, 0);
+  }
+  __device__ __forceinline__ float running_max() const { return m; }
+  __device__ __forceinline__ float total() const {
+    const float t = l + __shfl_xor(l, 32, kWave);
+    return t + __shfl_xor(t, 16, kWave);
+  }
+  // The lane's chunks of four dimensions, for the merge.
+  template <class F>
+  __device__ __forceinline__ void chunks(F&& f) const {
+#pragma unroll
+    for (int db = 0; db < kD / 16; ++db) f(4 * db + (lane_id() >> 4), o[db]);
+  }
+};
+
+// A block of 32 rows (Block above).
+struct Rows32 {
+  static constexpr int kRows = 32;
+  struct Logits {
+    f32x16_t v;
+  };
+  struct Weights {
+    bf16x8_t v[2];
+  };
+  Block x;
+  bf16x8_t q[2][4];
+  int vofs[2][kD / 32];
+
+  __device__ __forceinline__ void init() {
+    block_init(x);
+    v_offsets(vofs);
+  }
+  static __device__ __forceinline__ int swizzle(int r) { return swz(r); }
+  static __device__ __forceinline__ int row() { return lane_id() & 31; }
+  static __device__ __forceinline__ bool first_of_row() { return lane_id() < 32; }
+  // Part i of a key is its group 2 * (lane / 32) + i.
+  static __device__ __forceinline__ int key_of(int) { return lane_id() & 31; }
+  static __device__ __forceinline__ int dim_of(int i) { return 64 * (lane_id() >> 5) + 32 * i; }
+  __device__ __forceinline__ void load_q(const uint16_t* p, bool valid) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint4 w = *reinterpret_cast<const uint4*>(p + dim_of(i) + 8 * j);
+        if (!valid) w = make_uint4(0, 0, 0, 0);
+        q[i][j] = as_bf16x8(w);
+      }
+  }
+  // From group `quad` of keys col and 16 + col to groups 2 * half + {0, 1} of key
+  // lane & 31: lanes 16 apart exchange one of their two.
+  static __device__ __forceinline__ void order_codes(uint4 (&k)[2], uint32_t (&e)[2]) {
+    uint32_t p[5] = {k[0].x, k[0].y, k[0].z, k[0].w, e[0]}, q[5] = {k[1].x, k[1].y, k[1].z, k[1].w, e[1]};
+#pragma unroll
+    for (int w = 0; w < 5; ++w) {
+      const auto t = __builtin_amdgcn_permlane16_swap(p[w], q[w], false, false);
+      p[w] = t[0];
+      q[w] = t[1];
+    }
+    k[0] = make_uint4(p[0], p[1], p[2], p[3]);
+    k[1] = make_uint4(q[0], q[1], q[2], q[3]);
+    e[0] = p[4];
+    e[1] = q[4];
+  }
+  template <class K>
+  __device__ __forceinline__ void products_s(K&& ka, Logits& s) const {
+    s.v = f32x16_t{};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s.v = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka(i, j), q[i][j], s.v, 0, 0, 0);
+  }
+  template <bool TREE>
+  static __device__ __forceinline__ void mask(Logits& s, int n, uint32_t bits) {
+    mask_keys<TREE>(s.v, n, bits);
+  }
+  __device__ __forceinline__ void move_max(const Logits& s, float sl2) {
+    const float mt = row_max(s.v) * sl2;
+    if (__ballot(mt > x.m + kRescaleSlack)) rescale_to(x, mt);
+  }
+  static __device__ __forceinline__ float weights(const Logits& s, float sl2, float m_use, Weights& p) {
+    float psum = 0.f;
+    exp_part(s.v, 0, sl2, m_use, p.v[0], psum);
+    exp_part(s.v, 1, sl2, m_use, p.v[1], psum);
+    return psum;
+  }
+  __device__ __forceinline__ void add(float psum) { x.l += psum; }
+  __device__ __forceinline__ void products_o(const lds_u8* v, const Weights& p) {
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < kD / 32; ++db)
+        x.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            v_fragment(v + 16 * s2 * kRowBytes, vofs[0][db], vofs[1][db]), p.v[s2], x.o[db], 0, 0, 0);
+  }
+  __device__ __forceinline__ float running_max() const { return x.m; }
+  __device__ __forceinline__ float total() const { return x.l + __shfl_xor(x.l, 32, kWave); }
+  template <class F>
+  __device__ __forceinline__ void chunks(F&& f) const {
+#pragma unroll
+    for (int db = 0; db < kD / 32; ++db)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4_t v = {x.o[db][4 * r4], x.o[db][4 * r4 + 1], x.o[db][4 * r4 + 2], x.o[db][4 * r4 + 3]};
+        f(8 * db + 2 * r4 + (lane_id() >> 5), v);
+      }
+  }
+};
+
+// STREAM: the codes are loaded with the non-temporal hint.
+template <class ROWS, int RB, bool STREAM>
+__global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
+  constexpr int kSlices = kWaves / RB;   // waves that share a row block's keys
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * 2 * kVBuffer];
+  __shared__ float2 s_ml[kWaves][ROWS::kRows];
   const VerifyKv4Call& c = a.c;
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
   const int b = bg / c.Hkv, g = bg - b * c.Hkv;
@@ -543,214 +775,208 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_narrow_kernel(const Kv4Args a
   const int tid = threadIdx.x;
   const int lane = lane_id();
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int col = lane & 31, half = lane >> 5;
-
-  // One memory round trip, as in the tile kernel.
+  const int slice = wave / RB, row0 = wave % RB * ROWS::kRows;
+  const int col = lane & 15, quad = lane >> 4;
   const int c0 = split * a.chunk;
   const bool do_tree = split == a.nsplit - 1 && c.k_tree;
-  PageLoad pages;
-  pages.begin(a, b, c0);
+
+  // One memory round trip for everything that no other load decides: the
+  // lengths, page ids, the queries of a full tree and its mask (what lies
+  // behind the sequence's own length and nodes goes unused).  Lane j holds the
+  // page ids of the two halves of the wave's step first + j.
+  const int32_t* const table = c.page_table + (size_t)b * c.max_pages;
+  int ids[2];
+  auto load_ids = [&](int first) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int pos = c0 + (slice + (first + lane) * kSlices) * kStep + 16 * i;
+      ids[i] = kv4_page_in_pool(table[min(pos >> a.page_shift, c.max_pages - 1)], c.n_pages);
+    }
+  };
+  load_ids(0);
   const int T = min(max(c.node_count[b], 0), c.T_max);
   const int L = min(max(c.lens[b], 0), c.L_max);
   const int rows = T * G;
-  // Query fragment (i, j): dims [32 * (2i + half) + 8j, +8) of the lane's row.
-  bf16x8_t qf[kQInLds ? 1 : NB][2][4];
-  uint64_t sees[NB];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const int qr = nb * 32 + col;
-    const int u = qr < a.rows_max ? qr / G : 0;
-    const int h = g * G + (qr < a.rows_max ? qr - u * G : 0);
-    const uint16_t* qp = c.q + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 32 * half;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (!kQInLds || wave == nb * 4 + i * 2 + j / 2) {
-          uint4 w = *reinterpret_cast<const uint4*>(qp + 64 * i + 8 * j);
-          if (qr >= rows) w = make_uint4(0, 0, 0, 0);
-          if constexpr (kQInLds) s_q[((nb * 2 + i) * 4 + j) * kWave + lane] = w;
-          else qf[nb][i][j] = as_bf16x8(w);
-        }
-    // at most 64 rows, so at most 64 nodes and one mask word
-    sees[nb] = do_tree ? c.tree_mask[(size_t)b * c.T_max + u] : 0ull;
-  }
-  pages.finish(c.n_pages, s_pages);
+  const int qr = row0 + ROWS::row();
+  const int qu = qr < a.rows_max ? qr / G : 0;
+  const int qh = g * G + (qr < a.rows_max ? qr - qu * G : 0);
+  ROWS x;
+  x.load_q(c.q + (((size_t)b * c.T_max + qu) * c.Hq + qh) * kD, qr < rows);
+  // at most 64 rows, so at most 64 nodes and one mask word
+  const uint64_t sees = do_tree ? c.tree_mask[(size_t)b * c.T_max + qu] : 0ull;
   if (rows == 0) return;
   const int c1 = min(c0 + a.chunk, L);
   const int n_ctx = c1 > c0 ? (c1 - c0 + kStep - 1) / kStep : 0;
   const int n_steps = n_ctx + (do_tree ? (T + kStep - 1) / kStep : 0);
-  const int p0 = c0 >> a.page_shift;
 
-  Block x[NB];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) block_init(x[nb]);
+  x.init();
   const float sl2 = a.scale_log2;
-  uint8_t* const vrows = smem + wave * kWaveLds;
-  const lds_u8* const vbase = (const lds_u8*)vrows;
-  const int vkey = lane & 15, vgrp = lane >> 4;   // loader: keys vkey, vkey + 16, one group
-  int vpos[4], vofs[2][kD / 32];
+  uint8_t* const vrows = smem + wave * 2 * kVBuffer;
+  int vpos[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) vpos[j] = vkey * kRowBytes + (((4 * vgrp + j) ^ swz(vkey)) << 4);
-  v_offsets(vofs);
+  for (int j = 0; j < 4; ++j) vpos[j] = col * kRowBytes + (((4 * quad + j) ^ ROWS::swizzle(col)) << 4);
 
   struct Raw {
     uint4 k[2], v[2];
-    uint32_t ke, ve[2];
-  };
-  auto row_of = [&](int pos) {
-    pos = min(pos, c1 - 1);   // keys behind the last read the last one again; they are masked
-    const int page = s_pages[(pos >> a.page_shift) - p0];
-    return kv4_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
+    uint32_t ke[2], ve[2];
   };
   auto load = [&](int s, Raw& r) {
-    const int k0 = c0 + s * kStep;
-    const size_t row = row_of(k0 + col);
-    const uint8_t* kc = c.k_codes + row * kKv4RowBytes + 16 * half;
-    r.k[0] = *reinterpret_cast<const uint4*>(kc);
-    r.k[1] = *reinterpret_cast<const uint4*>(kc + 32);
-    r.ke = *reinterpret_cast<const uint32_t*>(c.k_scales + row * kKv4Scales);
+    const int k0 = c0 + s * kStep, at = ((s - slice) / kSlices) & 63;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const size_t vr = row_of(k0 + vkey + 16 * i);
-      r.v[i] = *reinterpret_cast<const uint4*>(c.v_codes + vr * kKv4RowBytes + 16 * vgrp);
-      r.ve[i] = c.v_scales[vr * kKv4Scales + vgrp];
+      // Keys behind the last read the last one again; their logits are masked.
+      int pos = k0 + 16 * i;
+      uint32_t key = col;
+      int page = __builtin_amdgcn_readlane(ids[i], at);
+      if (pos + 16 > c1) {
+        if (pos >= c1) {
+          page = __builtin_amdgcn_readlane(ids[0], at);
+          pos = k0;
+        }
+        key = min((int)key, c1 - 1 - pos);
+      }
+      const size_t row = kv4_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
+      const uint32_t code_at = key * kKv4RowBytes + quad * 16, scale_at = key * kKv4Scales + quad;
+      r.k[i] = load_codes<STREAM>(c.k_codes + row * kKv4RowBytes + code_at);
+      r.v[i] = load_codes<STREAM>(c.v_codes + row * kKv4RowBytes + code_at);
+      r.ke[i] = (c.k_scales + row * kKv4Scales)[scale_at];
+      r.ve[i] = (c.v_scales + row * kKv4Scales)[scale_at];
     }
   };
-  // S, softmax and O of one step whose V rows are in LDS; ka(i, j) are its K fragments.
-  auto attend = [&](auto&& ka, auto tree, int n, int k0) {
-    // keeps the queries' reads in the loop: hoisted, they spill
-    if constexpr (kQInLds) asm volatile("" ::: "memory");
-    f32x16_t s[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) s[nb] = f32x16_t{};
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf16x8_t f = ka(i, j);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          s[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              f, kQInLds ? as_bf16x8(s_q[((nb * 2 + i) * 4 + j) * kWave + lane]) : qf[kQInLds ? 0 : nb][i][j], s[nb], 0,
-              0, 0);
-      }
-    bf16x8_t pb[NB][2];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      if constexpr (decltype(tree)::value) mask_keys<true>(s[nb], n, (uint32_t)(sees[nb] >> k0));
-      else if (n < kStep) mask_keys<false>(s[nb], n, 0u);
-      softmax_step(s[nb], sl2, x[nb], pb[nb]);
+  // Codes of step s + 2 * kSlices, once r's are used.
+  auto load_later = [&](int s, Raw& r) {
+    const int later = s + 2 * kSlices;
+    if (later < n_ctx) {
+      if ((later - slice) / kSlices % 64 == 0) load_ids((later - slice) / kSlices);
+      load(later, r);
     }
-#pragma unroll
-    for (int s2 = 0; s2 < 2; ++s2)
-#pragma unroll
-      for (int db = 0; db < kD / 32; ++db) {
-        const bf16x8_t f = v_fragment(vbase + 16 * s2 * kRowBytes, vofs[0][db], vofs[1][db]);
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-          x[nb].o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, pb[nb][s2], x[nb].o[db], 0, 0, 0);
-      }
   };
-  auto ctx_step = [&](int s, Raw& r) {
+  // V rows of a context step to buffer `buf`, and its S.
+  auto begin_ctx = [&](Raw& r, int buf, typename ROWS::Logits& s) {
+    uint8_t* const vb = vrows + buf * kVBuffer;
+    ROWS::order_codes(r.k, r.ke);
+    const float KX[2] = {__uint_as_float(r.ke[0] << 23), __uint_as_float(r.ke[1] << 23)};
+    x.products_s(
+        [&](int i, int j) {
+          const uint32_t w[4] = {r.k[i].x, r.k[i].y, r.k[i].z, r.k[i].w};
+          return as_bf16x8(dequant8(w[j], KX[i]));
+        },
+        s);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const float X = __uint_as_float(r.ve[i] << 23);
       const uint32_t w[4] = {r.v[i].x, r.v[i].y, r.v[i].z, r.v[i].w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j)   // keys 16 apart have the same swizzle
-        *reinterpret_cast<uint4*>(vrows + 16 * i * kRowBytes + vpos[j]) = dequant8(w[j], X);
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint4*>(vb + 16 * i * kRowBytes + vpos[j]) = dequant8(w[j], X);
     }
-    bf16x8_t f[2][4];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float X = __uint_as_float(((r.ke >> (8 * (2 * i + half))) & 0xffu) << 23);
-      const uint32_t w[4] = {r.k[i].x, r.k[i].y, r.k[i].z, r.k[i].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f[i][j] = as_bf16x8(dequant8(w[j], X));
-    }
-    if (s + kDepth * kWaves < n_ctx) load(s + kDepth * kWaves, r);
-    attend([&](int i, int j) { return f[i][j]; }, std::false_type{}, c1 - c0 - s * kStep, 0);
   };
-  auto tree_step = [&](int s) {
-    const int k0 = (s - n_ctx) * kStep;
-    const size_t node0 = (size_t)b * c.T_max;
+  auto begin_tree = [&](int step, int buf, typename ROWS::Logits& s) {
+    const int k0 = (step - n_ctx) * kStep;
+    auto row = [&](const uint16_t* p, int key) {
+      return p + (((size_t)b * c.T_max + min(k0 + key, T - 1)) * c.Hkv + g) * kD;
+    };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const uint4* src = reinterpret_cast<const uint4*>(
-          c.v_tree + ((node0 + min(k0 + vkey + 16 * i, T - 1)) * c.Hkv + g) * kD + 32 * vgrp);
+      const uint4* src = reinterpret_cast<const uint4*>(row(c.v_tree, col + 16 * i) + 32 * quad);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(vrows + 16 * i * kRowBytes + vpos[j]) = src[j];
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<uint4*>(vrows + buf * kVBuffer + 16 * i * kRowBytes + vpos[j]) = src[j];
     }
-    const uint16_t* kp = c.k_tree + ((node0 + min(k0 + col, T - 1)) * c.Hkv + g) * kD + 32 * half;
-    attend([&](int i, int j) { return as_bf16x8(*reinterpret_cast<const uint4*>(kp + 64 * i + 8 * j)); },
-           std::true_type{}, T - k0, k0);
+    const uint16_t* kp[2] = {row(c.k_tree, ROWS::key_of(0)) + ROWS::dim_of(0),
+                             row(c.k_tree, ROWS::key_of(1)) + ROWS::dim_of(1)};
+    x.products_s([&](int i, int j) { return as_bf16x8(*reinterpret_cast<const uint4*>(kp[i] + 8 * j)); }, s);
   };
 
-  __syncthreads();   // the page ids and the queries
   {
-    Raw r[kDepth];
-    int s = wave;
-#pragma unroll
-    for (int d = 0; d < kDepth; ++d)
-      if (s + d * kWaves < n_ctx) load(s + d * kWaves, r[d]);
-    for (; s + (kDepth - 1) * kWaves < n_ctx; s += kDepth * kWaves)
-#pragma unroll
-      for (int d = 0; d < kDepth; ++d) ctx_step(s + d * kWaves, r[d]);
-#pragma unroll
-    for (int d = 0; d + 1 < kDepth; ++d)
-      if (s < n_ctx) {
-        ctx_step(s, r[d]);
-        s += kWaves;
+    Raw r[2];
+    typename ROWS::Logits s_cur, s_nxt;
+    typename ROWS::Weights p;
+    int s = slice;
+    if (s < n_ctx) {
+      load(s, r[0]);
+      if (s + kSlices < n_ctx) load(s + kSlices, r[1]);
+      begin_ctx(r[0], 0, s_cur);
+      load_later(s, r[0]);
+      // a first max (keys behind the last repeat it)
+      x.move_max(s_cur, sl2);
+    } else if (s < n_steps) {
+      begin_tree(s, 0, s_cur);
+    }
+    auto ctx_pair = [&](int at, Raw& rn, int buf) {   // step `at` beside the start of the next, both of the context
+      // as in the tile kernel, the max is looked for when the weights grow
+      float psum = ROWS::weights(s_cur, sl2, x.running_max(), p);
+      if (__ballot(psum > kWeightLimit)) {
+        x.move_max(s_cur, sl2);
+        psum = ROWS::weights(s_cur, sl2, x.running_max(), p);
       }
-    for (; s < n_steps; s += kWaves) tree_step(s);
+      x.add(psum);
+      x.products_o((const lds_u8*)vrows + buf * kVBuffer, p);
+      begin_ctx(rn, buf ^ 1, s_nxt);
+      s_cur = s_nxt;
+      load_later(at + kSlices, rn);
+    };
+    // the next two steps are of the context, so this one and the next are full
+    for (; s + 2 * kSlices < n_ctx; s += 2 * kSlices) {
+      ctx_pair(s, r[1], 0);
+      ctx_pair(s + kSlices, r[0], 1);
+    }
+    int buf = 0;
+    for (; s < n_steps; s += kSlices) {
+      if (s >= n_ctx) {
+        const int k0 = (s - n_ctx) * kStep;
+        ROWS::template mask<true>(s_cur, T - k0, (uint32_t)(sees >> k0));
+      } else if (c1 - c0 - s * kStep < kStep) {
+        ROWS::template mask<false>(s_cur, c1 - c0 - s * kStep, 0u);
+      }
+      x.move_max(s_cur, sl2);
+      const float m = x.running_max();
+      x.add(ROWS::weights(s_cur, sl2, m == -INFINITY ? 0.f : m, p));
+      x.products_o((const lds_u8*)vrows + buf * kVBuffer, p);
+      buf ^= 1;
+      if (s + kSlices < n_ctx) begin_ctx(r[1], buf, s_cur);   // at most one context step is left here
+      else if (s + kSlices < n_steps) begin_tree(s + kSlices, buf, s_cur);
+    }
   }
 
-  // ---- merge: every wave's output relative to the common max, 16 rows at a
-  // time: [wave][row][dim], 16-byte chunks swizzled by the row.
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    const float l = x[nb].l + __shfl_xor(x[nb].l, 32, kWave);
-    if (half == 0) s_ml[wave][nb * 32 + col] = make_float2(x[nb].m, l);
+  // ---- merge: every wave's output relative to its rows' common max, 16 rows of
+  // each wave at a time: [wave][row][dim], 16-byte chunks swizzled by the row.
+  {
+    const float l = x.total();
+    if (ROWS::first_of_row()) s_ml[wave][ROWS::row()] = make_float2(x.running_max(), l);
   }
   __syncthreads();
-  float scale[NB];
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][nb * 32 + col].x);
-    scale[nb] = x[nb].m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[nb].m - M);
-  }
   float4* const xo = reinterpret_cast<float4*>(smem);   // [kWaves][16][32]
-  static_assert(kWaves * 16 * 32 * 16 <= kWaves * kWaveLds, "16 rows of every wave fit");
+  static_assert(kWaves * 16 * 32 * 16 <= sizeof(smem), "16 rows of every wave fit");
 #pragma unroll
-  for (int ph = 0; ph < 2 * NB; ++ph) {
-    if (ph * 16 >= rows) break;
-    const int nb = ph / 2;
+  for (int ph = 0; ph < ROWS::kRows / 16; ++ph) {
     if (ph > 0) __syncthreads();
-    if ((col >> 4) == (ph & 1) && nb * 32 + col < rows) {
-      const int r16 = col & 15;
+    if (ROWS::row() / 16 == ph && qr < rows) {
+      float M = -INFINITY;
 #pragma unroll
-      for (int db = 0; db < kD / 32; ++db)
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4)
-          xo[(wave * 16 + r16) * 32 + ((db * 8 + 2 * r4 + half) ^ r16)] =
-              make_float4(x[nb].o[db][4 * r4] * scale[nb], x[nb].o[db][4 * r4 + 1] * scale[nb],
-                          x[nb].o[db][4 * r4 + 2] * scale[nb], x[nb].o[db][4 * r4 + 3] * scale[nb]);
+      for (int w = 0; w < kSlices; ++w) M = fmaxf(M, s_ml[w * RB + wave % RB][ROWS::row()].x);
+      const float m = x.running_max();
+      const float scale = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+      const int r16 = ROWS::row() & 15;
+      x.chunks([&](int ch, f32x4_t v) {
+        xo[(wave * 16 + r16) * 32 + (ch ^ r16)] = make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+      });
     }
     __syncthreads();
-    const int r16 = tid >> 5, ch = tid & 31, qr = ph * 16 + r16;
-    if (qr < rows) {
+    const int r16 = tid >> 5, ch = tid & 31, in_block = ph * 16 + r16;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int out_row = rb * ROWS::kRows + in_block;
+      if (out_row >= rows) continue;
       float M = -INFINITY, l = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_ml[w][qr].x);
+      for (int w = 0; w < kSlices; ++w) M = fmaxf(M, s_ml[w * RB + rb][in_block].x);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float2 ml = s_ml[w][qr];
+      for (int w = 0; w < kSlices; ++w) {
+        const float2 ml = s_ml[w * RB + rb][in_block];
         l += ml.x == -INFINITY ? 0.f : ml.y * __builtin_amdgcn_exp2f(ml.x - M);
-        const float4 y = xo[(w * 16 + r16) * 32 + (ch ^ r16)];
+        const float4 y = xo[((w * RB + rb) * 16 + r16) * 32 + (ch ^ r16)];
         v.x += y.x;
         v.y += y.y;
         v.z += y.z;
@@ -762,7 +988,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_narrow_kernel(const Kv4Args a
       v.z *= inv;
       v.w *= inv;
       if (a.nsplit == 1) {
-        const int u = qr / G, h = g * G + (qr - u * G);
+        const int u = out_row / G, h = g * G + (out_row - u * G);
         uint2 pk;
         pk.x = f32_to_bf16_bits(v.x) | (f32_to_bf16_bits(v.y) << 16);
         pk.y = f32_to_bf16_bits(v.z) | (f32_to_bf16_bits(v.w) << 16);
@@ -770,7 +996,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_narrow_kernel(const Kv4Args a
         if (ch == 0 && c.lse)
           c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l > 0.f ? (M + log2f(l)) * kLn2 : -INFINITY;
       } else {
-        const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + qr;
+        const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + out_row;
         *reinterpret_cast<float4*>(a.ws_o + at * kD + 4 * ch) = v;
         if (ch == 0) a.ws_ml[at] = make_float2(M, l);
       }
@@ -841,18 +1067,20 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
   // a CU) times a workgroup's steps and start-up, plus the combine launch of
   // a split context.  The constants are in units of a SIMD's time for 32 rows
   // x 64 keys with two waves per SIMD.
-  struct Shape { int blocks; bool narrow; int unit; double per_unit, start; };
-  const Shape shapes[] = {{1, true, kWaves * kStep, 2.0, 12.0},
-                          {2, true, kWaves * kStep, 4.0, 12.0},
-                          {4, false, kKeyTile, 1.0, 12.0},
-                          {8, false, kKeyTile, 2.0, 12.0}};
+  // rows per workgroup; whether the waves share no keys; keys of a step of the workgroup
+  struct Shape { int rows; bool narrow; int unit; double per_unit, start; };
+  const Shape shapes[] = {{16, true, kWaves * kStep, 2.0, 12.0},
+                          {32, true, kWaves * kStep, 2.5, 12.0},
+                          {64, true, kWaves / 2 * kStep, 2.0, 12.0},
+                          {128, false, kKeyTile, 1.0, 12.0},
+                          {256, false, kKeyTile, 2.0, 12.0}};
   const int rows_max = T_max * (Hq / Hkv);
   VerifyKv4Plan best{};
   double best_cost = 0.0;
   for (const Shape& s : shapes) {
-    const int rowgroups = (rows_max + s.blocks * 32 - 1) / (s.blocks * 32);
-    if (s.narrow && rowgroups > 1) continue;
-    if (!s.narrow && rows_max <= 64) continue;
+    const int rowgroups = (rows_max + s.rows - 1) / s.rows;
+    // up to 64 rows: the narrow shape that just holds them
+    if (s.narrow ? rows_max > s.rows || (s.rows > 16 && rows_max <= s.rows / 2) : rows_max <= 64) continue;
     const int units = (L_max + s.unit - 1) / s.unit;   // L_max is at most 2^30
     const int least = (int)(((long)units * s.unit + kMaxChunk - 1) / kMaxChunk);
     const int most = std::max(least, std::min(64, units));
@@ -863,9 +1091,9 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
       const double rounds = (double)(((long)B * Hkv * rowgroups * nsplit + 255) / 256);
       const double tree = (double)((T_max + s.unit - 1) / s.unit);
       const double cost = rounds * (s.per_unit * (chunk / s.unit + tree) + s.start) + (nsplit > 1 ? 6.0 : 0.0);
-      if (best.blocks == 0 || cost < best_cost) {
+      if (best.rows == 0 || cost < best_cost) {
         best_cost = cost;
-        best = VerifyKv4Plan{rows_max, s.blocks, rowgroups, nsplit, chunk};
+        best = VerifyKv4Plan{rows_max, s.rows, rowgroups, nsplit, chunk};
       }
     }
   }
@@ -887,13 +1115,25 @@ hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Pl
   a.ws_o = static_cast<float*>(c.ws);
   a.ws_ml = c.ws ? reinterpret_cast<float2*>(static_cast<float*>(c.ws) + slots * kD) : nullptr;
   const int units = c.B * c.Hkv * p.nsplit;
+  constexpr size_t kPlainBytes = (size_t)64 << 20;
   const dim3 grid((unsigned)((units + 7) / 8 * 8 * p.rowgroups));
-  if (p.blocks == 1)
-    hipLaunchKernelGGL(kv4_narrow_kernel<1>, dim3((unsigned)units), dim3(kThreads), 0, stream, a);
-  else if (p.blocks == 2)
-    hipLaunchKernelGGL(kv4_narrow_kernel<2>, dim3((unsigned)units), dim3(kThreads), 0, stream, a);
-  else if (p.blocks == 8) hipLaunchKernelGGL(kv4_verify_kernel<8>, grid, dim3(kThreads), 0, stream, a);
-  else hipLaunchKernelGGL(kv4_verify_kernel<4>, grid, dim3(kThreads), 0, stream, a);
+  const bool stream_kv = (size_t)c.B * c.L_max * c.Hkv * 2 * kKv4RowBytes >= kPlainBytes;
+  auto narrow = [&](auto rows, auto rb) {
+    using Rows = decltype(rows);
+    constexpr int kRb = decltype(rb)::value;
+    const dim3 g((unsigned)units);
+    if (stream_kv) hipLaunchKernelGGL((kv4_narrow_kernel<Rows, kRb, true>), g, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((kv4_narrow_kernel<Rows, kRb, false>), g, dim3(kThreads), 0, stream, a);
+  };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  switch (p.rows) {
+    case 16: narrow(Rows16{}, One{}); break;
+    case 32: narrow(Rows32{}, One{}); break;
+    case 64: narrow(Rows32{}, Two{}); break;
+    case 128: hipLaunchKernelGGL(kv4_verify_kernel<4>, grid, dim3(kThreads), 0, stream, a); break;
+    default: hipLaunchKernelGGL(kv4_verify_kernel<8>, grid, dim3(kThreads), 0, stream, a); break;
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const unsigned n_rows = (unsigned)c.B * c.Hkv * p.rows_max;
