@@ -308,6 +308,14 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     if (t & 1) advance(t, even);
     else advance(t, odd);
   };
+  // The same where tile t has no masked key.  Behind the context its last tile
+  // is loaded again, so that the number of loads in flight does not depend on
+  // a branch (the wait for a tile's codes would then be one for all).
+  auto advance_plain = [&](int t, Codes& x) {
+    if (t + 1 < n_ctx) store(t + 1, x);
+    else if (t + 1 < n_tiles) store_tree(t + 1);
+    load(min(t + 3, n_ctx - 1), x);
+  };
 
   // ---- LDS offsets of the fragments within a stage (kh: the wave's half)
   const int half_off = (KH == 2 ? kh : 0) * 32 * kRowBytes;
@@ -413,8 +421,8 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
       constexpr int j = decltype(J)::value;
       pv((j + kPeriod - 1) % kPeriod, pb);
       if constexpr (j % HP == 0) {
-        if constexpr ((j / HP) & 1) advance(h / HP, even);
-        else advance(h / HP, odd);
+        if constexpr ((j / HP) & 1) advance_plain(h / HP, even);
+        else advance_plain(h / HP, odd);
       }
       // The exponentials use the running max as it stands, eight products on
       // either side of the tile barrier beside half of them each.  A weight's
@@ -843,13 +851,14 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
       r.ve[i] = (c.v_scales + row * kKv4Scales)[scale_at];
     }
   };
-  // Codes of step s + 2 * kSlices, once r's are used.
+  // Codes of step s + 2 * kSlices, once r's are used; behind the wave's last step
+  // that one again, so that the number of loads in flight does not depend on
+  // a branch (the wait for a step's codes would then be one for all).
+  const int last = slice + (n_ctx - 1 - slice) / kSlices * kSlices;
   auto load_later = [&](int s, Raw& r) {
-    const int later = s + 2 * kSlices;
-    if (later < n_ctx) {
-      if ((later - slice) / kSlices % 64 == 0) load_ids((later - slice) / kSlices);
-      load(later, r);
-    }
+    const int later = min(s + 2 * kSlices, last);
+    if ((later - slice) / kSlices % 64 == 0) load_ids((later - slice) / kSlices);
+    load(later, r);
   };
   // V rows of a context step to buffer `buf`, and its S.
   auto begin_ctx = [&](Raw& r, int buf, typename ROWS::Logits& s) {
@@ -895,7 +904,7 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
     int s = slice;
     if (s < n_ctx) {
       load(s, r[0]);
-      if (s + kSlices < n_ctx) load(s + kSlices, r[1]);
+      load(min(s + kSlices, last), r[1]);
       begin_ctx(r[0], 0, s_cur);
       load_later(s, r[0]);
       // a first max (keys behind the last repeat it)
