@@ -172,6 +172,29 @@ __device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, Block
   x.l += psum;
 }
 
+// Four dimensions (chunk ch of 32) of a finished row: to the output, or to the
+// partial outputs of a split context.  v is the unnormalised output, ml its max
+// and sum; 32 lanes store a row.
+__device__ __forceinline__ void store_row(const Kv4Args& a, int b, int g, int split, int qr, int ch, float2 ml,
+                                          float4 v) {
+  const VerifyKv4Call& c = a.c;
+  const float inv = ml.y > 0.f ? 1.f / ml.y : 0.f;   // a row without any key: 0
+  v = make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv);
+  if (a.nsplit == 1) {
+    const int u = qr / a.G, h = g * a.G + (qr - u * a.G);
+    uint2 pk;
+    pk.x = f32_to_bf16_bits(v.x) | (f32_to_bf16_bits(v.y) << 16);
+    pk.y = f32_to_bf16_bits(v.z) | (f32_to_bf16_bits(v.w) << 16);
+    *reinterpret_cast<uint2*>(c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 4 * ch) = pk;
+    if (ch == 0 && c.lse)
+      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = ml.y > 0.f ? (ml.x + log2f(ml.y)) * kLn2 : -INFINITY;
+  } else {
+    const size_t at = (((size_t)b * c.Hkv + g) * a.nsplit + split) * a.rows_max + qr;
+    *reinterpret_cast<float4*>(a.ws_o + at * kD + 4 * ch) = v;
+    if (ch == 0) a.ws_ml[at] = ml;
+  }
+}
+
 // V^T fragment of 16 keys x 32 dims from row-major bf16 rows: each 16-lane
 // group reads 4 keys x 16 dims transposed, in the key order of P^T.
 __device__ __forceinline__ bf16x8_t v_fragment(const lds_u8* rows, int lo_ofs, int hi_ofs) {
@@ -247,9 +270,6 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   const int rows = T * G;
   if (row_base >= rows) return;
   const bool valid = qr < rows;
-#pragma unroll
-  for (int ds = 0; ds < kD / 16; ++ds)
-    if (!valid) qf[ds] = as_bf16x8(make_uint4(0, 0, 0, 0));
   const int c1 = min(c0 + a.chunk, L);
   const int n_ctx = c1 > c0 ? (c1 - c0 + kKeyTile - 1) / kKeyTile : 0;
   const int n_tiles = n_ctx + (do_tree ? (T + kKeyTile - 1) / kKeyTile : 0);
@@ -385,6 +405,9 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     store_tree(0);
   }
   tile_barrier();
+#pragma unroll
+  for (int ds = 0; ds < kD / 16; ++ds)   // here, so that the first codes do not wait for the queries
+    if (!valid) qf[ds] = as_bf16x8(make_uint4(0, 0, 0, 0));
 
   const int H = HP * n_tiles;
   const int n_plain = max(c1 - c0, 0) / kKeyTile;   // leading context tiles with no masked key
@@ -591,13 +614,14 @@ struct Rows16 {
   static __device__ __forceinline__ int swizzle(int r) { return swz16(r); }
   static __device__ __forceinline__ int row() { return lane_id() & 15; }
   static __device__ __forceinline__ bool first_of_row() { return lane_id() < 16; }
-  __device__ __forceinline__ void load_q(const uint16_t* p, bool valid) {
+  __device__ __forceinline__ void load_q(const uint16_t* p) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint4 w = *reinterpret_cast<const uint4*>(p + 32 * (lane_id() >> 4) + 8 * j);
-      if (!valid) w = make_uint4(0, 0, 0, 0);
-      q[j] = as_bf16x8(w);
-    }
+    for (int j = 0; j < 4; ++j)
+      q[j] = as_bf16x8(*reinterpret_cast<const uint4*>(p + 32 * (lane_id() >> 4) + 8 * j));
+  }
+  __device__ __forceinline__ void clear_q() {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = as_bf16x8(make_uint4(0, 0, 0, 0));
   }
   // Codes as loaded are in order: part i is group quad of key 16*i + col.
   static __device__ __forceinline__ void order_codes(uint4 (&)[2], uint32_t (&)[2]) {}
@@ -700,15 +724,17 @@ struct Rows32 {
   // Part i of a key is its group 2 * (lane / 32) + i.
   static __device__ __forceinline__ int key_of(int) { return lane_id() & 31; }
   static __device__ __forceinline__ int dim_of(int i) { return 64 * (lane_id() >> 5) + 32 * i; }
-  __device__ __forceinline__ void load_q(const uint16_t* p, bool valid) {
+  __device__ __forceinline__ void load_q(const uint16_t* p) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint4 w = *reinterpret_cast<const uint4*>(p + dim_of(i) + 8 * j);
-        if (!valid) w = make_uint4(0, 0, 0, 0);
-        q[i][j] = as_bf16x8(w);
-      }
+      for (int j = 0; j < 4; ++j) q[i][j] = as_bf16x8(*reinterpret_cast<const uint4*>(p + dim_of(i) + 8 * j));
+  }
+  __device__ __forceinline__ void clear_q() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[i][j] = as_bf16x8(make_uint4(0, 0, 0, 0));
   }
   // From group `quad` of keys col and 16 + col to groups 2 * half + {0, 1} of key
   // lane & 31: lanes 16 apart exchange one of their two.
@@ -809,13 +835,12 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
   const int qu = qr < a.rows_max ? qr / G : 0;
   const int qh = g * G + (qr < a.rows_max ? qr - qu * G : 0);
   ROWS x;
-  x.load_q(c.q + (((size_t)b * c.T_max + qu) * c.Hq + qh) * kD, qr < rows);
+  x.load_q(c.q + (((size_t)b * c.T_max + qu) * c.Hq + qh) * kD);
   // at most 64 rows, so at most 64 nodes and one mask word
   const uint64_t sees = do_tree ? c.tree_mask[(size_t)b * c.T_max + qu] : 0ull;
   if (rows == 0) return;
   const int c1 = min(c0 + a.chunk, L);
   const int n_ctx = c1 > c0 ? (c1 - c0 + kStep - 1) / kStep : 0;
-  const int n_steps = n_ctx + (do_tree ? (T + kStep - 1) / kStep : 0);
 
   x.init();
   const float sl2 = a.scale_log2;
@@ -880,37 +905,53 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
         *reinterpret_cast<uint4*>(vb + 16 * i * kRowBytes + vpos[j]) = dequant8(w[j], X);
     }
   };
-  auto begin_tree = [&](int step, int buf, typename ROWS::Logits& s) {
-    const int k0 = (step - n_ctx) * kStep;
-    auto row = [&](const uint16_t* p, int key) {
-      return p + (((size_t)b * c.T_max + min(k0 + key, T - 1)) * c.Hkv + g) * kD;
-    };
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint4* src = reinterpret_cast<const uint4*>(row(c.v_tree, col + 16 * i) + 32 * quad);
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<uint4*>(vrows + buf * kVBuffer + 16 * i * kRowBytes + vpos[j]) = src[j];
-    }
-    const uint16_t* kp[2] = {row(c.k_tree, ROWS::key_of(0)) + ROWS::dim_of(0),
-                             row(c.k_tree, ROWS::key_of(1)) + ROWS::dim_of(1)};
-    x.products_s([&](int i, int j) { return as_bf16x8(*reinterpret_cast<const uint4*>(kp[i] + 8 * j)); }, s);
-  };
 
   {
     Raw r[2];
     typename ROWS::Logits s_cur, s_nxt;
     typename ROWS::Weights p;
+    // The tree's keys come first: their rows need no page ids, so they bridge the
+    // wait for the first codes.  Its (at most two) steps go to the last slices,
+    // which have no more context steps than the others.
+    const int tree0 = (kSlices - 1 - slice) * kStep;
+    const bool has_tree = do_tree && tree0 < T;
+    u32x4_t tk[2][4] = {}, tv[2][4] = {};
+    if (has_tree) {
+      auto row = [&](const uint16_t* p, int key) {
+        return p + (((size_t)b * c.T_max + min(tree0 + key, T - 1)) * c.Hkv + g) * kD;
+      };
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const u32x4_t* ks = reinterpret_cast<const u32x4_t*>(row(c.k_tree, ROWS::key_of(i)) + ROWS::dim_of(i));
+        const u32x4_t* vs = reinterpret_cast<const u32x4_t*>(row(c.v_tree, col + 16 * i) + 32 * quad);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          tk[i][j] = ks[j];
+          tv[i][j] = vs[j];
+        }
+      }
+    }
     int s = slice;
     if (s < n_ctx) {
       load(s, r[0]);
-      load(min(s + kSlices, last), r[1]);
-      begin_ctx(r[0], 0, s_cur);
-      load_later(s, r[0]);
-      // a first max (keys behind the last repeat it)
+      if (s + kSlices < n_ctx) load(s + kSlices, r[1]);
+    }
+    if (qr >= rows) x.clear_q();   // here, so that the first codes do not wait for the queries
+    if (has_tree) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4_t*>(vrows + 16 * i * kRowBytes + vpos[j]) = tv[i][j];
+      x.products_s([&](int i, int j) { return __builtin_bit_cast(bf16x8_t, tk[i][j]); }, s_cur);
+      ROWS::template mask<true>(s_cur, T - tree0, (uint32_t)(sees >> tree0));
       x.move_max(s_cur, sl2);
-    } else if (s < n_steps) {
-      begin_tree(s, 0, s_cur);
+      const float m = x.running_max();
+      x.add(ROWS::weights(s_cur, sl2, m == -INFINITY ? 0.f : m, p));
+      x.products_o((const lds_u8*)vrows, p);
+    }
+    if (s < n_ctx) {
+      begin_ctx(r[0], 0, s_cur);
+      x.move_max(s_cur, sl2);   // a first max (keys behind the last repeat it)
     }
     auto ctx_pair = [&](int at, Raw& rn, int buf) {   // step `at` beside the start of the next, both of the context
       // as in the tile kernel, the max is looked for when the weights grow
@@ -926,25 +967,17 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
       load_later(at + kSlices, rn);
     };
     // the next two steps are of the context, so this one and the next are full
+    if (s + 2 * kSlices < n_ctx) load_later(s, r[0]);
     for (; s + 2 * kSlices < n_ctx; s += 2 * kSlices) {
       ctx_pair(s, r[1], 0);
       ctx_pair(s + kSlices, r[0], 1);
     }
-    int buf = 0;
-    for (; s < n_steps; s += kSlices) {
-      if (s >= n_ctx) {
-        const int k0 = (s - n_ctx) * kStep;
-        ROWS::template mask<true>(s_cur, T - k0, (uint32_t)(sees >> k0));
-      } else if (c1 - c0 - s * kStep < kStep) {
-        ROWS::template mask<false>(s_cur, c1 - c0 - s * kStep, 0u);
-      }
+    for (int buf = 0; s < n_ctx; s += kSlices, buf ^= 1) {   // at most two steps
+      if (c1 - c0 - s * kStep < kStep) ROWS::template mask<false>(s_cur, c1 - c0 - s * kStep, 0u);
       x.move_max(s_cur, sl2);
-      const float m = x.running_max();
-      x.add(ROWS::weights(s_cur, sl2, m == -INFINITY ? 0.f : m, p));
+      x.add(ROWS::weights(s_cur, sl2, x.running_max(), p));
       x.products_o((const lds_u8*)vrows + buf * kVBuffer, p);
-      buf ^= 1;
-      if (s + kSlices < n_ctx) begin_ctx(r[1], buf, s_cur);   // at most one context step is left here
-      else if (s + kSlices < n_steps) begin_tree(s + kSlices, buf, s_cur);
+      if (s + kSlices < n_ctx) begin_ctx(r[1], buf ^ 1, s_cur);
     }
   }
 
@@ -991,24 +1024,7 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
         v.z += y.z;
         v.w += y.w;
       }
-      const float inv = l > 0.f ? 1.f / l : 0.f;   // a row without any key: 0
-      v.x *= inv;
-      v.y *= inv;
-      v.z *= inv;
-      v.w *= inv;
-      if (a.nsplit == 1) {
-        const int u = out_row / G, h = g * G + (out_row - u * G);
-        uint2 pk;
-        pk.x = f32_to_bf16_bits(v.x) | (f32_to_bf16_bits(v.y) << 16);
-        pk.y = f32_to_bf16_bits(v.z) | (f32_to_bf16_bits(v.w) << 16);
-        *reinterpret_cast<uint2*>(c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 4 * ch) = pk;
-        if (ch == 0 && c.lse)
-          c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l > 0.f ? (M + log2f(l)) * kLn2 : -INFINITY;
-      } else {
-        const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + out_row;
-        *reinterpret_cast<float4*>(a.ws_o + at * kD + 4 * ch) = v;
-        if (ch == 0) a.ws_ml[at] = make_float2(M, l);
-      }
+      store_row(a, b, g, split, out_row, ch, make_float2(M, l), v);
     }
   }
 }
@@ -1024,8 +1040,7 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
   const int qr = (int)(row - bg * (uint32_t)a.rows_max);
   const int b = (int)(bg / (uint32_t)c.Hkv);
   if (b >= c.B) return;
-  const int T = min(max(c.node_count[b], 0), c.T_max);
-  if (qr >= T * a.G) return;
+  const int nodes = c.node_count[b];
   const int dim = (threadIdx.x & 31) * 4;
   const size_t row0 = (size_t)bg * a.nsplit * a.rows_max + qr;
   // In index order, eight splits' loads in flight at a time.
@@ -1057,6 +1072,9 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
       }
     }
   }
+  // rows past the tree are dropped only here, so the node count shares the
+  // partials' memory round trip
+  if (qr >= min(max(nodes, 0), c.T_max) * a.G) return;
   const int g = (int)bg - b * c.Hkv;
   const int u = qr / a.G;
   const int h = g * a.G + (qr - u * a.G);
@@ -1072,37 +1090,57 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
 }  // namespace
 
 VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
-  // The estimated time is the number of rounds of workgroups over the CUs (one
-  // a CU) times a workgroup's steps and start-up, plus the combine launch of
-  // a split context.  The constants are in units of a SIMD's time for 32 rows
-  // x 64 keys with two waves per SIMD.
-  // rows per workgroup; whether the waves share no keys; keys of a step of the workgroup
-  struct Shape { int rows; bool narrow; int unit; double per_unit, start; };
-  const Shape shapes[] = {{16, true, kWaves * kStep, 2.0, 12.0},
-                          {32, true, kWaves * kStep, 2.5, 12.0},
-                          {64, true, kWaves / 2 * kStep, 2.0, 12.0},
-                          {128, false, kKeyTile, 1.0, 12.0},
-                          {256, false, kKeyTile, 2.0, 12.0}};
+  // The shape and the number of context splits with the least estimated time.
+  // A workgroup (one a CU) takes a start-up and a time per unit of keys, which
+  // for the 256-row shape depends on whether some SIMD has two row blocks; a
+  // call takes its rounds of workgroups over the 256 CUs at their mean time, at
+  // least the longest one's; a split context also the second launch and the
+  // partials' traffic.  Constants in us, fitted to calls like these (us at the
+  // choice / at the next best): 16 x 8192 keys, 32 heads over 8, 52 nodes 256
+  // rows in 2 splits 144 / 128 rows unsplit 153; 8 x 32768, 64 over 8, 72 nodes
+  // 256 rows in 4 636 / 128 in 4 681; 4 x 2048, 40 over 8, 136 nodes 128 unsplit
+  // 49 / 256 in 2 61; 1 x 4096, 32 over 8, 44 nodes 128 in 16 22.6 / in 8 23.6;
+  // single tokens, 4 x 30000, 64 over 8 in 8 34 / in 6 37; 8 x 2048, 32 over 8 in
+  // 4 12.9 / in 2 13.6.
+  constexpr int kCUs = 256;
+  constexpr double kCombine = 5.0, kPartialBytesPerUs = 6e6;
+  struct Shape {
+    int rows;       // stacked rows per workgroup
+    bool narrow;    // up to 64 rows: the shape that just holds them
+    int unit;       // keys of a step of the workgroup
+    double start, per_unit, per_unit_half;   // the latter where at most half the rows live
+  };
+  const Shape shapes[] = {{16, true, kWaves * kStep, 5.5, 1.3, 1.3},
+                          {32, true, kWaves * kStep, 5.5, 2.0, 2.0},
+                          {64, true, kWaves / 2 * kStep, 5.5, 1.7, 1.7},
+                          {128, false, kKeyTile, 10.0, 1.12, 1.12},
+                          {256, false, kKeyTile, 10.0, 1.9, 1.12}};
   const int rows_max = T_max * (Hq / Hkv);
+  const int64_t pairs = (int64_t)B * Hkv;
   VerifyKv4Plan best{};
   double best_cost = 0.0;
   for (const Shape& s : shapes) {
-    const int rowgroups = (rows_max + s.rows - 1) / s.rows;
-    // up to 64 rows: the narrow shape that just holds them
     if (s.narrow ? rows_max > s.rows || (s.rows > 16 && rows_max <= s.rows / 2) : rows_max <= 64) continue;
+    const int rowgroups = (rows_max + s.rows - 1) / s.rows;
+    const bool half_last = rows_max - (rowgroups - 1) * s.rows <= s.rows / 2;
+    const double longest = rowgroups == 1 && half_last ? s.per_unit_half : s.per_unit;
+    const double mean = ((rowgroups - 1) * s.per_unit + (half_last ? s.per_unit_half : s.per_unit)) / rowgroups;
+    const int tree = (T_max + s.unit - 1) / s.unit;
     const int units = (L_max + s.unit - 1) / s.unit;   // L_max is at most 2^30
-    const int least = (int)(((long)units * s.unit + kMaxChunk - 1) / kMaxChunk);
+    const int least = (int)(((int64_t)units * s.unit + kMaxChunk - 1) / kMaxChunk);
     const int most = std::max(least, std::min(64, units));
     for (int want = least; want <= most; ++want) {
-      const int chunk = (units + want - 1) / want * s.unit;
-      const int nsplit = (int)(((long)units * s.unit + chunk - 1) / chunk);
+      const int per = (units + want - 1) / want;   // units of a split
+      const int nsplit = (units + per - 1) / per;
       if (nsplit != want) continue;   // the same split as a smaller count
-      const double rounds = (double)(((long)B * Hkv * rowgroups * nsplit + 255) / 256);
-      const double tree = (double)((T_max + s.unit - 1) / s.unit);
-      const double cost = rounds * (s.per_unit * (chunk / s.unit + tree) + s.start) + (nsplit > 1 ? 6.0 : 0.0);
+      const int64_t wgs = pairs * rowgroups * nsplit;
+      const double rounds = (double)((wgs + kCUs - 1) / kCUs);
+      double cost = std::max(rounds * (s.start + mean * (per + tree)), s.start + longest * (per + tree));
+      if (nsplit > 1)
+        cost += kCombine + (double)(pairs * nsplit) * rows_max * 2 * (kD * 4 + 8) / kPartialBytesPerUs;
       if (best.rows == 0 || cost < best_cost) {
         best_cost = cost;
-        best = VerifyKv4Plan{rows_max, s.rows, rowgroups, nsplit, chunk};
+        best = VerifyKv4Plan{rows_max, s.rows, rowgroups, nsplit, per * s.unit};
       }
     }
   }
