@@ -29,7 +29,6 @@ constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kMaskWords = (ADAPLD_MAX_TREE_NODES + 63) / 64;
 constexpr int kMaxChunk = 32768;                  // context keys of one split
-constexpr int kMinPage = 16;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kRescaleSlack = 8.0f;             // log2 units the running max may lag
@@ -79,25 +78,6 @@ __device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
   else v = *q;
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
-
-// The page ids of a split's keys [c0, c0 + chunk) on their way to LDS (entries
-// of the sequence's table row only).  The first of each thread is requested by
-// begin(), before the queries: loads return in order, and the codes wait for
-// the page ids alone.
-struct PageLoad {
-  const int32_t* row;
-  int n, first;
-  __device__ __forceinline__ void begin(const Kv4Args& a, int b, int c0) {
-    const int p0 = c0 >> a.page_shift;
-    n = min(((c0 + a.chunk - 1) >> a.page_shift) - p0 + 1, a.c.max_pages - p0);
-    row = a.c.page_table + (size_t)b * a.c.max_pages + p0;
-    first = row[min((int)threadIdx.x, n - 1)];
-  }
-  __device__ __forceinline__ void finish(int n_pages, int* s_pages) {
-    if ((int)threadIdx.x < n) s_pages[threadIdx.x] = kv4_page_in_pool(first, n_pages);
-    for (int i = threadIdx.x + kThreads; i < n; i += kThreads) s_pages[i] = kv4_page_in_pool(row[i], n_pages);
-  }
-};
 
 // ------------------------------------------------- one 32-row block's softmax
 //
@@ -225,7 +205,6 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   constexpr int HP = 2 / KH;   // 32-key halves of a tile that one wave takes
   __shared__ __attribute__((aligned(1024))) uint8_t smem[2 * kVRegion];
   __shared__ uint64_t s_mask[ADAPLD_MAX_TREE_NODES * kMaskWords];
-  __shared__ int s_pages[kMaxChunk / kMinPage + 1];
   const VerifyKv4Call& c = a.c;
 
   // ---- the workgroup's job: the row groups of one (sequence, kv head, split)
@@ -248,8 +227,19 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   // lengths, the page ids of a full split, the queries of a full tree and its
   // mask (what lies behind the sequence's own length and nodes goes unused).
   const int c0 = split * a.chunk;
-  PageLoad pages;
-  pages.begin(a, b, c0);
+  // loader: waves 0-3 bring K, waves 4-7 V; a lane one group of 32 dimensions (16
+  // bytes of codes) of one key.  A wave's 16 keys never cross a page: lane j
+  // holds their page id of tile first + j, and an address is a scalar base plus a
+  // fixed lane offset.
+  const bool is_v = wave >= 4;
+  const int lkey = 16 * (wave & 3) + (lane & 15), lgrp = lane >> 4;
+  const int32_t* const table = c.page_table + (size_t)b * c.max_pages;
+  int ids;
+  auto load_ids = [&](int first) {
+    const int pos = c0 + (first + lane) * kKeyTile + 16 * (wave & 3);
+    ids = kv4_page_in_pool(table[min(pos >> a.page_shift, c.max_pages - 1)], c.n_pages);
+  };
+  load_ids(0);
   const int nodes = c.node_count[b], len = c.lens[b];
   // Query fragments (B operand): lane holds dims [16*ds + 8*half, +8) of its row.
   const int qr = row_base + wrow * 32 + col;
@@ -261,7 +251,6 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
 #pragma unroll
     for (int ds = 0; ds < kD / 16; ++ds) qf[ds] = as_bf16x8(*reinterpret_cast<const uint4*>(qp + 16 * ds));
   }
-  pages.finish(c.n_pages, s_pages);
   const bool do_tree = split == a.nsplit - 1 && c.k_tree;
   if (do_tree)
     for (int i = tid; i < c.T_max * a.nw; i += kThreads) s_mask[i] = c.tree_mask[(size_t)b * c.T_max * a.nw + i];
@@ -273,14 +262,9 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   const int c1 = min(c0 + a.chunk, L);
   const int n_ctx = c1 > c0 ? (c1 - c0 + kKeyTile - 1) / kKeyTile : 0;
   const int n_tiles = n_ctx + (do_tree ? (T + kKeyTile - 1) / kKeyTile : 0);
-  const int p0 = c0 >> a.page_shift;
 
-  // ---- loader: waves 0-3 bring K, waves 4-7 V; a lane one group of 32
-  // dimensions (16 bytes of codes) of one key.
-  const bool is_v = wave >= 4;
-  const int lkey = 16 * (wave & 3) + (lane & 15), lgrp = lane >> 4;
-  const uint8_t* codes = is_v ? c.v_codes : c.k_codes;
-  const uint8_t* scales = is_v ? c.v_scales : c.k_scales;
+  const uint8_t* const codes = is_v ? c.v_codes : c.k_codes;
+  const uint8_t* const scales = is_v ? c.v_scales : c.k_scales;
   uint8_t* const lrow = smem + (is_v ? kVRegion : 0) + lkey * kRowBytes;
   int lpos[4];
 #pragma unroll
@@ -290,13 +274,24 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     uint4 c;
     uint32_t e;
   };
-  // Keys behind the last read the last one again; their logits are masked.
   auto load = [&](int t, Codes& x) {
-    const int pos = min(c0 + t * kKeyTile + lkey, c1 - 1);
-    const int page = s_pages[(pos >> a.page_shift) - p0];
+    if (t > 0 && t % 64 == 0) load_ids(t);
+    // Keys behind the last read the last one again; their logits are masked.
+    int pos = c0 + t * kKeyTile + 16 * (wave & 3);
+    uint32_t key = lane & 15;
+    int page = __builtin_amdgcn_readlane(ids, t & 63);
+    if (pos + 16 > c1) {
+      const int last = c1 - 1;
+      if (pos > last) {   // none of the wave's keys: the tile's first page holds one of the context
+        pos = c0 + t * kKeyTile;
+        page = kv4_page_in_pool(table[pos >> a.page_shift], c.n_pages);
+        key = 0;
+      }
+      key = min((int)key, last - pos);
+    }
     const size_t row = kv4_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
-    x.c = *reinterpret_cast<const uint4*>(codes + row * kKv4RowBytes + lgrp * 16);
-    x.e = scales[row * kKv4Scales + lgrp];
+    x.c = *reinterpret_cast<const uint4*>(codes + row * kKv4RowBytes + (key * kKv4RowBytes + lgrp * 16));
+    x.e = (scales + row * kKv4Scales)[key * kKv4Scales + lgrp];
   };
   auto store = [&](int t, const Codes& x) {
     uint8_t* p = lrow + (t % kStages) * kTileBytes;
@@ -395,7 +390,6 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   // tile before the current one is free after it.  Loads stay in flight.
   auto tile_barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-  __syncthreads();   // the page ids and the mask
   if (n_ctx > 0) {
     load(0, even);
     if (n_ctx > 1) load(1, odd);
