@@ -11,21 +11,30 @@ namespace {
 
 // ------------------------------------------------------------------- page map
 //
-// One workgroup takes the sequences in index order, kMapThreads at a time, and
-// has one prefix sum for the pages given back and one for the pages asked for.
-// The moved pages of such a group are then laid end to end over the threads
-// (each finds its sequence in the prefix sums by bisection), so one long prompt
-// does not make one thread walk its pages.  Everything is given back before
-// anything is handed out: the stack's height after the first pass decides who
-// is served, and the second pass may pop what the first has pushed.
+// Workgroup 0 keeps the state: it takes the sequences in index order, kMapThreads
+// at a time, and has one prefix sum for the pages given back and one for the
+// pages asked for.  The moved pages of such a group are then laid end to end
+// over the threads (each finds its sequence in the prefix sums by bisection), so
+// one long prompt does not make one thread walk its pages.  Everything is given
+// back before anything is handed out: the stack's height after the first pass
+// decides who is served, and the second pass may pop what the first has pushed.
+//
+// The slots of a batch that is one such group are filled in the same launch by
+// the other workgroups, which repeat the prefix sums and work out the page of a
+// new token from what workgroup 0 does not write: the old count, the stack below
+// it and the table entries that were held before the call.  Calls with few slots
+// leave them to workgroup 0; larger batches, and calls that update the count in
+// place, take a second launch.
 constexpr int kMapThreads = 1024;
 constexpr int kMapWaves = kMapThreads / kWave;
+constexpr int kSlotsPerThread = 4;
+enum SlotsBy { kSlotsByFirst, kSlotsByOthers, kSlotsLater };
 
 struct MapArgs {
   const int32_t* lens_old;
   const int32_t* lens_new;
   int B, page_shift, max_pages, n_pages, N;
-  int32_t* page_table;   // read and written by one workgroup: never through the scalar cache
+  int32_t* page_table;   // read and written by one launch: never through the scalar cache
   int32_t* free_pages;
   const int32_t* free_count;
   int32_t* free_count_out;
@@ -33,7 +42,7 @@ struct MapArgs {
   int32_t* granted;
 };
 
-// Slots of 32-bit positions; top = max_pages << page_shift fits by the host's check.
+// Lengths in [0, max_pages << page_shift], which fits 31 bits by the host's check.
 __device__ __forceinline__ int clamp_len(int len, const MapArgs& a) {
   return min(max(len, 0), a.max_pages << a.page_shift);
 }
@@ -68,16 +77,72 @@ __device__ __forceinline__ int find_in_prefix(const int* s_incl, int p) {
   return lo;
 }
 
-__device__ __forceinline__ int slot_at(const MapArgs& a, int b, int pos) {
-  const int page = a.page_table[(size_t)b * a.max_pages + (pos >> a.page_shift)];
+__device__ __forceinline__ int slot_in_page(const MapArgs& a, int page, int pos) {
   if (page < 0 || page >= a.n_pages) return -1;
   return (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
 }
+__device__ __forceinline__ int slot_at(const MapArgs& a, int b, int pos) {
+  return slot_in_page(a, a.page_table[(size_t)b * a.max_pages + (pos >> a.page_shift)], pos);
+}
 
-__global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapArgs a, int fill_slots) {
+// Slots of a batch of at most kMapThreads sequences, beside workgroup 0.
+__device__ void fill_slots_beside(const MapArgs& a, int* s_back, int* s_need, int* s_wave, int* s_first) {
+  const int tid = threadIdx.x, shift = a.page_shift;
+  int back = 0, need = 0;
+  if (tid < a.B) {
+    const int held = pages_of(clamp_len(a.lens_old[tid], a), shift);
+    const int want = pages_of(clamp_len(a.lens_new[tid], a), shift);
+    back = max(held - want, 0);
+    need = max(want - held, 0);
+    s_first[tid] = want;
+  }
+  const int start = min(max(a.free_count[0], 0), a.n_pages);
+  int total;
+  s_back[tid] = block_incl_scan(back, s_wave, total);
+  const int height = (int)min<int64_t>((int64_t)start + total, a.n_pages);
+  s_need[tid] = block_incl_scan(need, s_wave, total);
+  __syncthreads();
+  const int per_row = (a.N + kMapThreads * kSlotsPerThread - 1) / (kMapThreads * kSlotsPerThread);   // workgroups of a row
+  const int wg = blockIdx.x - 1, b = wg / per_row;
+  const int o = clamp_len(a.lens_old[b], a), n = clamp_len(a.lens_new[b], a);
+  const int held = pages_of(o, shift);
+  const int before = b > 0 ? s_need[b - 1] : 0;
+  const bool granted = s_need[b] <= height || s_need[b] == before;
+  const int i0 = (wg - b * per_row) * kMapThreads * kSlotsPerThread;
+#pragma unroll
+  for (int k = 0; k < kSlotsPerThread; ++k) {
+    const int i = i0 + k * kMapThreads + tid;
+    if (i >= a.N) break;
+    int slot = -1;
+    if (granted && i < n - o) {
+      const int pos = o + i, at = pos >> shift;
+      int page;
+      if (at < held) {
+        page = a.page_table[(size_t)b * a.max_pages + at];
+      } else {
+        const int from = height - 1 - (before + at - held);   // its place on the stack
+        if (from < start) {
+          page = a.free_pages[from];
+        } else {   // given back by this call
+          const int p = from - start, seq = find_in_prefix(s_back, p);
+          page = a.page_table[(size_t)seq * a.max_pages + s_first[seq] + p - (seq > 0 ? s_back[seq - 1] : 0)];
+        }
+      }
+      slot = slot_in_page(a, page, pos);
+    }
+    a.slot_map[(size_t)b * a.N + i] = slot;
+  }
+}
+
+__global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapArgs a, SlotsBy slots) {
   __shared__ int s_incl[kMapThreads];
   __shared__ int s_first[kMapThreads];   // first page index of the sequence's moved pages
+  __shared__ int s_need[kMapThreads];
   __shared__ int s_wave[kMapWaves];
+  if (blockIdx.x > 0) {
+    fill_slots_beside(a, s_incl, s_need, s_wave, s_first);
+    return;
+  }
   const int tid = threadIdx.x;
   const int shift = a.page_shift;
   const int start = min(max(a.free_count[0], 0), a.n_pages);
@@ -144,7 +209,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapArgs a, 
   }
   if (tid == 0) a.free_count_out[0] = left;
 
-  if (!fill_slots) return;
+  if (slots != kSlotsByFirst) return;
   __syncthreads();
   for (int idx = tid; idx < a.B * a.N; idx += kMapThreads) {
     const int b = idx / a.N, i = idx - b * a.N;
@@ -153,15 +218,17 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapArgs a, 
   }
 }
 
-// Slots of a call with many: four tokens of one sequence a thread.
+// Slots of a larger batch, after the pages.
 constexpr int kSlotThreads = 256;
 __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(const MapArgs a) {
   const int b = blockIdx.y;
   const int o = clamp_len(a.lens_old[b], a), n = clamp_len(a.lens_new[b], a);
   const bool ok = a.granted[b] != 0;
-  const int i0 = (blockIdx.x * kSlotThreads + threadIdx.x) * 4;
-  for (int i = i0; i < min(i0 + 4, a.N); ++i)
-    a.slot_map[(size_t)b * a.N + i] = ok && i < n - o ? slot_at(a, b, o + i) : -1;
+#pragma unroll
+  for (int k = 0; k < kSlotsPerThread; ++k) {
+    const int i = (blockIdx.x * kSlotsPerThread + k) * kSlotThreads + threadIdx.x;
+    if (i < a.N) a.slot_map[(size_t)b * a.N + i] = ok && i < n - o ? slot_at(a, b, o + i) : -1;
+  }
 }
 
 // --------------------------------------------------------------- append, gather
@@ -285,13 +352,17 @@ hipError_t launch_kv4_page_map(const int32_t* lens_old, const int32_t* lens_new,
   a.B = B; a.page_shift = log2_pow2(page_size); a.max_pages = max_pages; a.n_pages = n_pages; a.N = N;
   a.page_table = page_table; a.free_pages = free_pages; a.free_count = free_count;
   a.free_count_out = free_count_out; a.slot_map = slot_map; a.granted = granted;
-  constexpr int kFusedSlots = 4 * kMapThreads;
-  const bool fused = (int64_t)B * N <= kFusedSlots;
-  hipLaunchKernelGGL(page_map_kernel, dim3(1), dim3(kMapThreads), 0, stream, a, fused ? 1 : 0);
+  constexpr int kFewSlots = 4 * kMapThreads;
+  const SlotsBy slots = (int64_t)B * N <= kFewSlots                           ? kSlotsByFirst
+                        : B <= kMapThreads && free_count_out != free_count ? kSlotsByOthers
+                                                                           : kSlotsLater;
+  constexpr int kPerGroup = kMapThreads * kSlotsPerThread;
+  const unsigned others = slots == kSlotsByOthers ? (unsigned)((N + kPerGroup - 1) / kPerGroup) * B : 0u;
+  hipLaunchKernelGGL(page_map_kernel, dim3(1 + others), dim3(kMapThreads), 0, stream, a, slots);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || fused) return e;
-  hipLaunchKernelGGL(slot_map_kernel, dim3((N + 4 * kSlotThreads - 1) / (4 * kSlotThreads), B), dim3(kSlotThreads), 0,
-                     stream, a);
+  if (e != hipSuccess || slots != kSlotsLater) return e;
+  constexpr int kPerBlock = kSlotThreads * kSlotsPerThread;
+  hipLaunchKernelGGL(slot_map_kernel, dim3((N + kPerBlock - 1) / kPerBlock, B), dim3(kSlotThreads), 0, stream, a);
   return hipGetLastError();
 }
 
