@@ -670,8 +670,8 @@ int adapld_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uin
  * page_size, a page_size other than the five, scale not finite and > 0, or
  * misaligned pointers; UNSUPPORTED for D != 128, T_max >
  * ADAPLD_MAX_TREE_NODES, n_pages * page_size or max_pages * page_size >
- * INT32_MAX, L_max > 2^30, or more work than one launch holds (B * Hkv * T_max * Hq / Hkv
- * times the number of context splits up to 2^23 - 8); WORKSPACE_TOO_SMALL.
+ * INT32_MAX, L_max > 2^30, B * T_max * Hq > 2^27 - 8, or more workgroups than one
+ * launch holds (some 2^23); WORKSPACE_TOO_SMALL.
  */
 int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,
                                 const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* page_table,

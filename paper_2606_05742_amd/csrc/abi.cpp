@@ -1,6 +1,5 @@
 // C ABI of libadapld: argument validation, workspace sizing, status reporting.
 // Every check runs on the host before anything is enqueued.
-#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -27,6 +26,12 @@ size_t semantic_ws(int B, int L_stride, int k) {
 // adapld_step: the scan's lists first (rounded to 256 bytes), then the verify
 // workspace.
 size_t step_sem_part(int B, int L_stride, int k) { return (semantic_ws(B, L_stride, k) + 255) / 256 * 256; }
+
+// A launch holds less than 2^32 threads: 16 a cache row, 32 an output row, 512 a
+// workgroup of the verify.
+constexpr int64_t kKv4MaxRows = (1 << 28) - 16;
+constexpr int64_t kKv4MaxOutRows = (1 << 27) - 8;
+constexpr int64_t kKv4MaxGroups = (1 << 23) - 8;
 
 // The embedding fallback's own part (16-byte aligned), then the scan's lists.
 size_t embed_head_ws(int B, int L_stride) { return (adapld::embed_ws_bytes(B, L_stride) + 15) / 16 * 16; }
@@ -153,7 +158,9 @@ size_t adapld_workspace_bytes(int op, int B, int L_stride, int d, int k, int T_m
       return adapld::verify_ws_bytes(p, B, Hkv);
     }
     case ADAPLD_OP_TREE_VERIFY_ATTN_KV4: {
-      if (T_max < 1 || T_max > ADAPLD_MAX_TREE_NODES || Hq < 1 || Hkv < 1 || Hq % Hkv || L_stride > (1 << 30)) return 0;
+      if (T_max < 1 || T_max > ADAPLD_MAX_TREE_NODES || Hq < 1 || Hkv < 1 || Hq % Hkv || L_stride > (1 << 30) ||
+          (double)B * T_max * Hq > kKv4MaxOutRows)
+        return 0;
       return adapld::verify_kv4_ws_bytes(adapld::plan_verify_kv4(B, L_stride, T_max, Hq, Hkv), B, Hkv);
     }
     default:
@@ -441,10 +448,6 @@ int check_kv4_pool(int page_size, int n_pages) {
   return ADAPLD_OK;
 }
 
-// A launch holds less than 2^32 threads: 16 a row, 512 a verify workgroup.
-constexpr int64_t kKv4MaxRows = (1 << 28) - 16;
-constexpr int64_t kKv4MaxGroups = (1 << 23) - 8;
-
 bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
 int check_kv4_arrays(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
@@ -533,13 +536,13 @@ int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const
     return ADAPLD_ERR_INVALID_ARG;
   if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
   if (D != ADAPLD_HEAD_DIM || T_max > ADAPLD_MAX_TREE_NODES || (int64_t)max_pages * page_size > INT32_MAX ||
-      L_max > (1 << 30))
+      L_max > (1 << 30) || (double)B * T_max * Hq > kKv4MaxOutRows)
     return ADAPLD_ERR_UNSUPPORTED;
   if (L_max > max_pages * page_size || misaligned16(q) || misaligned16(out) || misaligned16(k_tree) ||
       misaligned16(v_tree))
     return ADAPLD_ERR_INVALID_ARG;
   const adapld::VerifyKv4Plan p = adapld::plan_verify_kv4(B, L_max, T_max, Hq, Hkv);
-  if ((double)B * Hkv * p.nsplit * std::max(p.rowgroups, p.rows_max) > kKv4MaxGroups) return ADAPLD_ERR_UNSUPPORTED;
+  if ((double)B * Hkv * p.nsplit * p.rowgroups > kKv4MaxGroups - 8.0 * p.rowgroups) return ADAPLD_ERR_UNSUPPORTED;
   const size_t need = adapld::verify_kv4_ws_bytes(p, B, Hkv);
   if (need > 0 && !ws) return ADAPLD_ERR_NULL_ARG;
   if (ws_bytes < need) return ADAPLD_ERR_WORKSPACE_TOO_SMALL;

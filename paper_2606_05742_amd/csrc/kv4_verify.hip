@@ -1,5 +1,24 @@
 // Tree-masked verify attention over the paged 4-bit K/V cache (Sec. 3.6: all
 // draft paths are scored in one target forward with tree attention).
+//
+// For one sequence and kv head the T*G query rows (node u, query head g*G + i) are
+// stacked as row = u*G + i, so the G heads that share a kv head share every byte
+// of the cache.  A workgroup of 8 waves takes a number of rows and one split of
+// the context; the last split also takes the tree's keys, which are bf16.  Two
+// kernels share the work by the number of rows: up to 64 rows a pass of
+// independent waves (kv4_narrow_kernel), above a pipeline over tiles of 64 keys
+// (kv4_verify_kernel).  Both convert the codes to bf16 (exact: E2M1 times a power
+// of two; v_cvt_scalef32_pk_bf16_fp4, two values in 6 to 8 cycles of a wave) and
+// multiply on bf16 matrix products with fp32 sums.  The matrix instructions that
+// take 4-bit operands beside 8-bit ones would save K's conversion, but drop
+// products below 2^-13 of the largest in a sum (measured), so they are not used.
+//
+// Where it stands (us a call, bytes and flops of the definition): single tokens,
+// 32 sequences x 8192 keys, 32 heads over 8: 48, 6.0 TB/s, HBM bound (a copy
+// moves 4.8, the fastest reads here 6.0 to 6.5); 16 x 8192, 52 nodes: 134, 0.83
+// PFLOP/s, and 8 x 32768, 64 over 8, 72 nodes: 640, 0.97 PFLOP/s, of the 1.14 of a
+// large library product: the matrix products (49 % of the cycles), the
+// exponentials and the conversions share two waves a SIMD.
 #include <algorithm>
 #include <type_traits>
 
@@ -109,11 +128,12 @@ __device__ __forceinline__ void mask_keys(f32x16_t& s, int n, uint32_t bits) {
   }
 }
 
-// Max, lazy rescale and the exponentials of 32 keys: P^T packed to bf16 in the
-// order of the B operand.  The running max moves only when it grows by more
-// than kRescaleSlack (a factor 256), which keeps the rescale of the output off
-// the common path; the weights are rounded to bf16 once for the product and
-// summed before that in fp32.
+// The softmax of 32 keys in pieces.  Logits, the running max (in log2 units), the
+// sum and O are fp32; the weights are rounded to bf16 once, as the operand of P V
+// (relative 2^-8, the size of the output's own rounding), and summed before that.
+// P^T comes in the order of the B operand.  The running max is any reference
+// within the exponent's range, not the true maximum: softmax_step moves it when
+// it lags by more than kRescaleSlack.
 __device__ __forceinline__ float row_max(const f32x16_t& s) {
   float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
@@ -196,8 +216,28 @@ __device__ __forceinline__ void v_offsets(int (&vofs)[2][kD / 32]) {
   }
 }
 
-// R 32-row blocks per workgroup; 8 / R waves share one and take 32 * R / 4 keys
-// of every tile each.
+// ------------------------------------------------------------ more than 64 rows
+//
+// R 32-row blocks per workgroup; with R = 8 every wave owns one and takes both
+// 32-key halves of each tile, with R = 4 two waves share one and take a half
+// each.  Tiles of 64 keys are converted once per workgroup, by all its waves, into
+// a ring of 4 bf16 stages in LDS (128 KiB): while tile t is computed, tile t + 1 is
+// written and the codes of t + 2 and t + 3 are in flight in registers (10 of
+// them, against 128 KiB of LDS for bf16 tiles).  One barrier a tile publishes the
+// next tile and frees the one before.  The loop is software-pipelined over half
+// tiles: the products P V of half h - 1 and S of half h + 1 are issued beside the
+// exponentials of half h, with every LDS address a lane offset plus an immediate
+// (the loop is unrolled over the ring).
+//
+// A tile takes 1.9 us with R = 8 and 1.1 with R = 4, all CUs busy; a SIMD's share
+// is 64 products (1.0 us) and some 2200 cycles of vector instructions, of which
+// the exponentials are 1000 and the conversions 450.  What did not help, us a call
+// before / after: matrix products at a raised wave priority 141 / 149 (16 x 8192,
+// 52 nodes), the exponentials 141 / 148, the two waves of a SIMD in turn 141 / 146;
+// one product to four vector instructions by scheduling groups 141 / 146; V
+// fragments requested a half ahead 141 / 142; the tree's tiles first 22.5 / 23.3 (1
+// x 4096, 44 nodes); results written through LDS in whole lines 49 / 51 (4 x 2048,
+// 136 nodes).
 template <int R>
 __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a) {
   static_assert(R == 8 || R == 4, "one or two waves per row block");
@@ -1186,22 +1226,33 @@ hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Pl
   a.ws_o = static_cast<float*>(c.ws);
   a.ws_ml = c.ws ? reinterpret_cast<float2*>(static_cast<float*>(c.ws) + slots * kD) : nullptr;
   const int units = c.B * c.Hkv * p.nsplit;
-  constexpr size_t kPlainBytes = (size_t)64 << 20;
   const dim3 grid((unsigned)((units + 7) / 8 * 8 * p.rowgroups));
+  // A model's layers each bring their own cache, so a call finds its codes in
+  // HBM; where one wave reads each of them, large ones are streamed past the
+  // caches.  us a call over rotating caches, plain / non-temporal: single tokens,
+  // 32 x 8192 keys of 8 kv heads (256 MiB of codes) 58.5 / 54.5, 4 x 30000 (117)
+  // 35.4 / 32.5; 8 nodes, 16 x 4096 (64) 29.4 / 27.9; 8 x 2048 (16) 12.9 / 12.9.
+  // Called again on the same cache, plain loads find it in the last-level cache:
+  // 49.4 / 54.4, 29.4 / 30.8, 25.4 / 27.3, 10.8 / 11.3; so small ones load plainly.
+  // Two row blocks read the codes twice: chains of 16 nodes, 32 x 4096 62.5 / 63.5.
+  constexpr size_t kPlainBytes = (size_t)64 << 20;
   const bool stream_kv = (size_t)c.B * c.L_max * c.Hkv * 2 * kKv4RowBytes >= kPlainBytes;
-  auto narrow = [&](auto rows, auto rb) {
-    using Rows = decltype(rows);
-    constexpr int kRb = decltype(rb)::value;
-    const dim3 g((unsigned)units);
-    if (stream_kv) hipLaunchKernelGGL((kv4_narrow_kernel<Rows, kRb, true>), g, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv4_narrow_kernel<Rows, kRb, false>), g, dim3(kThreads), 0, stream, a);
+  auto narrow = [&](auto rows, auto rb, auto st) {
+    hipLaunchKernelGGL((kv4_narrow_kernel<decltype(rows), decltype(rb)::value, decltype(st)::value>),
+                       dim3((unsigned)units), dim3(kThreads), 0, stream, a);
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
   switch (p.rows) {
-    case 16: narrow(Rows16{}, One{}); break;
-    case 32: narrow(Rows32{}, One{}); break;
-    case 64: narrow(Rows32{}, Two{}); break;
+    case 16:
+      if (stream_kv) narrow(Rows16{}, One{}, std::true_type{});
+      else narrow(Rows16{}, One{}, std::false_type{});
+      break;
+    case 32:
+      if (stream_kv) narrow(Rows32{}, One{}, std::true_type{});
+      else narrow(Rows32{}, One{}, std::false_type{});
+      break;
+    case 64: narrow(Rows32{}, Two{}, std::false_type{}); break;
     case 128: hipLaunchKernelGGL(kv4_verify_kernel<4>, grid, dim3(kThreads), 0, stream, a); break;
     default: hipLaunchKernelGGL(kv4_verify_kernel<8>, grid, dim3(kThreads), 0, stream, a); break;
   }
