@@ -200,3 +200,18 @@ def test_layout_stays_in_the_pool(tmp_path):
                     build.INCLUDE, "-I", build.CSRC, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout == "ok\n", r.returncode
+
+
+@pytest.mark.skipif(shutil.which("g++") is None or "ADAPLD_LIB" in os.environ, reason="needs g++; not from its own child")
+def test_refusals_under_sanitizers():
+    """This file's calls against the C-ABI glue under AddressSanitizer and UBSan."""
+    import sys
+    lib = build.build_host_sanitized()
+    env = dict(os.environ, ADAPLD_LIB=lib, LD_PRELOAD=build.sanitizer_preload(),
+               ASAN_OPTIONS="detect_leaks=0:halt_on_error=1:abort_on_error=1",
+               UBSAN_OPTIONS="halt_on_error=1:print_stacktrace=1")
+    r = subprocess.run([sys.executable, "-m", "pytest", "-q", "-p", "no:cacheprovider", "-k", "refusals or workspace",
+                        os.path.abspath(__file__)], cwd=build.ROOT, env=env, capture_output=True, text=True, timeout=600)
+    out = r.stdout + r.stderr
+    assert r.returncode == 0, out[-4000:]
+    assert "AddressSanitizer" not in out and "runtime error" not in out, out[-4000:]
