@@ -9,6 +9,7 @@ the same bits.  If the library is missing, every call raises AdapldError.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -177,6 +178,17 @@ def _dptr(t, name, dtypes, shape, dev, nullable=False):
     if p is not None and t.get_device() != dev:
         raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
     return p
+
+
+def _on(stream, dev):
+    """Where a call on the 4-bit cache makes its buffers: on the stream that it
+    launches on, so that the allocator hands a freed one out again in that
+    stream's order, and a new one's fill comes before the kernel."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if stream.device.index != dev:
+        raise AdapldError(-2, f"the stream is of {stream.device}, the current device is cuda:{dev}")
+    return torch.cuda.stream(stream)
 
 
 def _device_of(t, name):
@@ -475,7 +487,7 @@ class Kv4Cache:
     takes the table and the stack, the other calls the pool and (the attention)
     the table.  allocate() makes an empty cache.  The buffers are checked and
     their pointers marshalled at the first call, and again after one of the
-    fields is assigned."""
+    fields is assigned or a buffer's memory has moved."""
     k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
     k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
     v_codes: torch.Tensor
@@ -509,7 +521,10 @@ class Kv4Cache:
 
     def _marshal_pool(self, dev):
         """(device, pointers of the four arrays, n_pages, Hkv, D)."""
-        if self._pool is None or self._pool[0] != dev:
+        pool = self._pool
+        if (pool is None or pool[0] != dev
+                or pool[1] != (self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
+                               self.v_scales.data_ptr())):
             u8 = (torch.uint8,)
             _device_of(self.k_codes, "k_codes")
             if self.k_codes.dim() != 4:
@@ -519,16 +534,19 @@ class Kv4Cache:
             scales = (n_pages, Hkv, self.page_size, 2 * half // KV4_GROUP)
             ptrs = (_dptr(self.k_codes, "k_codes", u8, codes, dev), _dptr(self.k_scales, "k_scales", u8, scales, dev),
                     _dptr(self.v_codes, "v_codes", u8, codes, dev), _dptr(self.v_scales, "v_scales", u8, scales, dev))
-            object.__setattr__(self, "_pool", (dev, ptrs, n_pages, Hkv, 2 * half))
-        return self._pool
+            pool = (dev, ptrs, n_pages, Hkv, 2 * half)
+            object.__setattr__(self, "_pool", pool)
+        return pool
 
     def _marshal_pages(self, dev):
         """(device, pointer of the page table, B, max_pages)."""
-        if self._pages is None or self._pages[0] != dev:
+        pages = self._pages
+        if pages is None or pages[0] != dev or pages[1] != self.page_table.data_ptr():
             _device_of(self.page_table, "page_table")
             B, max_pages = self.page_table.shape
-            object.__setattr__(self, "_pages", (dev, _dptr(self.page_table, "page_table", _I32, (B, max_pages), dev), B, max_pages))
-        return self._pages
+            pages = (dev, _dptr(self.page_table, "page_table", _I32, (B, max_pages), dev), B, max_pages)
+            object.__setattr__(self, "_pages", pages)
+        return pages
 
 
 _I32 = (torch.int32,)
@@ -545,10 +563,12 @@ def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, gran
     stack's count goes to free_count_out (default: in place)."""
     dev = _device_of(lens_old, "lens_old")
     _, table, B, max_pages = cache._marshal_pages(dev)
-    if slot_map is None:
-        slot_map = torch.empty((B, 0 if N is None else N), dtype=torch.int32, device=lens_old.device)
+    if slot_map is None or granted is None or stream is not None:
+        with _on(stream, dev):
+            if slot_map is None:
+                slot_map = torch.empty((B, 0 if N is None else N), dtype=torch.int32, device=lens_old.device)
+            granted = _i32(B, lens_old.device) if granted is None else granted
     N = slot_map.shape[1] if N is None else N
-    granted = _i32(B, lens_old.device) if granted is None else granted
     free_count = cache.free_count
     count = _dptr(free_count, "free_count", _I32, (1,), dev)
     count_out = count if free_count_out is None else _dptr(free_count_out, "free_count_out", _I32, (1,), dev)
@@ -572,6 +592,8 @@ def kv4_append(cache: Kv4Cache, k_new, v_new, slot_map, *, rows=None, stream=Non
     shape = k_new.shape
     B, n_src, heads, D = shape
     N = slot_map.shape[1]
+    if stream is not None:
+        _on(stream, dev)
     if heads != Hkv:
         raise AdapldError(-2, f"k_new has {heads} kv heads, the cache {Hkv}")
     st = load_library().adapld_kv4_append(
@@ -592,8 +614,10 @@ def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None
     B, N = slot_map.shape
     shape = (B, N, Hkv, D)
     new = lambda: torch.zeros(shape, dtype=torch.bfloat16, device=slot_map.device)  # noqa: E731
-    k_out = new() if k_out is None else k_out
-    v_out = new() if v_out is None else v_out
+    if k_out is None or v_out is None or stream is not None:
+        with _on(stream, dev):
+            k_out = new() if k_out is None else k_out
+            v_out = new() if v_out is None else v_out
     st = load_library().adapld_kv4_gather(
         *pool, _dptr(slot_map, "slot_map", _I32, None, dev), B, N, Hkv, D, cache.page_size, n_pages,
         _dptr(k_out, "k_out", _BF16_DTYPES, shape, dev), _dptr(v_out, "v_out", _BF16_DTYPES, shape, dev),
@@ -618,12 +642,14 @@ def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v
     T_max, Hq = shape[1], shape[2]
     L_max = max_pages * cache.page_size if L_max is None else L_max
     scale = 1.0 / math.sqrt(D) if scale is None else scale
-    out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if out is None else out
-    if lse is None and with_lse:
-        lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=q.device)
-    if ws is None:
-        need = workspace_bytes(OP_TREE_VERIFY_ATTN_KV4, B, L_max, 0, 0, T_max, Hq, Hkv, D)
-        ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    if out is None or lse is None or ws is None or stream is not None:
+        with _on(stream, dev):
+            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if out is None else out
+            if lse is None and with_lse:
+                lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=q.device)
+            if ws is None:
+                need = workspace_bytes(OP_TREE_VERIFY_ATTN_KV4, B, L_max, 0, 0, T_max, Hq, Hkv, D)
+                ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
     kt = vt = mask = None
     if k_tree is not None or v_tree is not None or tree_mask is not None:
         tree = (B, T_max, Hkv, D)

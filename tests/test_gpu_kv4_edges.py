@@ -136,10 +136,12 @@ def test_two_calls_at_once():
     outs = [(torch.zeros_like(o), torch.zeros_like(l)) for o, l in want]
     ws = [torch.empty(max(adapld.workspace_bytes(adapld.OP_TREE_VERIFY_ATTN_KV4, 2, c.L_max, 0, 0, c.T, 8, 2, 128), 16),
                       dtype=torch.uint8, device="cuda") for c in (a, d)]
+    sizes = [(i32(c.lens), i32(c.counts)) for c in (a, d)]
     torch.cuda.synchronize()
     for _ in range(5):
-        a.run(out=outs[0][0], lse=outs[0][1], ws=ws[0], stream=s1)
-        d.run(out=outs[1][0], lse=outs[1][1], ws=ws[1], stream=s2)
+        for c, n, (o, l), w, s in zip((a, d), sizes, outs, ws, (s1, s2)):
+            adapld.tree_verify_attn_kv4(c.q, c.cache, *n, k_tree=c.kt, v_tree=c.vt, tree_mask=c.mask, L_max=c.L_max,
+                                        out=o, lse=l, ws=w, stream=s)
     torch.cuda.synchronize()
     for (o, l), (wo, wl), c in zip(outs, want, (a, d)):
         for b, t in enumerate(c.counts):
@@ -166,6 +168,47 @@ def test_exchanged_buffers_are_seen():
     c.cache.k_scales = old.cpu()
     with pytest.raises(adapld.AdapldError):
         c.run()
+
+
+def test_moved_buffers_are_seen():
+    """A buffer whose memory is exchanged in place is marshalled again."""
+    c = Case([64], 4, 2, 1, [1], 16, 64, 109)
+    out, lse = c.run()
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales", "page_table"):
+        t = getattr(c.cache, name)
+        old = t.data
+        t.data = old.clone()
+        old.fill_(1)             # finite codes, page 1
+        o2, l2 = c.run()
+        assert torch.equal(out, o2) and torch.equal(lse, l2), name
+
+
+def test_own_buffers_belong_to_the_stream():
+    """What a call on another stream makes for itself is of that stream: its
+    fill comes before the kernel, and memory that it frees is not handed out on
+    the current stream while the kernel is still to come."""
+    c = Case([3000, 2000], 8, 2, 5, [5, 5], 64, 3000, 127, tree="random")
+    want, want_lse = (t.clone() for t in c.run())
+    slots = i32([[0, 5, 17]])
+    k_want, v_want = (t.clone() for t in adapld.kv4_gather(c.cache, slots))
+    lens, counts = i32(c.lens), i32(c.counts)
+    need = adapld.workspace_bytes(adapld.OP_TREE_VERIFY_ATTN_KV4, 2, c.L_max, 0, 0, 5, 8, 2, 128)
+    assert need > 0
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    out, lse = adapld.tree_verify_attn_kv4(c.q, c.cache, lens, counts, k_tree=c.kt, v_tree=c.vt, tree_mask=c.mask,
+                                           L_max=c.L_max, stream=s)
+    others = [torch.full((n,), 7, dtype=torch.uint8, device="cuda") for n in (need, out.numel() * 2, lse.numel() * 4)]
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert all(bool((t == 7).all()) for t in others)
+    torch.cuda._sleep(20_000_000)           # a fill on the current stream would come late
+    k, v = adapld.kv4_gather(c.cache, slots, stream=s)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(k, k_want) and torch.equal(v, v_want)
 
 
 def test_refusals_of_gpu_tensors():
