@@ -1097,6 +1097,7 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
 // O_s/l_s with weight l_s 2^(m_s - M).
 constexpr int kCombineThreads = 256;
 constexpr int kCombineRows = kCombineThreads / 32;
+template <int GROUP>
 __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4Args a) {
   const VerifyKv4Call& c = a.c;
   const uint32_t row = blockIdx.x * kCombineRows + threadIdx.x / 32;
@@ -1107,22 +1108,21 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
   const int nodes = c.node_count[b];
   const int dim = (threadIdx.x & 31) * 4;
   const size_t row0 = (size_t)bg * a.nsplit * a.rows_max + qr;
-  // In index order, eight splits' loads in flight at a time.
+  // In index order, GROUP splits' loads in flight at a time.
   float M = -INFINITY, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int kGroup = 8;
-  for (int s0 = 0; s0 < a.nsplit; s0 += kGroup) {
-    float2 ml[kGroup];
-    float4 v[kGroup];
+  for (int s0 = 0; s0 < a.nsplit; s0 += GROUP) {
+    float2 ml[GROUP];
+    float4 v[GROUP];
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
+    for (int j = 0; j < GROUP; ++j) {
       const bool in = s0 + j < a.nsplit;
       const size_t at = row0 + (size_t)(s0 + j) * a.rows_max;
       ml[j] = in ? a.ws_ml[at] : make_float2(-INFINITY, 0.f);
       v[j] = in ? *reinterpret_cast<const float4*>(a.ws_o + at * kD + dim) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
-    for (int j = 0; j < kGroup; ++j) {
+    for (int j = 0; j < GROUP; ++j) {
       if (ml[j].y > 0.f) {
         const float m_new = fmaxf(M, ml[j].x);
         const float keep = exp2f(M - m_new);   // 0 while nothing has been merged
@@ -1193,13 +1193,18 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
     const int units = (L_max + s.unit - 1) / s.unit;   // L_max is at most 2^30
     const int least = (int)(((int64_t)units * s.unit + kMaxChunk - 1) / kMaxChunk);
     const int most = std::max(least, std::min(64, units));
+    // Of the tile shapes the last split's units include the tree's (1 x 4096, 44
+    // nodes: 13 splits of 5 tiles 21.6, 16 of 4 and one more 21.9).  Of the narrow
+    // ones two waves take the tree beside the others' context (counted the same
+    // way, single tokens, 1 x 4096, 11.6 -> 12.7).
+    const int beside = s.narrow ? tree : 0;
     for (int want = least; want <= most; ++want) {
-      const int per = (units + want - 1) / want;   // units of a split
+      const int per = (units + tree - beside + want - 1) / want;   // units of a split
       const int nsplit = (units + per - 1) / per;
-      if (nsplit != want) continue;   // the same split as a smaller count
+      if (nsplit != want && want > least) continue;   // the same split as a smaller count
       const int64_t wgs = pairs * rowgroups * nsplit;
       const double rounds = (double)((wgs + kCUs - 1) / kCUs);
-      double cost = std::max(rounds * (s.start + mean * (per + tree)), s.start + longest * (per + tree));
+      double cost = std::max(rounds * (s.start + mean * (per + beside)), s.start + longest * (per + beside));
       if (nsplit > 1)
         cost += kCombine + (double)(pairs * nsplit) * rows_max * 2 * (kD * 4 + 8) / kPartialBytesPerUs;
       if (best.rows == 0 || cost < best_cost) {
@@ -1259,8 +1264,13 @@ hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Pl
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const unsigned n_rows = (unsigned)c.B * c.Hkv * p.rows_max;
-  hipLaunchKernelGGL(kv4_combine_kernel, dim3((n_rows + kCombineRows - 1) / kCombineRows), dim3(kCombineThreads), 0,
-                     stream, a);
+  const dim3 merge_grid((n_rows + kCombineRows - 1) / kCombineRows);
+  // us a call, eight / four at a time: 2 splits 140.9 / 139.6 and 94.0 / 92.8 (registers
+  // that no split fills cost waves), 16 splits 11.8 / 12.2 (more round trips).
+  if (p.nsplit <= 4)
+    hipLaunchKernelGGL(kv4_combine_kernel<4>, merge_grid, dim3(kCombineThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(kv4_combine_kernel<8>, merge_grid, dim3(kCombineThreads), 0, stream, a);
   return hipGetLastError();
 }
 
