@@ -180,6 +180,11 @@ def _dptr(t, name, dtypes, shape, dev, nullable=False):
     return p
 
 
+def _stream_on(stream, dev):
+    """_stream for a call that has asked for the current device already."""
+    return _raw_stream(dev) if stream is None and _raw_stream is not None else _stream(stream)
+
+
 def _on(stream, dev):
     """Where a call on the 4-bit cache makes its buffers: on the stream that it
     launches on, so that the allocator hands a freed one out again in that
@@ -193,7 +198,7 @@ def _on(stream, dev):
 
 def _device_of(t, name):
     """The current device, for a call whose first tensor is t."""
-    if not isinstance(t, torch.Tensor):
+    if type(t) is not _Tensor and not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.get_device() < 0:
         raise AdapldError(-2, f"{name} must live on the GPU (got {t.device})")
@@ -577,7 +582,7 @@ def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, gran
         _dptr(lens_old, "lens_old", _I32, (B,), dev), _dptr(lens_new, "lens_new", _I32, (B,), dev), B,
         cache.page_size, max_pages, n_pages, N, table, _dptr(cache.free_pages, "free_pages", _I32, (n_pages,), dev),
         count, count_out, _dptr(slot_map, "slot_map", _I32, (B, N), dev), _dptr(granted, "granted", _I32, (B,), dev),
-        _stream(stream))
+        _stream_on(stream, dev))
     if st:
         _check(st, "adapld_kv4_page_map")
     return slot_map, granted
@@ -600,7 +605,7 @@ def kv4_append(cache: Kv4Cache, k_new, v_new, slot_map, *, rows=None, stream=Non
         _dptr(k_new, "k_new", _BF16_DTYPES, None, dev), _dptr(v_new, "v_new", _BF16_DTYPES, shape, dev),
         None if rows is None else _dptr(rows, "rows", _I32, (B, N), dev),
         _dptr(slot_map, "slot_map", _I32, (B, N), dev), B, n_src, N, Hkv, D, cache.page_size, n_pages, *pool,
-        _stream(stream))
+        _stream_on(stream, dev))
     if st:
         _check(st, "adapld_kv4_append")
 
@@ -621,7 +626,7 @@ def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None
     st = load_library().adapld_kv4_gather(
         *pool, _dptr(slot_map, "slot_map", _I32, None, dev), B, N, Hkv, D, cache.page_size, n_pages,
         _dptr(k_out, "k_out", _BF16_DTYPES, shape, dev), _dptr(v_out, "v_out", _BF16_DTYPES, shape, dev),
-        _stream(stream))
+        _stream_on(stream, dev))
     if st:
         _check(st, "adapld_kv4_gather")
     return k_out, v_out
@@ -661,7 +666,7 @@ def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v
         _dptr(node_count, "node_count", _I32, (B,), dev), mask, B, L_max, T_max, Hq, Hkv, D, cache.page_size, n_pages,
         max_pages, scale, _dptr(out, "out", _BF16_DTYPES, shape, dev),
         None if lse is None else _dptr(lse, "lse", _F32, (B, Hq, T_max), dev),
-        _dptr(ws, "ws", _U8, None, dev), ws.numel(), _stream(stream))
+        _dptr(ws, "ws", _U8, None, dev), ws.numel(), _stream_on(stream, dev))
     if st:
         _check(st, "adapld_tree_verify_attn_kv4")
     return out, lse

@@ -17,7 +17,7 @@
 // 32 sequences x 8192 keys, 32 heads over 8: 48, 6.0 TB/s, HBM bound (a copy
 // moves 4.8, the fastest reads here 6.0 to 6.5); 16 x 8192, 52 nodes: 134, 0.83
 // PFLOP/s, and 8 x 32768, 64 over 8, 72 nodes: 640, 0.97 PFLOP/s, of the 1.14 of a
-// large library product: the matrix products (49 % of the cycles), the
+// large library product: the matrix products (48 % of the cycles), the
 // exponentials and the conversions share two waves a SIMD.
 #include <algorithm>
 #include <type_traits>
