@@ -14,11 +14,12 @@
 // products below 2^-13 of the largest in a sum (measured), so they are not used.
 //
 // Where it stands (us a call, bytes and flops of the definition): single tokens,
-// 32 sequences x 8192 keys, 32 heads over 8: 48, 6.0 TB/s, HBM bound (a copy
-// moves 4.8, the fastest reads here 6.0 to 6.5); 16 x 8192, 52 nodes: 134, 0.83
-// PFLOP/s, and 8 x 32768, 64 over 8, 72 nodes: 640, 0.97 PFLOP/s, of the 1.14 of a
-// large library product: the matrix products (48 % of the cycles), the
-// exponentials and the conversions share two waves a SIMD.
+// 32 sequences x 8192 keys, 32 heads over 8: 46, 6.2 TB/s, HBM bound (a copy
+// moves 4.8, the fastest reads here 6.0 to 6.5); chains of 16 nodes, 32 x 4096: 53,
+// two row blocks convert the same codes; 16 x 8192, 52 nodes: 129 to 137 by the box,
+// 0.82 to 0.86 PFLOP/s, and 8 x 32768, 64 over 8, 72 nodes: 623 to 658, 0.94 to 0.99,
+// of the 1.14 of a large library product: the matrix products (48 % of the cycles),
+// the exponentials and the conversions share two waves a SIMD.
 #include <algorithm>
 #include <type_traits>
 
@@ -1163,7 +1164,7 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
   // choice / at the next best): 16 x 8192 keys, 32 heads over 8, 52 nodes 256
   // rows in 2 splits 144 / 128 rows unsplit 153; 8 x 32768, 64 over 8, 72 nodes
   // 256 rows in 4 636 / 128 in 4 681; 4 x 2048, 40 over 8, 136 nodes 128 unsplit
-  // 49 / 256 in 2 61; 1 x 4096, 32 over 8, 44 nodes 128 in 16 22.6 / in 8 23.6;
+  // 49 / 256 in 2 61; 1 x 4096, 32 over 8, 44 nodes 128 in 13 21.6 / in 16 21.9;
   // single tokens, 4 x 30000, 64 over 8 in 8 34 / in 6 37; 8 x 2048, 32 over 8 in
   // 4 12.9 / in 2 13.6.
   constexpr int kCUs = 256;
