@@ -533,6 +533,8 @@ int adapld_accept_greedy(const int32_t* node_token, const int32_t* node_parent,
  * (E2M1: sign, then 0 .5 1 1.5 2 3 4 6; dimension 2i in the low half of byte
  * i, 2i + 1 in the high half) and one scale byte e for every
  * ADAPLD_KV4_GROUP dimensions; a value is E2M1 * 2^(e - 127), exact in bf16.
+ * e is 1..252 (adapld_kv4_append writes no other byte; rows with another one
+ * read as unspecified values).
  *
  *   k_codes, v_codes    uint8 [n_pages, Hkv, page_size, D / 2]
  *   k_scales, v_scales  uint8 [n_pages, Hkv, page_size, D / ADAPLD_KV4_GROUP]
