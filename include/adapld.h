@@ -579,9 +579,8 @@ int adapld_accept_greedy(const int32_t* node_token, const int32_t* node_parent,
  *   free_count          int32 [1]              pages on the stack
  *   free_count_out      int32 [1]       (out)  the count after the call; may be
  *                       free_count itself.  With another buffer the call can
- *                       be made again on the same inputs, and many slots
- *                       (B * N > 4096) of up to 1024 sequences cost no second
- *                       launch.
+ *                       be made again on the same inputs, and the slots of up
+ *                       to 1024 sequences are filled beside the pages.
  *   N                   >= 0 slots per sequence; slot_map may be NULL if 0
  *   slot_map            int32 [B, N]    (out)
  *   granted             int32 [B]       (out)  1, or 0 where pages ran out

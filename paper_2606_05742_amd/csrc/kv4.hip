@@ -22,12 +22,11 @@ namespace {
 // The slots of a batch that is one such group are filled in the same launch by
 // the other workgroups, which repeat the prefix sums and work out the page of a
 // new token from what workgroup 0 does not write: the old count, the stack below
-// it and the table entries that were held before the call.  Calls with few slots
-// leave them to workgroup 0; larger batches, and calls that update the count in
-// place, take a second launch.
+// it and the table entries that were held before the call.  Larger batches, and
+// calls that update the count in place, leave few slots to workgroup 0 and take a
+// second launch for many.
 constexpr int kMapThreads = 1024;
 constexpr int kMapWaves = kMapThreads / kWave;
-constexpr int kSlotsPerThread = 4;
 enum SlotsBy { kSlotsByFirst, kSlotsByOthers, kSlotsLater };
 
 struct MapArgs {
@@ -102,19 +101,17 @@ __device__ void fill_slots_beside(const MapArgs& a, int* s_back, int* s_need, in
   const int height = (int)min<int64_t>((int64_t)start + total, a.n_pages);
   s_need[tid] = block_incl_scan(need, s_wave, total);
   __syncthreads();
-  const int per_row = (a.N + kMapThreads * kSlotsPerThread - 1) / (kMapThreads * kSlotsPerThread);   // workgroups of a row
-  const int wg = blockIdx.x - 1, b = wg / per_row;
-  const int o = clamp_len(a.lens_old[b], a), n = clamp_len(a.lens_new[b], a);
-  const int held = pages_of(o, shift);
-  const int before = b > 0 ? s_need[b - 1] : 0;
-  const bool granted = s_need[b] <= height || s_need[b] == before;
-  const int i0 = (wg - b * per_row) * kMapThreads * kSlotsPerThread;
-#pragma unroll
-  for (int k = 0; k < kSlotsPerThread; ++k) {
-    const int i = i0 + k * kMapThreads + tid;
-    if (i >= a.N) break;
+  // The batch's slots end to end over the workgroups; B * N fits 31 bits by the
+  // host's check, so one more round fits 32.
+  const uint32_t end = (uint32_t)a.B * (uint32_t)a.N, step = (gridDim.x - 1) * kMapThreads;
+  for (uint32_t at_slot = (blockIdx.x - 1) * kMapThreads + tid; at_slot < end; at_slot += step) {
+    const int b = (int)(at_slot / (uint32_t)a.N), i = (int)(at_slot - (uint32_t)b * (uint32_t)a.N);
+    const int o = clamp_len(a.lens_old[b], a), n = clamp_len(a.lens_new[b], a);
+    const int before = b > 0 ? s_need[b - 1] : 0;
+    const bool granted = s_need[b] <= height || s_need[b] == before;
     int slot = -1;
     if (granted && i < n - o) {
+      const int held = pages_of(o, shift);
       const int pos = o + i, at = pos >> shift;
       int page;
       if (at < held) {
@@ -130,7 +127,7 @@ __device__ void fill_slots_beside(const MapArgs& a, int* s_back, int* s_need, in
       }
       slot = slot_in_page(a, page, pos);
     }
-    a.slot_map[(size_t)b * a.N + i] = slot;
+    a.slot_map[at_slot] = slot;
   }
 }
 
@@ -220,6 +217,7 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapArgs a, 
 
 // Slots of a larger batch, after the pages.
 constexpr int kSlotThreads = 256;
+constexpr int kSlotsPerThread = 4;
 __global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(const MapArgs a) {
   const int b = blockIdx.y;
   const int o = clamp_len(a.lens_old[b], a), n = clamp_len(a.lens_new[b], a);
@@ -364,12 +362,18 @@ hipError_t launch_kv4_page_map(const int32_t* lens_old, const int32_t* lens_new,
   a.B = B; a.page_shift = log2_pow2(page_size); a.max_pages = max_pages; a.n_pages = n_pages; a.N = N;
   a.page_table = page_table; a.free_pages = free_pages; a.free_count = free_count;
   a.free_count_out = free_count_out; a.slot_map = slot_map; a.granted = granted;
+  // us a call inside a graph, slots by the other workgroups / by the first: 16 x 13
+  // slots 4.2 / 4.5, 64 x 64 4.2 / 5.9, 16 x 2048 5.0 / 18.  In place, by a second
+  // launch / by the first: 16 x 13 5.6 / 4.1, 64 x 64 5.8 / 5.0, 64 x 128 5.6 / 6.1.
   constexpr int kFewSlots = 4 * kMapThreads;
-  const SlotsBy slots = (int64_t)B * N <= kFewSlots                           ? kSlotsByFirst
+  constexpr int64_t kOthersMax = 2 * 256 - 1;   // two workgroups a CU; they take the slots in turn
+  const int64_t total = (int64_t)B * N;
+  const SlotsBy slots = N == 0                                               ? kSlotsByFirst
                         : B <= kMapThreads && free_count_out != free_count ? kSlotsByOthers
+                        : total <= kFewSlots                               ? kSlotsByFirst
                                                                            : kSlotsLater;
-  constexpr int kPerGroup = kMapThreads * kSlotsPerThread;
-  const unsigned others = slots == kSlotsByOthers ? (unsigned)((N + kPerGroup - 1) / kPerGroup) * B : 0u;
+  const int64_t groups = (total + kMapThreads - 1) / kMapThreads;
+  const unsigned others = slots == kSlotsByOthers ? (unsigned)(groups < kOthersMax ? groups : kOthersMax) : 0u;
   hipLaunchKernelGGL(page_map_kernel, dim3(1 + others), dim3(kMapThreads), 0, stream, a, slots);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || slots != kSlotsLater) return e;

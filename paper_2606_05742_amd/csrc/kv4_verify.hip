@@ -1175,6 +1175,10 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
     int unit;       // keys of a step of the workgroup
     double start, per_unit, per_unit_half;   // the latter where at most half the rows live
   };
+  // Up to 64 rows the narrow shape that just holds them, us at it / at the next
+  // larger one: single tokens 32 x 8192 55 / 61, 1 x 4096 11.1 / 11.5 (4 rows); 32
+  // rows, 16 x 4096 27.5 / 37.5; 64 rows, 32 x 4096 60.8 / 76.7, 4 x 4096 20.1 / 22.2
+  // (through a graph that keeps the card at its power limit).
   const Shape shapes[] = {{16, true, kWaves * kStep, 5.5, 1.3, 1.3},
                           {32, true, kWaves * kStep, 5.5, 2.0, 2.0},
                           {64, true, kWaves / 2 * kStep, 5.5, 1.7, 1.7},

@@ -239,7 +239,7 @@ def test_refusals_of_gpu_tensors():
 
 
 @pytest.mark.parametrize("B, N, in_place", [(1024, 9, False), (1025, 9, False), (1024, 9, True), (3, 6000, True),
-                                            (2, 4096, False), (700, 33, False)])
+                                            (2, 4096, False), (700, 33, False), (1, 1, True), (90, 6000, False)])
 def test_page_map_every_way_to_the_slots(B, N, in_place):
     """Slots by the first workgroup, by others beside it, by a second launch,
     with sequences that give back what others take."""
