@@ -506,6 +506,7 @@ class Kv4Cache:
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_pool", None)
         object.__setattr__(self, "_pages", None)
+        object.__setattr__(self, "_stack", None)
 
     @staticmethod
     def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
@@ -553,6 +554,18 @@ class Kv4Cache:
             object.__setattr__(self, "_pages", pages)
         return pages
 
+    def _marshal_stack(self, dev):
+        """(device, pointers of free_pages and free_count, n_pages)."""
+        stack = self._stack
+        if stack is None or stack[0] != dev or stack[1] != (self.free_pages.data_ptr(), self.free_count.data_ptr()):
+            _device_of(self.free_pages, "free_pages")
+            n_pages = self.free_pages.shape[0]
+            ptrs = (_dptr(self.free_pages, "free_pages", _I32, (n_pages,), dev),
+                    _dptr(self.free_count, "free_count", _I32, (1,), dev))
+            stack = (dev, ptrs, n_pages)
+            object.__setattr__(self, "_stack", stack)
+        return stack
+
 
 _I32 = (torch.int32,)
 _F32 = (torch.float32,)
@@ -574,14 +587,12 @@ def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, gran
                 slot_map = torch.empty((B, 0 if N is None else N), dtype=torch.int32, device=lens_old.device)
             granted = _i32(B, lens_old.device) if granted is None else granted
     N = slot_map.shape[1] if N is None else N
-    free_count = cache.free_count
-    count = _dptr(free_count, "free_count", _I32, (1,), dev)
+    _, (free_pages, count), n_pages = cache._marshal_stack(dev)
     count_out = count if free_count_out is None else _dptr(free_count_out, "free_count_out", _I32, (1,), dev)
-    n_pages = cache.free_pages.shape[0]
     st = load_library().adapld_kv4_page_map(
         _dptr(lens_old, "lens_old", _I32, (B,), dev), _dptr(lens_new, "lens_new", _I32, (B,), dev), B,
-        cache.page_size, max_pages, n_pages, N, table, _dptr(cache.free_pages, "free_pages", _I32, (n_pages,), dev),
-        count, count_out, _dptr(slot_map, "slot_map", _I32, (B, N), dev), _dptr(granted, "granted", _I32, (B,), dev),
+        cache.page_size, max_pages, n_pages, N, table, free_pages, count, count_out,
+        _dptr(slot_map, "slot_map", _I32, (B, N), dev), _dptr(granted, "granted", _I32, (B,), dev),
         _stream_on(stream, dev))
     if st:
         _check(st, "adapld_kv4_page_map")

@@ -183,6 +183,21 @@ def test_moved_buffers_are_seen():
         assert torch.equal(out, o2) and torch.equal(lse, l2), name
 
 
+def test_moved_stack_is_seen():
+    cache = adapld.Kv4Cache.allocate(6, 16, 1, 2, 3)
+    assert adapld.page_map(cache, i32([0, 0]), i32([16, 17]), 1)[0].tolist() == [[0], [16]]
+    for t, v in ((cache.free_pages, [5, 4, 3, -1, -1, -1]), (cache.free_count, [3])):
+        old = t.data
+        t.data = i32(v)
+        old.fill_(0)             # an empty stack of page 0
+    slots, granted = adapld.page_map(cache, i32([16, 17]), i32([32, 33]), 17)
+    assert granted.tolist() == [1, 1] and slots[0, :16].tolist() == list(range(48, 64))
+    assert slots[1].tolist() == list(range(33, 48)) + [64, -1] and cache.free_count.tolist() == [1]
+    with pytest.raises(adapld.AdapldError):
+        cache.free_count = cache.free_count.long()
+        adapld.page_map(cache, i32([32, 33]), i32([32, 33]), 1)
+
+
 def test_own_buffers_belong_to_the_stream():
     """What a call on another stream makes for itself is of that stream: its
     fill comes before the kernel, and memory that it frees is not handed out on
