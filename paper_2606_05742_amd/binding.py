@@ -510,6 +510,8 @@ class Kv4Cache:
 
     @staticmethod
     def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
+        if D != HEAD_DIM:
+            raise AdapldError(-3, f"the cache's rows have {HEAD_DIM} dimensions, not {D}")
         u8 = lambda n: torch.empty((n_pages, Hkv, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
         return Kv4Cache(
             k_codes=u8(D // 2), k_scales=u8(D // KV4_GROUP), v_codes=u8(D // 2), v_scales=u8(D // KV4_GROUP),
@@ -604,14 +606,14 @@ def kv4_append(cache: Kv4Cache, k_new, v_new, slot_map, *, rows=None, stream=Non
     rows[b, i] (row i without rows) of sequence b at slot_map[b, i]; slots of
     -1 are padding."""
     dev = _device_of(k_new, "k_new")
-    _, pool, n_pages, Hkv, _ = cache._marshal_pool(dev)
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
     shape = k_new.shape
-    B, n_src, heads, D = shape
+    if len(shape) != 4 or shape[2] != Hkv or shape[3] != D:
+        raise AdapldError(-2, f"k_new has shape {tuple(shape)}, expected (B, n_src, {Hkv}, {D})")
+    B, n_src = shape[0], shape[1]
     N = slot_map.shape[1]
     if stream is not None:
         _on(stream, dev)
-    if heads != Hkv:
-        raise AdapldError(-2, f"k_new has {heads} kv heads, the cache {Hkv}")
     st = load_library().adapld_kv4_append(
         _dptr(k_new, "k_new", _BF16_DTYPES, None, dev), _dptr(v_new, "v_new", _BF16_DTYPES, shape, dev),
         None if rows is None else _dptr(rows, "rows", _I32, (B, N), dev),
