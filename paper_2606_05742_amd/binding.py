@@ -492,7 +492,7 @@ class Kv4Cache:
     takes the table and the stack, the other calls the pool and (the attention)
     the table.  allocate() makes an empty cache.  The buffers are checked and
     their pointers marshalled at the first call, and again after one of the
-    fields is assigned or a buffer's memory has moved."""
+    fields is assigned or a buffer has another address, shape, type or layout."""
     k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
     k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
     v_codes: torch.Tensor
@@ -527,12 +527,26 @@ class Kv4Cache:
     def Hkv(self):
         return self.k_codes.shape[1]
 
+    # What the marshalled pointers hold for: the device and every buffer's
+    # address, shape, type and contiguity, all of which a tensor can change in place.
+    def _pool_key(self, dev):
+        kc, ks, vc, vs = self.k_codes, self.k_scales, self.v_codes, self.v_scales
+        return (dev, kc.data_ptr(), kc.shape, kc.dtype, kc.is_contiguous(), ks.data_ptr(), ks.shape, ks.dtype,
+                ks.is_contiguous(), vc.data_ptr(), vc.shape, vc.dtype, vc.is_contiguous(), vs.data_ptr(), vs.shape,
+                vs.dtype, vs.is_contiguous())
+
+    def _pages_key(self, dev):
+        t = self.page_table
+        return dev, t.data_ptr(), t.shape, t.dtype, t.is_contiguous()
+
+    def _stack_key(self, dev):
+        t, n = self.free_pages, self.free_count
+        return dev, t.data_ptr(), t.shape, t.dtype, t.is_contiguous(), n.data_ptr(), n.shape, n.dtype, n.is_contiguous()
+
     def _marshal_pool(self, dev):
-        """(device, pointers of the four arrays, n_pages, Hkv, D)."""
+        """(key, pointers of the four arrays, n_pages, Hkv, D)."""
         pool = self._pool
-        if (pool is None or pool[0] != dev
-                or pool[1] != (self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(),
-                               self.v_scales.data_ptr())):
+        if pool is None or pool[0] != self._pool_key(dev):
             u8 = (torch.uint8,)
             _device_of(self.k_codes, "k_codes")
             if self.k_codes.dim() != 4:
@@ -542,29 +556,31 @@ class Kv4Cache:
             scales = (n_pages, Hkv, self.page_size, 2 * half // KV4_GROUP)
             ptrs = (_dptr(self.k_codes, "k_codes", u8, codes, dev), _dptr(self.k_scales, "k_scales", u8, scales, dev),
                     _dptr(self.v_codes, "v_codes", u8, codes, dev), _dptr(self.v_scales, "v_scales", u8, scales, dev))
-            pool = (dev, ptrs, n_pages, Hkv, 2 * half)
+            pool = (self._pool_key(dev), ptrs, n_pages, Hkv, 2 * half)
             object.__setattr__(self, "_pool", pool)
         return pool
 
     def _marshal_pages(self, dev):
-        """(device, pointer of the page table, B, max_pages)."""
+        """(key, pointer of the page table, B, max_pages)."""
         pages = self._pages
-        if pages is None or pages[0] != dev or pages[1] != self.page_table.data_ptr():
+        if pages is None or pages[0] != self._pages_key(dev):
             _device_of(self.page_table, "page_table")
+            if self.page_table.dim() != 2:
+                raise AdapldError(-2, f"page_table has shape {tuple(self.page_table.shape)}, expected 2 dimensions")
             B, max_pages = self.page_table.shape
-            pages = (dev, _dptr(self.page_table, "page_table", _I32, (B, max_pages), dev), B, max_pages)
+            pages = (self._pages_key(dev), _dptr(self.page_table, "page_table", _I32, (B, max_pages), dev), B, max_pages)
             object.__setattr__(self, "_pages", pages)
         return pages
 
     def _marshal_stack(self, dev):
-        """(device, pointers of free_pages and free_count, n_pages)."""
+        """(key, pointers of free_pages and free_count, n_pages)."""
         stack = self._stack
-        if stack is None or stack[0] != dev or stack[1] != (self.free_pages.data_ptr(), self.free_count.data_ptr()):
+        if stack is None or stack[0] != self._stack_key(dev):
             _device_of(self.free_pages, "free_pages")
-            n_pages = self.free_pages.shape[0]
+            n_pages = self.free_pages.numel()
             ptrs = (_dptr(self.free_pages, "free_pages", _I32, (n_pages,), dev),
                     _dptr(self.free_count, "free_count", _I32, (1,), dev))
-            stack = (dev, ptrs, n_pages)
+            stack = (self._stack_key(dev), ptrs, n_pages)
             object.__setattr__(self, "_stack", stack)
         return stack
 

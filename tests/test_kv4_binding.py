@@ -70,3 +70,72 @@ def test_allocate_refuses_other_head_dimensions():
     for D in (64, 96, 256, 0):
         with pytest.raises(adapld.AdapldError):
             adapld.Kv4Cache.allocate(4, 16, 2, 1, 2, D=D, device="cpu")
+
+
+def _calls(c):
+    """One call of each kind on a cache of two sequences and two kv heads."""
+    lens, slots, x = i32([3, 3]), i32([[0], [1]]), bf16(2, 1, 2, 128)
+    return {
+        "page_map": lambda: adapld.page_map(c, lens, lens, slot_map=slots, granted=i32([0, 0])),
+        "append": lambda: adapld.kv4_append(c, x, x, slots),
+        "gather": lambda: adapld.kv4_gather(c, slots, k_out=x, v_out=x),
+        "verify": lambda: adapld.tree_verify_attn_kv4(
+            bf16(2, 1, 4, 128), c, lens, lens, L_max=16, out=bf16(2, 1, 4, 128), lse=torch.zeros((2, 4, 1)),
+            ws=torch.zeros(16, dtype=torch.uint8))}
+
+
+POOL = ("append", "gather", "verify")
+# What may become of a buffer at its old address: another shape, fewer pages,
+# other strides, another type.
+SAME_ADDRESS = {
+    "half": lambda t: t[:t.shape[0] // 2],
+    "flat": lambda t: t.view(-1),
+    "transposed": lambda t: t.transpose(0, -1),
+    "strided": lambda t: t[::2],
+    "int8": lambda t: t.view(torch.int8)}
+
+
+@pytest.mark.parametrize("name, kinds, hows", [
+    *((name, POOL, sorted(SAME_ADDRESS)) for name in ("k_codes", "k_scales", "v_codes", "v_scales")),
+    ("page_table", ("page_map", "verify"), ("half", "flat", "transposed", "int8")),
+    ("free_pages", ("page_map",), ("strided", "int8")), ("free_count", ("page_map",), ("half", "int8"))])
+def test_buffers_reshaped_at_the_same_address(lib, name, kinds, hows):
+    """A buffer that no longer fits is refused though its address is the old
+    one, and every call goes on once it fits again."""
+    c = cache_of(B=2)
+    calls = _calls(c)
+    for kind in kinds:
+        calls[kind]()
+    t = getattr(c, name)
+    whole = t.data
+    for how in hows:
+        lib.calls.clear()
+        t.data = SAME_ADDRESS[how](whole)
+        assert t.numel() == 0 or t.data_ptr() == whole.data_ptr()
+        for kind in kinds:
+            for _ in range(2):
+                with pytest.raises(adapld.AdapldError):
+                    calls[kind]()
+        assert lib.calls == [], how
+        t.data = whole
+        for kind in kinds:
+            calls[kind]()
+        assert len(lib.calls) == len(kinds)
+
+
+def test_smaller_pool_at_the_same_address(lib):
+    """Buffers that shrink together are the smaller cache from the next call on."""
+    c = cache_of(B=2, max_pages=2)
+    calls = _calls(c)
+    for kind in POOL:
+        calls[kind]()
+    lib.calls.clear()
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        t = getattr(c, name)
+        t.data = t.data[:3]
+    c.page_table.data = c.page_table.data[:, :1].contiguous()
+    for kind in POOL:
+        calls[kind]()
+    sizes = {name: args for name, args in lib.calls}
+    assert sizes["adapld_kv4_append"][10] == 3 and sizes["adapld_kv4_gather"][10] == 3
+    assert sizes["adapld_tree_verify_attn_kv4"][18:20] == (3, 1)     # n_pages, max_pages
