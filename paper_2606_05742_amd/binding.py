@@ -489,10 +489,11 @@ class Kv4Cache:
     """The paged 4-bit K/V cache of B sequences: a pool of pages, the page
     table of each sequence and the stack of free pages (adapld_kv4_*).  The
     buffers may be the caller's own, and those that no call uses None: page_map
-    takes the table and the stack, the other calls the pool and (the attention)
-    the table.  allocate() makes an empty cache.  The buffers are checked and
-    their pointers marshalled at the first call, and again after one of the
-    fields is assigned or a buffer has another address, shape, type or layout."""
+    takes the table and the stack (of as many pages as the pool, where there is
+    one), the other calls the pool and (the attention) the table.  allocate()
+    makes an empty cache.  The buffers are checked and their pointers marshalled
+    at the first call, and again after one of the fields is assigned or a buffer
+    has another address, shape, type or layout."""
     k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
     k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
     v_codes: torch.Tensor
@@ -540,8 +541,9 @@ class Kv4Cache:
         return dev, t.data_ptr(), t.shape, t.dtype, t.is_contiguous()
 
     def _stack_key(self, dev):
-        t, n = self.free_pages, self.free_count
-        return dev, t.data_ptr(), t.shape, t.dtype, t.is_contiguous(), n.data_ptr(), n.shape, n.dtype, n.is_contiguous()
+        t, n, pool = self.free_pages, self.free_count, self.k_codes
+        return (dev, t.data_ptr(), t.shape, t.dtype, t.is_contiguous(), n.data_ptr(), n.shape, n.dtype,
+                n.is_contiguous(), None if pool is None else pool.shape)
 
     def _marshal_pool(self, dev):
         """(key, pointers of the four arrays, n_pages, Hkv, D)."""
@@ -578,6 +580,8 @@ class Kv4Cache:
         if stack is None or stack[0] != self._stack_key(dev):
             _device_of(self.free_pages, "free_pages")
             n_pages = self.free_pages.numel()
+            if self.k_codes is not None and self.n_pages != n_pages:
+                raise AdapldError(-2, f"free_pages is a stack of {n_pages} pages, the pool has {self.n_pages}")
             ptrs = (_dptr(self.free_pages, "free_pages", _I32, (n_pages,), dev),
                     _dptr(self.free_count, "free_count", _I32, (1,), dev))
             stack = (self._stack_key(dev), ptrs, n_pages)

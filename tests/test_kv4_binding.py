@@ -139,3 +139,32 @@ def test_smaller_pool_at_the_same_address(lib):
     sizes = {name: args for name, args in lib.calls}
     assert sizes["adapld_kv4_append"][10] == 3 and sizes["adapld_kv4_gather"][10] == 3
     assert sizes["adapld_tree_verify_attn_kv4"][18:20] == (3, 1)     # n_pages, max_pages
+
+
+@pytest.mark.parametrize("n", (3, 5))
+def test_page_map_refuses_a_stack_of_another_pool(lib, n):
+    """Page ids of a longer stack lie outside the pool: their rows would be
+    dropped by the append and read as another page's by the attention; a shorter
+    one takes ids of the pool for pages outside."""
+    c = cache_of(B=2)
+    call = _calls(c)["page_map"]
+    call()
+    whole = c.free_pages
+    c.free_pages = torch.zeros(n, dtype=torch.int32)
+    for _ in range(2):
+        with pytest.raises(adapld.AdapldError):
+            call()
+    c.free_pages = whole
+    call()
+    whole.data = whole.data[:3]                 # in place
+    with pytest.raises(adapld.AdapldError):
+        call()
+    for name in ("k_codes", "k_scales", "v_codes", "v_scales"):
+        setattr(c, name, getattr(c, name)[:3])
+    call()                                      # the pool of the smaller stack
+    c.k_codes.data = c.k_codes.data[:2]
+    with pytest.raises(adapld.AdapldError):
+        call()
+    c.k_codes = None                            # a stack without a pool
+    call()
+    assert [args[5] for _, args in lib.calls] == [4, 4, 3, 3]
