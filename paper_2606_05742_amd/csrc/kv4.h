@@ -30,6 +30,14 @@ __host__ __device__ inline size_t kv4_row(int page, int g, int off, int Hkv, int
   return ((((size_t)page * Hkv + g) << page_shift) + off);
 }
 
+// Blocks of the slot map's own launch for N slots of a sequence.  N may be
+// INT32_MAX, so the sum is formed in 64 bits.
+constexpr int kKv4SlotThreads = 256;
+constexpr int kKv4SlotsPerBlock = 4 * kKv4SlotThreads;
+constexpr unsigned kv4_slot_blocks(int N) {
+  return (unsigned)(((int64_t)N + kKv4SlotsPerBlock - 1) / kKv4SlotsPerBlock);
+}
+
 // A page id from a table, inside the pool whatever the table holds.
 __host__ __device__ inline int kv4_page_in_pool(int page, int n_pages) {
   return page < 0 ? 0 : page >= n_pages ? n_pages - 1 : page;

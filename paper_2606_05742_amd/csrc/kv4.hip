@@ -216,15 +216,13 @@ __global__ __launch_bounds__(kMapThreads) void page_map_kernel(const MapArgs a, 
 }
 
 // Slots of a larger batch, after the pages.
-constexpr int kSlotThreads = 256;
-constexpr int kSlotsPerThread = 4;
-__global__ __launch_bounds__(kSlotThreads) void slot_map_kernel(const MapArgs a) {
+__global__ __launch_bounds__(kKv4SlotThreads) void slot_map_kernel(const MapArgs a) {
   const int b = blockIdx.y;
   const int o = clamp_len(a.lens_old[b], a), n = clamp_len(a.lens_new[b], a);
   const bool ok = a.granted[b] != 0;
 #pragma unroll
-  for (int k = 0; k < kSlotsPerThread; ++k) {
-    const int i = (blockIdx.x * kSlotsPerThread + k) * kSlotThreads + threadIdx.x;
+  for (int k = 0; k < kKv4SlotsPerBlock / kKv4SlotThreads; ++k) {
+    const int i = blockIdx.x * kKv4SlotsPerBlock + k * kKv4SlotThreads + threadIdx.x;
     if (i < a.N) a.slot_map[(size_t)b * a.N + i] = ok && i < n - o ? slot_at(a, b, o + i) : -1;
   }
 }
@@ -377,8 +375,7 @@ hipError_t launch_kv4_page_map(const int32_t* lens_old, const int32_t* lens_new,
   hipLaunchKernelGGL(page_map_kernel, dim3(1 + others), dim3(kMapThreads), 0, stream, a, slots);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || slots != kSlotsLater) return e;
-  constexpr int kPerBlock = kSlotThreads * kSlotsPerThread;
-  hipLaunchKernelGGL(slot_map_kernel, dim3((N + kPerBlock - 1) / kPerBlock, B), dim3(kSlotThreads), 0, stream, a);
+  hipLaunchKernelGGL(slot_map_kernel, dim3(kv4_slot_blocks(N), B), dim3(kKv4SlotThreads), 0, stream, a);
   return hipGetLastError();
 }
 
