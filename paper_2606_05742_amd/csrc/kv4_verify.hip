@@ -21,6 +21,7 @@
 // of the 1.14 of a large library product: the matrix products (48 % of the cycles),
 // the exponentials and the conversions share two waves a SIMD.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "adapld_internal.h"
@@ -51,15 +52,29 @@ constexpr int kMaskWords = (ADAPLD_MAX_TREE_NODES + 63) / 64;
 constexpr int kMaxChunk = 32768;                  // context keys of one split: about 1 ms of a workgroup
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kRescaleSlack = 8.0f;             // log2 units the running max may lag
-constexpr float kWeightLimit = 16777216.0f;       // sum of one lane's weights of a step that moves the max
+
+// Weights are taken relative to a reference: a maximum of the row's logits seen
+// so far (log2 units) plus a margin.  The maximum may lag: a step that looks for it
+// moves it where it is more than kRescaleSlack behind, the others where a lane's
+// weights of the step (16 at most) sum up to more than 2^kLag times the weight of
+// the maximum.  The margin keeps a row's sum of weights below 1 even if all n of
+// its keys are at that limit (8 at least share a lane's sum), so that no sum of
+// weights times values leaves fp32's range, whatever finite values V holds, and no
+// partial output or merge does: 2^margin is at least 2^kLag * n.  Weights of less
+// than 2^(margin - 126) times the row's largest (2^-100 for 8192 keys) are zero, and
+// products of a weight and a value below 2^-126 may be.
+constexpr float kRescaleSlack = 8.0f;
+constexpr int kLag = 12;   // log2(16) + kRescaleSlack: where the second rule asks, the first moves
+inline int weight_margin(int L_max, int T_max) { return kLag + 1 + log2_pow2(std::max(L_max, T_max)); }
 
 struct Kv4Args {
   VerifyKv4Call c;
   int G, rows_max, nw, nsplit, chunk, rowgroups, page_shift;
+  int margin;          // weight_margin(L_max, T_max)
+  float weight_limit;  // 2^(kLag - margin)
   float scale_log2;
   float* ws_o;     // [B*Hkv][nsplit][rows_max][D]  partial outputs O/l
-  float2* ws_ml;   // [B*Hkv][nsplit][rows_max]     (running max in log2 units, sum)
+  float2* ws_ml;   // [B*Hkv][nsplit][rows_max]     (reference in log2 units, sum)
 };
 
 // Physical 16-byte chunk of logical chunk c in key row r is c ^ swz(r).  LDS has 64
@@ -107,7 +122,7 @@ __device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
 // one exchange with the other half of the wave, and P^T goes straight back as
 // the B operand of O^T = V^T P^T.
 struct Block {
-  float m, l;              // running max (log2 units) and this lane's share of the sum
+  float m, l;              // reference (log2 units) and this lane's share of the sum
   f32x16_t o[kD / 32];     // O^T: value r is dim 32*db + 8*(r/4) + 4*(lane/32) + r%4
 };
 
@@ -129,12 +144,10 @@ __device__ __forceinline__ void mask_keys(f32x16_t& s, int n, uint32_t bits) {
   }
 }
 
-// The softmax of 32 keys in pieces.  Logits, the running max (in log2 units), the
+// The softmax of 32 keys in pieces.  Logits, the reference (in log2 units), the
 // sum and O are fp32; the weights are rounded to bf16 once, as the operand of P V
 // (relative 2^-8, the size of the output's own rounding), and summed before that.
-// P^T comes in the order of the B operand.  The running max is any reference
-// within the exponent's range, not the true maximum: softmax_step moves it when
-// it lags by more than kRescaleSlack.
+// P^T comes in the order of the B operand.
 __device__ __forceinline__ float row_max(const f32x16_t& s) {
   float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
@@ -163,8 +176,11 @@ __device__ __forceinline__ void exp_part(const f32x16_t& s, int s2, float sl2, f
     pb[i + 1] = pk[1];
   }
 }
-__device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, Block& x, bf16x8_t (&pb)[2]) {
-  const float mt = row_max(s) * sl2;   // scale > 0, so the max commutes with scaling
+// The reference that a step's own maximum gives (scale > 0, so the max commutes
+// with scaling).
+__device__ __forceinline__ float reference_of(float mx, float sl2, float margin) { return fmaf(mx, sl2, margin); }
+__device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, float margin, Block& x, bf16x8_t (&pb)[2]) {
+  const float mt = reference_of(row_max(s), sl2, margin);
   if (__ballot(mt > x.m + kRescaleSlack)) rescale_to(x, mt);
   const float m_use = x.m == -INFINITY ? 0.f : x.m;
   float psum = 0.f;
@@ -173,9 +189,15 @@ __device__ __forceinline__ void softmax_step(const f32x16_t& s, float sl2, Block
   x.l += psum;
 }
 
+// Natural logarithm of the sum of exponentials that a reference and a sum of
+// weights (> 0) stand for.
+__device__ __forceinline__ float lse_of(const Kv4Args& a, float m, float l) {
+  return (m - (float)a.margin + log2f(ldexpf(l, a.margin))) * kLn2;
+}
+
 // Four dimensions (chunk ch of 32) of a finished row: to the output, or to the
-// partial outputs of a split context.  v is the unnormalised output, ml its max
-// and sum; 32 lanes store a row.
+// partial outputs of a split context.  v is the unnormalised output, ml its
+// reference and sum; 32 lanes store a row.
 __device__ __forceinline__ void store_row(const Kv4Args& a, int b, int g, int split, int qr, int ch, float2 ml,
                                           float4 v) {
   const VerifyKv4Call& c = a.c;
@@ -188,7 +210,7 @@ __device__ __forceinline__ void store_row(const Kv4Args& a, int b, int g, int sp
     pk.y = f32_to_bf16_bits(v.z) | (f32_to_bf16_bits(v.w) << 16);
     *reinterpret_cast<uint2*>(c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + 4 * ch) = pk;
     if (ch == 0 && c.lse)
-      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = ml.y > 0.f ? (ml.x + log2f(ml.y)) * kLn2 : -INFINITY;
+      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = ml.y > 0.f ? lse_of(a, ml.x, ml.y) : -INFINITY;
   } else {
     const size_t at = (((size_t)b * c.Hkv + g) * a.nsplit + split) * a.rows_max + qr;
     *reinterpret_cast<float4*>(a.ws_o + at * kD + 4 * ch) = v;
@@ -389,7 +411,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
 
   Block x;
   block_init(x);
-  const float sl2 = a.scale_log2;
+  const float sl2 = a.scale_log2, margin = (float)a.margin;
 
   // The wave's half h lies in tile h / HP; with KH = 1 it covers keys
   // [32*(h&1), +32) of that tile, with KH = 2 the wave's own half.  hs is h,
@@ -462,7 +484,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
     advance_any(0);
     if (HP == 1 && H > 1) tile_barrier();   // half 1 is in tile 1
     qk(1, s_nxt);
-    softmax_step(s_cur, sl2, x, pb);
+    softmax_step(s_cur, sl2, margin, x, pb);
     s_cur = s_nxt;
     // Half h: its softmax runs beside the products of P V of half h - 1 and of
     // S of half h + 1.  (Past the last half qk reads a stale stage; unused.)
@@ -472,7 +494,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
       if (masked) mask(h, s_cur);
       if (h % HP == HP - 1 && h + 1 < H) tile_barrier();
       qk(h + 1, s_nxt);
-      softmax_step(s_cur, sl2, x, pb);
+      softmax_step(s_cur, sl2, margin, x, pb);
       s_cur = s_nxt;
     };
     auto body_c = [&](auto J, int h) {
@@ -482,11 +504,11 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
         if constexpr ((j / HP) & 1) advance_plain(h / HP, even);
         else advance_plain(h / HP, odd);
       }
-      // The exponentials use the running max as it stands, eight products on
+      // The exponentials use the reference as it stands, eight products on
       // either side of the tile barrier beside half of them each.  A weight's
       // scale costs no accuracy, so the max is not even looked for unless a lane's
-      // weights of the half sum up to kWeightLimit: then the half is done again
-      // with the max moved.
+      // weights of the half pass the limit: then the half is done again with the
+      // reference moved.
       float psum = 0.f;
       bf16x8_t pn[2];
       exp_part(s_cur, 0, sl2, x.m, pn[0], psum);
@@ -497,8 +519,8 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
       qk((j + 1) % kPeriod, s_nxt);
       exp_part(s_cur, 1, sl2, x.m, pn[1], psum);
       asm volatile("" ::"v"(pn[1]), "v"(psum));
-      if (__ballot(psum > kWeightLimit)) {
-        rescale_to(x, row_max(s_cur) * sl2);
+      if (__ballot(psum > a.weight_limit)) {
+        rescale_to(x, reference_of(row_max(s_cur), sl2, margin));
         psum = 0.f;
         exp_part(s_cur, 0, sl2, x.m, pn[0], psum);
         exp_part(s_cur, 1, sl2, x.m, pn[1], psum);
@@ -537,7 +559,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
   float l_tot = x.l + __shfl_xor(x.l, 32, kWave);
   if constexpr (KH == 2) {
     // The wave with the other half of the keys hands its state over; each
-    // state is relative to its own running max, the merged one to M.
+    // state is relative to its own reference, the merged one to M.
     float4* xo = reinterpret_cast<float4*>(smem);                        // [R][16][64]
     float2* xml = reinterpret_cast<float2*>(s_mask);                     // [R][64]
     static_assert(R * 16 * 64 * 16 <= 2 * kVRegion && R * 64 <= ADAPLD_MAX_TREE_NODES * kMaskWords,
@@ -585,7 +607,7 @@ __global__ __launch_bounds__(kThreads, 1) void kv4_verify_kernel(const Kv4Args a
         *reinterpret_cast<uint2*>(op + db * 32 + 8 * r4 + 4 * half) = pk;
       }
     if (half == 0 && c.lse)
-      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l_tot > 0.f ? (x.m + log2f(l_tot)) * kLn2 : -INFINITY;
+      c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = l_tot > 0.f ? lse_of(a, x.m, l_tot) : -INFINITY;
   } else {
     const size_t at = ((size_t)bg * a.nsplit + split) * a.rows_max + qr;
     float* wp = a.ws_o + at * kD;
@@ -681,7 +703,7 @@ struct Rows16 {
         s.v[i][r] = key < n && (!TREE || ((bits >> key) & 1u)) ? s.v[i][r] : -INFINITY;
       }
   }
-  __device__ __forceinline__ void move_max(const Logits& s, float sl2) {
+  __device__ __forceinline__ void move_reference(const Logits& s, float sl2, float margin) {
     float mx = fmaxf(fmaxf(s.v[0][0], s.v[0][1]), s.v[0][2]);
     mx = fmaxf(fmaxf(mx, s.v[0][3]), s.v[1][0]);
     mx = fmaxf(fmaxf(mx, s.v[1][1]), s.v[1][2]);
@@ -690,7 +712,7 @@ struct Rows16 {
     mx = fmaxf(__int_as_float(w32[0]), __int_as_float(w32[1]));
     const auto w16 = __builtin_amdgcn_permlane16_swap(__float_as_int(mx), __float_as_int(mx), false, false);
     mx = fmaxf(__int_as_float(w16[0]), __int_as_float(w16[1]));
-    const float mt = mx * sl2;   // scale > 0, so the max commutes with scaling
+    const float mt = reference_of(mx, sl2, margin);
     if (__ballot(mt > m + kRescaleSlack)) {
       const float m_new = fmaxf(m, mt);
       const float alpha = m_new == m ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -726,7 +748,7 @@ struct Rows16 {
       o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_fragment(v, vofs[db], vofs[db] + 16 * kRowBytes), p, o[db], 0,
                                                       0, 0);
   }
-  __device__ __forceinline__ float running_max() const { return m; }
+  __device__ __forceinline__ float reference() const { return m; }
   __device__ __forceinline__ float total() const {
     const float t = l + __shfl_xor(l, 32, kWave);
     return t + __shfl_xor(t, 16, kWave);
@@ -801,8 +823,8 @@ struct Rows32 {
   static __device__ __forceinline__ void mask(Logits& s, int n, uint32_t bits) {
     mask_keys<TREE>(s.v, n, bits);
   }
-  __device__ __forceinline__ void move_max(const Logits& s, float sl2) {
-    const float mt = row_max(s.v) * sl2;
+  __device__ __forceinline__ void move_reference(const Logits& s, float sl2, float margin) {
+    const float mt = reference_of(row_max(s.v), sl2, margin);
     if (__ballot(mt > x.m + kRescaleSlack)) rescale_to(x, mt);
   }
   static __device__ __forceinline__ float weights(const Logits& s, float sl2, float m_use, Weights& p) {
@@ -839,7 +861,7 @@ struct Rows32 {
       __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
     }
   }
-  __device__ __forceinline__ float running_max() const { return x.m; }
+  __device__ __forceinline__ float reference() const { return x.m; }
   __device__ __forceinline__ float total() const { return x.l + __shfl_xor(x.l, 32, kWave); }
   template <class F>
   __device__ __forceinline__ void chunks(F&& f) const {
@@ -900,7 +922,7 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
   const int n_ctx = c1 > c0 ? (c1 - c0 + kStep - 1) / kStep : 0;
 
   x.init();
-  const float sl2 = a.scale_log2;
+  const float sl2 = a.scale_log2, margin = (float)a.margin;
   uint8_t* const vrows = smem + wave * 2 * kVBuffer;
   int vpos[4];
 #pragma unroll
@@ -1001,8 +1023,8 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
         for (int j = 0; j < 4; ++j) *reinterpret_cast<u32x4_t*>(vrows + 16 * i * kRowBytes + vpos[j]) = tv[i][j];
       x.products_s([&](int i, int j) { return __builtin_bit_cast(bf16x8_t, tk[i][j]); }, s_cur);
       ROWS::template mask<true>(s_cur, T - tree0, (uint32_t)(sees >> tree0));
-      x.move_max(s_cur, sl2);
-      const float m = x.running_max();
+      x.move_reference(s_cur, sl2, margin);
+      const float m = x.reference();
       x.add(ROWS::weights(s_cur, sl2, m == -INFINITY ? 0.f : m, p));
       typename ROWS::VAhead f;
       x.read_v((const lds_u8*)vrows, f);
@@ -1010,17 +1032,17 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
     }
     if (s < n_ctx) {
       begin_ctx(r[0], 0, s_cur);
-      x.move_max(s_cur, sl2);   // a first max (keys behind the last repeat it)
+      x.move_reference(s_cur, sl2, margin);   // a first max (keys behind the last repeat it)
     }
     auto ctx_pair = [&](int at, Raw& rn, int buf) {   // step `at` beside the start of the next, both of the context
       const lds_u8* const v = (const lds_u8*)vrows + buf * kVBuffer;
       typename ROWS::VAhead f;
       x.read_v(v, f);
       // as in the tile kernel, the max is looked for when the weights grow
-      float psum = ROWS::weights(s_cur, sl2, x.running_max(), p);
-      if (__ballot(psum > kWeightLimit)) {
-        x.move_max(s_cur, sl2);
-        psum = ROWS::weights(s_cur, sl2, x.running_max(), p);
+      float psum = ROWS::weights(s_cur, sl2, x.reference(), p);
+      if (__ballot(psum > a.weight_limit)) {
+        x.move_reference(s_cur, sl2, margin);
+        psum = ROWS::weights(s_cur, sl2, x.reference(), p);
       }
       x.add(psum);
       x.products_o(v, f, p);
@@ -1043,8 +1065,8 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
     }
     for (int buf = 0; s < n_ctx; s += kSlices, buf ^= 1) {   // at most two steps
       if (c1 - c0 - s * kStep < kStep) ROWS::template mask<false>(s_cur, c1 - c0 - s * kStep, 0u);
-      x.move_max(s_cur, sl2);
-      x.add(ROWS::weights(s_cur, sl2, x.running_max(), p));
+      x.move_reference(s_cur, sl2, margin);
+      x.add(ROWS::weights(s_cur, sl2, x.reference(), p));
       typename ROWS::VAhead f;
       x.read_v((const lds_u8*)vrows + buf * kVBuffer, f);
       x.products_o((const lds_u8*)vrows + buf * kVBuffer, f, p);
@@ -1061,7 +1083,7 @@ __global__ __launch_bounds__(kThreads) void kv4_narrow_kernel(const Kv4Args a) {
   {
     const float l = x.total();
     const int r = ROWS::row();
-    if (ROWS::first_of_row()) s_ml[wave][r] = make_float2(x.running_max(), l);
+    if (ROWS::first_of_row()) s_ml[wave][r] = make_float2(x.reference(), l);
     x.chunks([&](int ch, f32x4_t v) {
       xo[(wave * kMergeRows + r) * 32 + (ch ^ (r & 15))] = make_float4(v[0], v[1], v[2], v[3]);
     });
@@ -1149,7 +1171,7 @@ __global__ __launch_bounds__(kCombineThreads) void kv4_combine_kernel(const Kv4A
   pk.y = f32_to_bf16_bits(num.z * inv) | (f32_to_bf16_bits(num.w * inv) << 16);
   *reinterpret_cast<uint2*>(c.out + (((size_t)b * c.T_max + u) * c.Hq + h) * kD + dim) = pk;
   if (dim == 0 && c.lse)
-    c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = den > 0.f ? (M + log2f(den)) * kLn2 : -INFINITY;
+    c.lse[((size_t)b * c.Hq + h) * c.T_max + u] = den > 0.f ? lse_of(a, M, den) : -INFINITY;
 }
 
 }  // namespace
@@ -1231,6 +1253,8 @@ hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Pl
   a.c = c;
   a.G = c.Hq / c.Hkv; a.rows_max = p.rows_max; a.nw = (c.T_max + 63) / 64;
   a.nsplit = p.nsplit; a.chunk = p.chunk; a.rowgroups = p.rowgroups; a.page_shift = log2_pow2(c.page_size);
+  a.margin = weight_margin(c.L_max, c.T_max);
+  a.weight_limit = std::ldexp(1.f, kLag - a.margin);
   a.scale_log2 = c.scale * kLog2e;
   const size_t slots = (size_t)c.B * c.Hkv * p.nsplit * p.rows_max;
   a.ws_o = static_cast<float*>(c.ws);
