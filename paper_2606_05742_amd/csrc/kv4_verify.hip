@@ -49,7 +49,7 @@ constexpr int kVRegion = kStages * kTileBytes;    // the V tiles behind the K ti
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kMaskWords = (ADAPLD_MAX_TREE_NODES + 63) / 64;
-constexpr int kMaxChunk = 32768;                  // context keys of one split: about 1 ms of a workgroup
+constexpr int kMaxChunk = 32768;                  // keys of one split, less the tree's: about 1 ms of a workgroup
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -1182,13 +1182,16 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
   // for the 256-row shape depends on whether some SIMD has two row blocks; a
   // call takes its rounds of workgroups over the 256 CUs at their mean time, at
   // least the longest one's; a split context also the second launch and the
-  // partials' traffic.  Constants in us, fitted to calls like these (us at the
-  // choice / at the next best): 16 x 8192 keys, 32 heads over 8, 52 nodes 256
-  // rows in 2 splits 144 / 128 rows unsplit 153; 8 x 32768, 64 over 8, 72 nodes
-  // 256 rows in 4 636 / 128 in 4 681; 4 x 2048, 40 over 8, 136 nodes 128 unsplit
-  // 49 / 256 in 2 61; 1 x 4096, 32 over 8, 44 nodes 128 in 13 21.6 / in 16 21.9;
-  // single tokens, 4 x 30000, 64 over 8 in 8 34 / in 6 37; 8 x 2048, 32 over 8 in
-  // 4 12.9 / in 2 13.6.
+  // partials' traffic.  The constants (us) were fitted before the kernels' last
+  // steps and read up to 36 % high; what counts is the order of the candidates,
+  // which holds.  us a call inside a graph over three sets of inputs, at the choice
+  // / at others: 16 x 8192 keys, 32 heads over 8, 52 nodes 256 rows in 2 splits 133
+  // to 138 / 128 rows unsplit 141, in 2 154; 8 x 32768, 64 over 8, 72 nodes 256 rows
+  // in 4 616 / 128 in 4 675; 4 x 2048, 40 over 8, 136 nodes 128 unsplit 46 / 256 in 2
+  // 48; 1 x 4096, 32 over 8, 44 nodes 128 in 13 20.8 / in 16 20.8, in 11 20.2; 24 x
+  // 6007 at most, 28 over 4, 35 nodes 256 in 2 89 / in 3 96, 128 unsplit 98; single
+  // tokens, 4 x 30000, 64 over 8 in 8 29 / in 6 32; 8 x 2048, 32 over 8 in 4 11.2 /
+  // in 2 12.0.
   constexpr int kCUs = 256;
   constexpr double kCombine = 5.0, kPartialBytesPerUs = 6e6;
   struct Shape {
@@ -1198,9 +1201,9 @@ VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
     double start, per_unit, per_unit_half;   // the latter where at most half the rows live
   };
   // Up to 64 rows the narrow shape that just holds them, us at it / at the next
-  // larger one: single tokens 32 x 8192 55 / 61, 1 x 4096 11.1 / 11.5 (4 rows); 32
-  // rows, 16 x 4096 27.5 / 37.5; 64 rows, 32 x 4096 60.8 / 76.7, 4 x 4096 20.1 / 22.2
-  // (through a graph that keeps the card at its power limit).
+  // larger one (as above): single tokens 32 x 8192 47 to 49 / 53, 1 x 4096 9.7 /
+  // 10.5 (4 rows); 32 rows, 16 x 4096 24.2 / 30.5; 64 rows, 32 x 4096 56 / 76, 4 x
+  // 4096 19.1 / 21.1.
   const Shape shapes[] = {{16, true, kWaves * kStep, 5.5, 1.3, 1.3},
                           {32, true, kWaves * kStep, 5.5, 2.0, 2.0},
                           {64, true, kWaves / 2 * kStep, 5.5, 1.7, 1.7},
