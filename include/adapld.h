@@ -566,7 +566,8 @@ int adapld_accept_greedy(const int32_t* node_token, const int32_t* node_parent,
  *   2. A sequence that needs more gets them from the top of the stack, in
  *      order of b, then of page index, and they are written to its table
  *      row.  Sequence b is served if the pages asked for by sequences 0..b
- *      fit the stack; if not it gets none, and granted[b] = 0.
+ *      fit the stack; if not it gets none, and granted[b] = 0: it still has
+ *      lens_old[b] tokens for the calls that follow.
  *   3. slot_map[b, i], i < N, is the slot of position lens_old[b] + i where
  *      that is below lens_new[b], granted[b] is 1 and the table entry is a
  *      page of the pool; otherwise -1.

@@ -17,7 +17,7 @@
 // 32 sequences x 8192 keys, 32 heads over 8: 46, 6.2 TB/s, HBM bound (a copy
 // moves 4.8, the fastest reads here 6.0 to 6.5); chains of 16 nodes, 32 x 4096: 53,
 // two row blocks convert the same codes; 16 x 8192, 52 nodes: 126 to 137 by the box,
-// 0.82 to 0.89 PFLOP/s, and 8 x 32768, 64 over 8, 72 nodes: 613 to 658, 0.94 to 1.01,
+// 0.82 to 0.89 PFLOP/s, and 8 x 32768, 64 over 8, 72 nodes: 611 to 658, 0.94 to 1.01,
 // of the 1.14 of a large library product: the matrix products (48 % of the cycles),
 // the exponentials and the conversions share two waves a SIMD.
 #include <algorithm>
