@@ -665,17 +665,17 @@ int adapld_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, const uin
  * A sequence's results depend on its own inputs and the sizes alone, not on
  * its batch-mates, page ids or page size.
  * q, the cache's values and the tree's K/V must be finite and so must, in fp32,
- * scale * q.k * log2(e); scale must be finite and > 0.  Values of any finite size
- * give finite sums (adapld_kv4_append stores infinities as 6 * 2^125, which takes
- * part like any other value).  Logits, sums and partial outputs are fp32; a
- * key's weight is rounded to bf16 once, as the operand of the product with V.
- * A weight counts as zero below 2^-100 of the row's largest for up to 8192 keys
- * and twice that for every doubling of L_max (2^-83 at 2^30), and a product of
- * weight and value below 2^-126 may.
+ * scale * q.k * log2(e); scale must be > 0 and scale * log2(e) finite.  Values
+ * of any finite size give finite sums (adapld_kv4_append stores infinities as 6 *
+ * 2^125, which takes part like any other value).  Logits, sums and partial
+ * outputs are fp32; a key's weight is rounded to bf16 once, as the operand of the
+ * product with V.  A weight counts as zero below 2^-100 of the row's largest for up
+ * to 8192 keys and twice that for every doubling of L_max (2^-83 at 2^30), and a
+ * product of weight and value below 2^-126 may.
  *
  * Errors: NULL_ARG (also for some but not all of k_tree, v_tree, tree_mask);
  * INVALID_ARG for Hq % Hkv != 0, non-positive sizes, L_max > max_pages *
- * page_size, a page_size other than the five, scale not finite and > 0, or
+ * page_size, a page_size other than the five, scale not > 0 or too large, or
  * misaligned pointers; UNSUPPORTED for D != 128, T_max >
  * ADAPLD_MAX_TREE_NODES, n_pages * page_size or max_pages * page_size >
  * INT32_MAX, L_max > 2^30, B * T_max * Hq > 2^27 - 8, or more workgroups than one

@@ -531,8 +531,8 @@ int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const
   const int n_tree = (k_tree != nullptr) + (v_tree != nullptr) + (tree_mask != nullptr);
   if (n_tree != 0 && n_tree != 3) return ADAPLD_ERR_NULL_ARG;
   if (const int st = check_kv4_arrays(k_codes, k_scales, v_codes, v_scales); st != ADAPLD_OK) return st;
-  if (L_max < 1 || T_max < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || !std::isfinite(scale) ||
-      !(scale > 0.f))
+  if (L_max < 1 || T_max < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || !(scale > 0.f) ||
+      !std::isfinite(scale * 1.4426950408889634f))   // the kernels take logits in units of log2
     return ADAPLD_ERR_INVALID_ARG;
   if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
   if (D != ADAPLD_HEAD_DIM || T_max > ADAPLD_MAX_TREE_NODES || (int64_t)max_pages * page_size > INT32_MAX ||

@@ -134,6 +134,12 @@ def test_verify_refusals(lib):
     assert f(*_args(VERIFY, ws=ODD, **big)) == INVALID
 
 
+def test_scale_refusals(lib):
+    """A finite scale that no longer fits fp32 in units of log2."""
+    for scale in (3.4e38, 2.4e38):
+        assert lib.adapld_tree_verify_attn_kv4(*_args(VERIFY, scale=scale)) == INVALID
+
+
 def test_workspace_sizes(lib):
     ws = lib.adapld_workspace_bytes
     for bad in (dict(T_max=0), dict(T_max=257), dict(Hq=7), dict(Hkv=0), dict(B=0), dict(L=0), dict(L=(1 << 30) + 1)):
