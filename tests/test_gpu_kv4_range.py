@@ -19,7 +19,7 @@ import torch
 
 import oracle
 import paper_2606_05742_amd as adapld
-from test_gpu_kv4 import f64, i32
+from test_gpu_kv4 import Case, f64, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +103,12 @@ def test_stored_infinities():
         assert ((out[..., 0::2].double() / (6 * 2.0 ** 125) - 1).abs() <= 2.0 ** -7).all()
         assert ((out[..., 1::2].double() / (-6 * 2.0 ** 125) - 1).abs() <= 2.0 ** -7).all()
         assert (lse.double() - math.log(L)).abs().max() <= 2.0 ** -20 * math.log(L)
+
+
+@pytest.mark.parametrize("scale", (1e-42, 1e-30))
+@pytest.mark.parametrize("T", (1, 7, 40))
+def test_smallest_scales(T, scale):
+    """Logits near 0, one of the scales subnormal: masked keys stay out."""
+    c = Case([333, 41], 8, 2, T, [T, T], 16, 400, 137, tree="random")
+    out, lse = c.run(scale=scale)
+    c.check(out, lse, scale=scale)
