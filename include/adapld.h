@@ -692,4 +692,6 @@ int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const
 }
 #endif
 
+#include "adapld_kv8.h"   /* the paged 8-bit cache and the operators around it */
+
 #endif /* ADAPLD_H */

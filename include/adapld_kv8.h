@@ -1,0 +1,98 @@
+/*
+ * adapld_kv8.h -- the paged 8-bit K/V cache of libadapld and the operators
+ * around it: the norm and rotation of the queries and keys that enter it, its
+ * rows, the verify attention over it (Sec. 3.6), the weight its tokens gather
+ * and the eviction of those with the least.  Included by adapld.h, whose
+ * conventions hold.
+ */
+#ifndef ADAPLD_KV8_H
+#define ADAPLD_KV8_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include <hip/hip_runtime_api.h>
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Operation id for adapld_workspace_bytes. */
+#define ADAPLD_OP_TREE_VERIFY_ATTN_KV8 10
+
+/*
+ * Paged 8-bit K/V cache -- the context's K/V of the verify attention in pages
+ * of a pool, at 256 bytes and an eighth per token and kv head.
+ *
+ * A row is one token of one kv head, for K and for V: 128 codes of 8 bits
+ * (E4M3: sign, 4 bits of exponent with bias 7, 3 of fraction; no infinities,
+ * 0x7f and 0xff are NaN).  The ADAPLD_KV8_BLOCK tokens of an aligned block of a
+ * page share one scale byte e for each kv head, K and V apart; a value is E4M3 *
+ * 2^(e - 127), exact in bf16.  e is 10..246 (adapld_kv8_append writes no other
+ * byte; a block with another one reads as unspecified values).
+ *
+ *   k_codes, v_codes    uint8 [n_pages, Hkv, page_size, D], 16-byte aligned
+ *   k_scales, v_scales  uint8 [n_pages, Hkv, page_size / ADAPLD_KV8_BLOCK]
+ *   page_table          int32 [B, max_pages]: page i of sequence b holds its
+ *                       positions [i * page_size, (i + 1) * page_size)
+ *   page_size           16, 32, 64, 128 or 256 tokens
+ * Pages, their stack and adapld_kv4_page_map are those of the 4-bit cache.
+ */
+#define ADAPLD_KV8_BLOCK 16
+
+/*
+ * adapld_kv8_append -- quantises new tokens' rows of K/V into the cache.
+ *
+ * Sequence b goes from lens_old[b] to lens_new[b] tokens (each clamped on the
+ * device to [0, max_pages * page_size]; at most N are added, none if lens_new is
+ * not larger).  Position lens_old[b] + i gets the Hkv rows k_new[b, r], v_new[b, r],
+ * r = rows[b, i] (i itself if `rows` is NULL); for an r outside [0, n_src) zeros.
+ *
+ * For each block that gets rows, kv head, and K and V apart: amax is the largest
+ * finite magnitude of the new rows; the least e in 10..246 with amax <= 448 *
+ * 2^(e - 127) is needed.  A block whose first position is at or behind
+ * lens_old[b] takes that e.  One that held tokens keeps its own or, if that is
+ * less, takes the needed one, and its older rows are rounded again to the new
+ * scale: exactly, but for values below 2^-6 of it.  Values are rounded once, to
+ * the nearest E4M3 with ties to even; infinities and finite values above 448 *
+ * 2^119 are stored as the largest value, a NaN as 0x7f, and neither changes
+ * another value.
+ * A block that gets rows belongs to one sequence: its page is in the table of no
+ * other sequence of the call.  A block of a page id outside the pool is skipped.
+ * Rows at or behind the new length are left as they are.
+ *
+ *   k_new, v_new  bf16 [B, n_src, Hkv, D]   the layout of k_tree, v_tree
+ *   rows          int32 [B, N] or NULL      e.g. accept_nodes (NULL: N <= n_src)
+ *   lens_old, lens_new  int32 [B]
+ *
+ * Errors: NULL_ARG; INVALID_ARG for B < 0, n_src, N, Hkv, n_pages, max_pages < 1,
+ * a page_size other than the five, N > n_src without rows or misaligned pointers;
+ * UNSUPPORTED for D != 128, n_pages * page_size or max_pages * page_size >
+ * INT32_MAX, or more than 2^26 blocks of a kv head.
+ */
+int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* lens_old,
+                      const int32_t* lens_new, const int32_t* page_table, int B, int n_src, int N, int Hkv, int D,
+                      int page_size, int n_pages, int max_pages, uint8_t* k_codes, uint8_t* k_scales,
+                      uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream);
+
+/*
+ * adapld_tree_verify_attn_kv8 -- adapld_tree_verify_attn with the context's K/V in
+ * the paged 8-bit cache.
+ *
+ * Everything is as in adapld_tree_verify_attn_kv4 (arguments, single tokens without
+ * a tree, rows without any key, which entries and rows may hold anything, what has
+ * to be finite, how weights are rounded, limits and errors), but for the cache's
+ * format; the workspace is that of ADAPLD_OP_TREE_VERIFY_ATTN_KV8.
+ */
+int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,
+                                const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* page_table,
+                                const uint16_t* k_tree, const uint16_t* v_tree, const int32_t* lens,
+                                const int32_t* node_count, const uint64_t* tree_mask, int B, int L_max, int T_max,
+                                int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, float scale,
+                                uint16_t* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* ADAPLD_KV8_H */

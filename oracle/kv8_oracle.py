@@ -1,0 +1,87 @@
+"""CPU reference of the paged 8-bit K/V cache and the operators around it, in
+float64 and plain Python.
+
+Rows are quantised by looking up the nearest E4M3 value in its table, blocks and
+evicted tokens are taken one at a time; nothing here shares code with the HIP path.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+
+BLOCK = 16
+MIN_EXP, MAX_EXP = 10, 246
+# magnitude of codes 0..126 (127 is NaN): 4 bits of exponent with bias 7, 3 of fraction
+E4M3 = np.array([(c & 7) * 2.0 ** -9 if c < 8 else (8 + (c & 7)) * 2.0 ** ((c >> 3) - 10) for c in range(127)])
+
+
+def kv8_codes(x, e):
+    """Codes of float64 x at exponent byte e: nearest, ties to the even code,
+    magnitudes above the largest as the largest, NaN as 0x7f."""
+    x = np.asarray(x, np.float64)
+    y = np.abs(x) / 2.0 ** (e - 127.0)
+    y = np.where(np.isnan(y), 0.0, np.minimum(y, E4M3[-1]))
+    hi = np.minimum(np.searchsorted(E4M3, y), 126)
+    lo = np.maximum(hi - 1, 0)
+    up, down = E4M3[hi] - y, y - E4M3[lo]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)), hi, lo).astype(np.uint8)
+    return np.where(np.isnan(x), 127, code | (np.signbit(x).astype(np.uint8) << 7)).astype(np.uint8)
+
+
+def kv8_values(codes, e):
+    """float64 values of codes at exponent byte(s) e (broadcast)."""
+    c = np.asarray(codes)
+    m = np.where((c & 127) == 127, np.nan, E4M3[np.minimum(c & 127, 126)])
+    return np.where(c & 128, -m, m) * 2.0 ** (np.asarray(e, np.float64) - 127.0)
+
+
+def kv8_exponent(x):
+    """The least e in 10..246 of which 448 * 2^(e - 127) holds every finite |x|."""
+    x = np.abs(np.asarray(x, np.float64))
+    x = x[np.isfinite(x)]
+    amax = x.max() if x.size else 0.0
+    e = MIN_EXP
+    while e < MAX_EXP and 448.0 * 2.0 ** (e - 127) < amax:
+        e += 1
+    return e
+
+
+def kv8_append(k, v, lens_old, lens_new, table, page, cache, rows=None, N=None):
+    """Stores rows of k, v (float64 [B, n_src, Hkv, D]) into `cache`, the arrays
+    (k_codes, k_scales, v_codes, v_scales), in place."""
+    B, n_src, Hkv, D = k.shape
+    N = (n_src if rows is None else len(rows[0])) if N is None else N
+    n_pages, cap = cache[0].shape[0], len(table[0]) * page
+    for b in range(B):
+        old = min(max(int(lens_old[b]), 0), cap)
+        new = min(min(max(int(lens_new[b]), 0), cap), old + N)
+        if new <= old:
+            continue
+        for start in range(old // BLOCK * BLOCK, new, BLOCK):
+            p, off = int(table[b][start // page]), start % page
+            if not 0 <= p < n_pages:
+                continue
+            fresh = range(max(start, old), min(start + BLOCK, new))
+            src = [i - old if rows is None else int(rows[b][i - old]) for i in fresh]
+            for x, codes, scales in ((k, cache[0], cache[1]), (v, cache[2], cache[3])):
+                got = np.stack([x[b, r] if 0 <= r < n_src else np.zeros((Hkv, D)) for r in src])
+                for g in range(Hkv):
+                    e, before, kept = kv8_exponent(got[:, g]), int(scales[p, g, off // BLOCK]), max(old - start, 0)
+                    if kept:
+                        e = max(e, before)
+                        if e != before:
+                            codes[p, g, off:off + kept] = kv8_codes(kv8_values(codes[p, g, off:off + kept], before), e)
+                    at = off + fresh[0] - start
+                    codes[p, g, at:at + len(src)] = kv8_codes(got[:, g], e)
+                    scales[p, g, off // BLOCK] = e
+    return cache
+
+
+def kv8_rows(codes, scales, table, page, L):
+    """float64 [Hkv, L, D]: the values of positions 0..L-1 of a table row."""
+    out = np.zeros((codes.shape[1], L, codes.shape[3]))
+    for j in range(L):
+        p, off = int(table[j // page]), j % page
+        out[:, j] = kv8_values(codes[p, :, off], scales[p, :, off // BLOCK][:, None])
+    return out

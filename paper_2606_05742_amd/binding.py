@@ -23,9 +23,11 @@ OP_SEMANTIC_TOPK_EMBED = 5
 OP_BUILD_DRAFT_TREE_PAPER = 6
 OP_STEP = 7
 OP_TREE_VERIFY_ATTN_KV4 = 8
+OP_TREE_VERIFY_ATTN_KV8 = 10
 SUCC_EVERY_BRANCH, SUCC_SEMANTIC_ONLY = 0, 1
 HEAD_DIM = 128
 KV4_GROUP = 32   # dimensions that share a scale of the 4-bit cache
+KV8_BLOCK = 16   # tokens that share a scale of the 8-bit cache
 
 # ADAPLD_LIB names another build of the library (the sanitized host test
 # build); by default the in-tree libadapld.so.
@@ -93,6 +95,9 @@ SIGNATURES = {
     "adapld_kv4_append": (ctypes.c_int, [ctypes.c_void_p] * 4 + [ctypes.c_int] * 7 + [ctypes.c_void_p] * 5),
     "adapld_kv4_gather": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int] * 6 + [ctypes.c_void_p] * 3),
     "adapld_tree_verify_attn_kv4": (ctypes.c_int, [ctypes.c_void_p] * 11 + [ctypes.c_int] * 9 + [ctypes.c_float]
+                                    + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
+    "adapld_kv8_append": (ctypes.c_int, [ctypes.c_void_p] * 6 + [ctypes.c_int] * 8 + [ctypes.c_void_p] * 5),
+    "adapld_tree_verify_attn_kv8": (ctypes.c_int, [ctypes.c_void_p] * 11 + [ctypes.c_int] * 9 + [ctypes.c_float]
                                     + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
 }
 
@@ -168,7 +173,7 @@ _raw_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_d
 
 
 def _dptr(t, name, dtypes, shape, dev, nullable=False):
-    """_ptr for the calls on the 4-bit cache, which launch on the current
+    """_ptr for the calls on a paged cache, which launch on the current
     device `dev`: the tensor must live there.  One that passes every check
     takes one line of attribute reads."""
     if (type(t) is _Tensor and t.get_device() == dev and t.dtype in dtypes and (shape is None or t.shape == shape)
@@ -186,7 +191,7 @@ def _stream_on(stream, dev):
 
 
 def _on(stream, dev):
-    """Where a call on the 4-bit cache makes its buffers: on the stream that it
+    """Where a call on a paged cache makes its buffers: on the stream that it
     launches on, so that the allocator hands a freed one out again in that
     stream's order, and a new one's fill comes before the kernel."""
     if stream is None:
@@ -484,41 +489,16 @@ class NgramIndex:
         return outs
 
 
-@dataclass
-class Kv4Cache:
-    """The paged 4-bit K/V cache of B sequences: a pool of pages, the page
-    table of each sequence and the stack of free pages (adapld_kv4_*).  The
-    buffers may be the caller's own, and those that no call uses None: page_map
-    takes the table and the stack (of as many pages as the pool, where there is
-    one), the other calls the pool and (the attention) the table.  allocate()
-    makes an empty cache.  The buffers are checked and their pointers marshalled
+class _PagedCache:
+    """What the paged caches share: the checks of their buffers, which are made
     at the first call, and again after one of the fields is assigned or a buffer
     has another address, shape, type or layout."""
-    k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
-    k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
-    v_codes: torch.Tensor
-    v_scales: torch.Tensor
-    page_table: torch.Tensor    # int32 [B, max_pages]
-    free_pages: torch.Tensor    # int32 [n_pages], the stack
-    free_count: torch.Tensor    # int32 [1]
-    page_size: int
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_pool", None)
         object.__setattr__(self, "_pages", None)
         object.__setattr__(self, "_stack", None)
-
-    @staticmethod
-    def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
-        if D != HEAD_DIM:
-            raise AdapldError(-3, f"the cache's rows have {HEAD_DIM} dimensions, not {D}")
-        u8 = lambda n: torch.empty((n_pages, Hkv, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
-        return Kv4Cache(
-            k_codes=u8(D // 2), k_scales=u8(D // KV4_GROUP), v_codes=u8(D // 2), v_scales=u8(D // KV4_GROUP),
-            page_table=torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
-            free_pages=torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
-            free_count=torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size=page_size)
 
     @property
     def n_pages(self):
@@ -553,12 +533,12 @@ class Kv4Cache:
             _device_of(self.k_codes, "k_codes")
             if self.k_codes.dim() != 4:
                 raise AdapldError(-2, f"k_codes has shape {tuple(self.k_codes.shape)}, expected 4 dimensions")
-            n_pages, Hkv, page_size, half = self.k_codes.shape
-            codes = (n_pages, Hkv, self.page_size, half)
-            scales = (n_pages, Hkv, self.page_size, 2 * half // KV4_GROUP)
+            n_pages, Hkv = self.k_codes.shape[:2]
+            codes, scales, D = self._row_shapes(self.k_codes.shape[3])
+            codes, scales = (n_pages, Hkv, *codes), (n_pages, Hkv, *scales)
             ptrs = (_dptr(self.k_codes, "k_codes", u8, codes, dev), _dptr(self.k_scales, "k_scales", u8, scales, dev),
                     _dptr(self.v_codes, "v_codes", u8, codes, dev), _dptr(self.v_scales, "v_scales", u8, scales, dev))
-            pool = (self._pool_key(dev), ptrs, n_pages, Hkv, 2 * half)
+            pool = (self._pool_key(dev), ptrs, n_pages, Hkv, D)
             object.__setattr__(self, "_pool", pool)
         return pool
 
@@ -589,13 +569,78 @@ class Kv4Cache:
         return stack
 
 
+@dataclass
+class Kv4Cache(_PagedCache):
+    """The paged 4-bit K/V cache of B sequences: a pool of pages, the page
+    table of each sequence and the stack of free pages (adapld_kv4_*).  The
+    buffers may be the caller's own, and those that no call uses None: page_map
+    takes the table and the stack (of as many pages as the pool, where there is
+    one), the other calls the pool and (the attention) the table.  allocate()
+    makes an empty cache.  The buffers are checked and their pointers marshalled
+    at the first call, and again after one of the fields is assigned or a buffer
+    has another address, shape, type or layout."""
+    k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D / 2]
+    k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size, D / KV4_GROUP]
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    page_table: torch.Tensor    # int32 [B, max_pages]
+    free_pages: torch.Tensor    # int32 [n_pages], the stack
+    free_count: torch.Tensor    # int32 [1]
+    page_size: int
+
+    @staticmethod
+    def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
+        if D != HEAD_DIM:
+            raise AdapldError(-3, f"the cache's rows have {HEAD_DIM} dimensions, not {D}")
+        u8 = lambda n: torch.empty((n_pages, Hkv, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
+        return Kv4Cache(
+            k_codes=u8(D // 2), k_scales=u8(D // KV4_GROUP), v_codes=u8(D // 2), v_scales=u8(D // KV4_GROUP),
+            page_table=torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+            free_pages=torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+            free_count=torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size=page_size)
+
+    def _row_shapes(self, row_bytes):
+        """(shape of a page's codes, of its scales, dimensions of a row)."""
+        return (self.page_size, row_bytes), (self.page_size, 2 * row_bytes // KV4_GROUP), 2 * row_bytes
+
+
+@dataclass
+class Kv8Cache(_PagedCache):
+    """The paged 8-bit K/V cache of B sequences, with pages, table and stack as
+    in Kv4Cache (page_map serves both): E4M3 codes and a scale for each
+    KV8_BLOCK tokens of a page and kv head."""
+    k_codes: torch.Tensor       # uint8 [n_pages, Hkv, page_size, D]
+    k_scales: torch.Tensor      # uint8 [n_pages, Hkv, page_size / KV8_BLOCK]
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    page_table: torch.Tensor    # int32 [B, max_pages]
+    free_pages: torch.Tensor    # int32 [n_pages], the stack
+    free_count: torch.Tensor    # int32 [1]
+    page_size: int
+
+    @staticmethod
+    def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
+        if D != HEAD_DIM:
+            raise AdapldError(-3, f"the cache's rows have {HEAD_DIM} dimensions, not {D}")
+        u8 = lambda *n: torch.empty((n_pages, Hkv, *n), dtype=torch.uint8, device=device)  # noqa: E731
+        return Kv8Cache(
+            k_codes=u8(page_size, D), k_scales=u8(page_size // KV8_BLOCK), v_codes=u8(page_size, D),
+            v_scales=u8(page_size // KV8_BLOCK),
+            page_table=torch.full((B, max_pages), -1, dtype=torch.int32, device=device),
+            free_pages=torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+            free_count=torch.full((1,), n_pages, dtype=torch.int32, device=device), page_size=page_size)
+
+    def _row_shapes(self, row_bytes):
+        return (self.page_size, row_bytes), (self.page_size // KV8_BLOCK,), row_bytes
+
+
 _I32 = (torch.int32,)
 _F32 = (torch.float32,)
 _U8 = (torch.uint8,)
 _MASK = (torch.int64, torch.uint64)
 
 
-def page_map(cache: Kv4Cache, lens_old, lens_new, N=None, *, slot_map=None, granted=None, free_count_out=None,
+def page_map(cache: Kv4Cache | Kv8Cache, lens_old, lens_new, N=None, *, slot_map=None, granted=None, free_count_out=None,
              stream=None):
     """Pages for sequences that go from lens_old to lens_new tokens, and the
     slots of their first N new ones (N from slot_map if it is given); returns
@@ -665,12 +710,9 @@ def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None
     return k_out, v_out
 
 
-def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None,
-                         L_max=None, scale=None, out=None, lse=None, ws=None, with_lse=True, stream=None):
-    """tree_verify_attn with the context in the 4-bit cache; without k_tree,
-    v_tree and tree_mask every row attends to the context alone.  L_max bounds
-    the lengths (default: what the page table holds).  Returns (out, lse)."""
-    lib = load_library()
+def _tree_verify_attn_paged(name, op, q, cache, lens, node_count, k_tree, v_tree, tree_mask, L_max, scale, out, lse, ws,
+                            with_lse, stream):
+    fn = getattr(load_library(), name)
     dev = _device_of(q, "q")
     _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
     _, table, B, max_pages = cache._marshal_pages(dev)
@@ -686,7 +728,7 @@ def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v
             if lse is None and with_lse:
                 lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=q.device)
             if ws is None:
-                need = workspace_bytes(OP_TREE_VERIFY_ATTN_KV4, B, L_max, 0, 0, T_max, Hq, Hkv, D)
+                need = workspace_bytes(op, B, L_max, 0, 0, T_max, Hq, Hkv, D)
                 ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
     kt = vt = mask = None
     if k_tree is not None or v_tree is not None or tree_mask is not None:
@@ -694,15 +736,56 @@ def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v
         kt = _dptr(k_tree, "k_tree", _BF16_DTYPES, tree, dev)
         vt = _dptr(v_tree, "v_tree", _BF16_DTYPES, tree, dev)
         mask = _dptr(tree_mask, "tree_mask", _MASK, (B, T_max, (T_max + 63) // 64), dev)
-    st = lib.adapld_tree_verify_attn_kv4(
+    st = fn(
         _dptr(q, "q", _BF16_DTYPES, None, dev), *pool, table, kt, vt, _dptr(lens, "lens", _I32, (B,), dev),
         _dptr(node_count, "node_count", _I32, (B,), dev), mask, B, L_max, T_max, Hq, Hkv, D, cache.page_size, n_pages,
         max_pages, scale, _dptr(out, "out", _BF16_DTYPES, shape, dev),
         None if lse is None else _dptr(lse, "lse", _F32, (B, Hq, T_max), dev),
         _dptr(ws, "ws", _U8, None, dev), ws.numel(), _stream_on(stream, dev))
     if st:
-        _check(st, "adapld_tree_verify_attn_kv4")
+        _check(st, name)
     return out, lse
+
+
+def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None,
+                         L_max=None, scale=None, out=None, lse=None, ws=None, with_lse=True, stream=None):
+    """tree_verify_attn with the context in the 4-bit cache; without k_tree,
+    v_tree and tree_mask every row attends to the context alone.  L_max bounds
+    the lengths (default: what the page table holds).  Returns (out, lse)."""
+    return _tree_verify_attn_paged("adapld_tree_verify_attn_kv4", OP_TREE_VERIFY_ATTN_KV4, q, cache, lens, node_count,
+                                   k_tree, v_tree, tree_mask, L_max, scale, out, lse, ws, with_lse, stream)
+
+
+def kv8_append(cache: Kv8Cache, k_new, v_new, lens_old, lens_new, *, rows=None, N=None, stream=None):
+    """Quantises K/V rows (bf16 [B, n_src, Hkv, D]) into the cache: sequence b
+    goes from lens_old[b] to lens_new[b] tokens, of which the i-th new one is row
+    rows[b, i] (row i without rows).  N bounds the new tokens of a sequence
+    (default: the width of rows, or n_src)."""
+    dev = _device_of(k_new, "k_new")
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
+    _, table, B, max_pages = cache._marshal_pages(dev)
+    shape = k_new.shape
+    if len(shape) != 4 or shape[0] != B or shape[2] != Hkv or shape[3] != D:
+        raise AdapldError(-2, f"k_new has shape {tuple(shape)}, expected ({B}, n_src, {Hkv}, {D})")
+    n_src = shape[1]
+    if N is None:
+        N = n_src if rows is None else rows.shape[1]
+    if stream is not None:
+        _on(stream, dev)
+    st = load_library().adapld_kv8_append(
+        _dptr(k_new, "k_new", _BF16_DTYPES, None, dev), _dptr(v_new, "v_new", _BF16_DTYPES, shape, dev),
+        None if rows is None else _dptr(rows, "rows", _I32, (B, N), dev),
+        _dptr(lens_old, "lens_old", _I32, (B,), dev), _dptr(lens_new, "lens_new", _I32, (B,), dev), table, B, n_src, N,
+        Hkv, D, cache.page_size, n_pages, max_pages, *pool, _stream_on(stream, dev))
+    if st:
+        _check(st, "adapld_kv8_append")
+
+
+def tree_verify_attn_kv8(q, cache: Kv8Cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None,
+                         L_max=None, scale=None, out=None, lse=None, ws=None, with_lse=True, stream=None):
+    """tree_verify_attn_kv4 over the 8-bit cache.  Returns (out, lse)."""
+    return _tree_verify_attn_paged("adapld_tree_verify_attn_kv8", OP_TREE_VERIFY_ATTN_KV8, q, cache, lens, node_count,
+                                   k_tree, v_tree, tree_mask, L_max, scale, out, lse, ws, with_lse, stream)
 
 
 @dataclass

@@ -21,7 +21,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libadapld.so")
 
 SOURCES = ["lexical.hip", "semantic.hip", "tree.hip", "paper_tree.hip", "verify.hip", "accept.hip", "embed.hip", "ngram.hip", "noalloc.hip", "kv4.hip",
-           "kv4_verify.hip", "abi.cpp"]
+           "kv4_verify.hip", "kv8.hip", "kv8_verify.hip", "abi.cpp"]
 ARCH = "gfx950"
 
 # -packed-fp32-ops keeps the compiler from emitting packed fp32 VALU ops.
@@ -41,7 +41,8 @@ def hipcc() -> str:
 
 # Inputs of the verify attention are finite by contract, so its max reductions
 # need no NaN canonicalisation (v_max3 chains without quieting operations).
-PER_SOURCE_FLAGS = {"verify.hip": ["-fno-honor-nans"], "kv4_verify.hip": ["-fno-honor-nans"]}
+PER_SOURCE_FLAGS = {"verify.hip": ["-fno-honor-nans"], "kv4_verify.hip": ["-fno-honor-nans"],
+                    "kv8_verify.hip": ["-fno-honor-nans"]}
 
 
 def _compile(src: str) -> str:

@@ -4,6 +4,7 @@
 #include <cstdint>
 
 #include "adapld_internal.h"
+#include "kv8.h"
 
 namespace {
 
@@ -32,6 +33,7 @@ size_t step_sem_part(int B, int L_stride, int k) { return (semantic_ws(B, L_stri
 constexpr int64_t kKv4MaxRows = (1 << 28) - 16;
 constexpr int64_t kKv4MaxOutRows = (1 << 27) - 8;
 constexpr int64_t kKv4MaxGroups = (1 << 23) - 8;
+constexpr int64_t kKv8MaxBlocks = (1 << 26) - 4;
 
 // The embedding fallback's own part (16-byte aligned), then the scan's lists.
 size_t embed_head_ws(int B, int L_stride) { return (adapld::embed_ws_bytes(B, L_stride) + 15) / 16 * 16; }
@@ -157,10 +159,13 @@ size_t adapld_workspace_bytes(int op, int B, int L_stride, int d, int k, int T_m
       const adapld::VerifyPlan p = adapld::plan_verify(B, L_stride, T_max, Hq, Hkv);
       return adapld::verify_ws_bytes(p, B, Hkv);
     }
-    case ADAPLD_OP_TREE_VERIFY_ATTN_KV4: {
+    case ADAPLD_OP_TREE_VERIFY_ATTN_KV4:
+    case ADAPLD_OP_TREE_VERIFY_ATTN_KV8: {
       if (T_max < 1 || T_max > ADAPLD_MAX_TREE_NODES || Hq < 1 || Hkv < 1 || Hq % Hkv || L_stride > (1 << 30) ||
           (double)B * T_max * Hq > kKv4MaxOutRows)
         return 0;
+      if (op == ADAPLD_OP_TREE_VERIFY_ATTN_KV8)
+        return adapld::verify_kv8_ws_bytes(adapld::plan_verify_kv8(B, L_stride, T_max, Hq, Hkv), B, Hkv);
       return adapld::verify_kv4_ws_bytes(adapld::plan_verify_kv4(B, L_stride, T_max, Hq, Hkv), B, Hkv);
     }
     default:
@@ -471,6 +476,35 @@ int check_kv4_rows(const uint16_t* x, const uint16_t* y, const int32_t* slot_map
   return ADAPLD_OK;
 }
 
+// Checks of the verify attention over a paged cache, B != 0; `arrays` is the status
+// of the cache's own arrays.  On ADAPLD_OK p is the call's decomposition.
+int check_paged_verify(const adapld::VerifyPagedCall& c, int D, size_t ws_bytes, int arrays,
+                       adapld::VerifyPagedPlan (*plan)(int, int, int, int, int),
+                       size_t (*plan_bytes)(const adapld::VerifyPagedPlan&, int, int), adapld::VerifyPagedPlan& p) {
+  if (c.B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (!c.q || !c.page_table || !c.lens || !c.node_count || !c.out) return ADAPLD_ERR_NULL_ARG;
+  const int n_tree = (c.k_tree != nullptr) + (c.v_tree != nullptr) + (c.tree_mask != nullptr);
+  if (n_tree != 0 && n_tree != 3) return ADAPLD_ERR_NULL_ARG;
+  if (arrays != ADAPLD_OK) return arrays;
+  if (c.L_max < 1 || c.T_max < 1 || c.Hq < 1 || c.Hkv < 1 || c.Hq % c.Hkv != 0 || c.max_pages < 1 ||
+      !(c.scale > 0.f) || !std::isfinite(c.scale * 1.4426950408889634f))   // the kernels take logits in units of log2
+    return ADAPLD_ERR_INVALID_ARG;
+  if (const int st = check_kv4_pool(c.page_size, c.n_pages); st != ADAPLD_OK) return st;
+  if (D != ADAPLD_HEAD_DIM || c.T_max > ADAPLD_MAX_TREE_NODES || (int64_t)c.max_pages * c.page_size > INT32_MAX ||
+      c.L_max > (1 << 30) || (double)c.B * c.T_max * c.Hq > kKv4MaxOutRows)
+    return ADAPLD_ERR_UNSUPPORTED;
+  if (c.L_max > c.max_pages * c.page_size || misaligned16(c.q) || misaligned16(c.out) || misaligned16(c.k_tree) ||
+      misaligned16(c.v_tree))
+    return ADAPLD_ERR_INVALID_ARG;
+  p = plan(c.B, c.L_max, c.T_max, c.Hq, c.Hkv);
+  if ((double)c.B * c.Hkv * p.nsplit * p.rowgroups > kKv4MaxGroups - 8.0 * p.rowgroups) return ADAPLD_ERR_UNSUPPORTED;
+  const size_t need = plan_bytes(p, c.B, c.Hkv);
+  if (need > 0 && !c.ws) return ADAPLD_ERR_NULL_ARG;
+  if (ws_bytes < need) return ADAPLD_ERR_WORKSPACE_TOO_SMALL;
+  if (need > 0 && misaligned16(c.ws)) return ADAPLD_ERR_INVALID_ARG;
+  return ADAPLD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -525,32 +559,67 @@ int adapld_tree_verify_attn_kv4(const uint16_t* q, const uint8_t* k_codes, const
                                 const int32_t* node_count, const uint64_t* tree_mask, int B, int L_max, int T_max,
                                 int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, float scale,
                                 uint16_t* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const adapld::VerifyPagedCall c{q,   k_codes, k_scales, v_codes, v_scales, page_table, k_tree,   v_tree,  lens,
+                                  node_count, tree_mask, B,  L_max,   T_max,    Hq,      Hkv,      page_size,
+                                  n_pages, max_pages, scale, out, lse, ws};
+  if (B == 0) return ADAPLD_OK;
+  adapld::VerifyPagedPlan p;
+  const int st = check_paged_verify(c, D, ws_bytes, check_kv4_arrays(k_codes, k_scales, v_codes, v_scales),
+                                    adapld::plan_verify_kv4, adapld::verify_kv4_ws_bytes, p);
+  return st != ADAPLD_OK ? st : hip_status(adapld::launch_tree_verify_attn_kv4(c, p, stream));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------ paged 8-bit K/V cache
+
+namespace {
+
+int check_kv8_arrays(const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                     const uint8_t* v_scales) {
+  if (!k_codes || !k_scales || !v_codes || !v_scales) return ADAPLD_ERR_NULL_ARG;
+  return misaligned16(k_codes) || misaligned16(v_codes) ? ADAPLD_ERR_INVALID_ARG : ADAPLD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* lens_old,
+                      const int32_t* lens_new, const int32_t* page_table, int B, int n_src, int N, int Hkv, int D,
+                      int page_size, int n_pages, int max_pages, uint8_t* k_codes, uint8_t* k_scales,
+                      uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream) {
   if (B < 0) return ADAPLD_ERR_INVALID_ARG;
   if (B == 0) return ADAPLD_OK;
-  if (!q || !page_table || !lens || !node_count || !out) return ADAPLD_ERR_NULL_ARG;
-  const int n_tree = (k_tree != nullptr) + (v_tree != nullptr) + (tree_mask != nullptr);
-  if (n_tree != 0 && n_tree != 3) return ADAPLD_ERR_NULL_ARG;
-  if (const int st = check_kv4_arrays(k_codes, k_scales, v_codes, v_scales); st != ADAPLD_OK) return st;
-  if (L_max < 1 || T_max < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || !(scale > 0.f) ||
-      !std::isfinite(scale * 1.4426950408889634f))   // the kernels take logits in units of log2
+  if (!k_new || !v_new || !lens_old || !lens_new || !page_table) return ADAPLD_ERR_NULL_ARG;
+  if (const int st = check_kv8_arrays(k_codes, k_scales, v_codes, v_scales); st != ADAPLD_OK) return st;
+  if (n_src < 1 || N < 1 || Hkv < 1 || max_pages < 1 || (!rows && N > n_src) || misaligned16(k_new) ||
+      misaligned16(v_new))
     return ADAPLD_ERR_INVALID_ARG;
   if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
-  if (D != ADAPLD_HEAD_DIM || T_max > ADAPLD_MAX_TREE_NODES || (int64_t)max_pages * page_size > INT32_MAX ||
-      L_max > (1 << 30) || (double)B * T_max * Hq > kKv4MaxOutRows)
+  // a wave of 64 threads a block of a kv head, below 2^32 threads a launch
+  if (D != ADAPLD_HEAD_DIM || (int64_t)max_pages * page_size > INT32_MAX ||
+      (double)B * adapld::kv8_blocks_touched(N) * Hkv > kKv8MaxBlocks)
     return ADAPLD_ERR_UNSUPPORTED;
-  if (L_max > max_pages * page_size || misaligned16(q) || misaligned16(out) || misaligned16(k_tree) ||
-      misaligned16(v_tree))
-    return ADAPLD_ERR_INVALID_ARG;
-  const adapld::VerifyKv4Plan p = adapld::plan_verify_kv4(B, L_max, T_max, Hq, Hkv);
-  if ((double)B * Hkv * p.nsplit * p.rowgroups > kKv4MaxGroups - 8.0 * p.rowgroups) return ADAPLD_ERR_UNSUPPORTED;
-  const size_t need = adapld::verify_kv4_ws_bytes(p, B, Hkv);
-  if (need > 0 && !ws) return ADAPLD_ERR_NULL_ARG;
-  if (ws_bytes < need) return ADAPLD_ERR_WORKSPACE_TOO_SMALL;
-  if (need > 0 && misaligned16(ws)) return ADAPLD_ERR_INVALID_ARG;
-  const adapld::VerifyKv4Call c{q,   k_codes, k_scales, v_codes, v_scales, page_table, k_tree,   v_tree,  lens,
-                                node_count, tree_mask, B,  L_max,   T_max,    Hq,      Hkv,      page_size,
-                                n_pages, max_pages, scale, out, lse, ws};
-  return hip_status(adapld::launch_tree_verify_attn_kv4(c, p, stream));
+  return hip_status(adapld::launch_kv8_append(k_new, v_new, rows, lens_old, lens_new, page_table, B, n_src, N, Hkv,
+                                              page_size, n_pages, max_pages, k_codes, k_scales, v_codes, v_scales,
+                                              stream));
+}
+
+int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,
+                                const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* page_table,
+                                const uint16_t* k_tree, const uint16_t* v_tree, const int32_t* lens,
+                                const int32_t* node_count, const uint64_t* tree_mask, int B, int L_max, int T_max,
+                                int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, float scale,
+                                uint16_t* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const adapld::VerifyPagedCall c{q,   k_codes, k_scales, v_codes, v_scales, page_table, k_tree,   v_tree,  lens,
+                                  node_count, tree_mask, B,  L_max,   T_max,    Hq,      Hkv,      page_size,
+                                  n_pages, max_pages, scale, out, lse, ws};
+  if (B == 0) return ADAPLD_OK;
+  adapld::VerifyPagedPlan p;
+  const int st = check_paged_verify(c, D, ws_bytes, check_kv8_arrays(k_codes, k_scales, v_codes, v_scales),
+                                    adapld::plan_verify_kv8, adapld::verify_kv8_ws_bytes, p);
+  return st != ADAPLD_OK ? st : hip_status(adapld::launch_tree_verify_attn_kv8(c, p, stream));
 }
 
 }  // extern "C"

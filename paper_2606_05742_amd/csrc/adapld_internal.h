@@ -174,18 +174,18 @@ hipError_t launch_kv4_gather(const uint8_t* k_codes, const uint8_t* k_scales, co
                              const uint8_t* v_scales, const int32_t* slot_map, int B, int N, int Hkv, int page_size,
                              int n_pages, uint16_t* k_out, uint16_t* v_out, hipStream_t stream);
 
-// How the verify attention over the 4-bit cache decomposes a problem.
-struct VerifyKv4Plan {
+// How the verify attention over a paged cache decomposes a problem.
+struct VerifyPagedPlan {
   int rows_max;    // T_max * G stacked query rows per (sequence, kv head)
   int rows;        // stacked rows per workgroup: 16, 32, 64 (narrow kernel), 128 or 256
   int rowgroups;   // workgroups along the rows
   int nsplit;      // context splits
   int chunk;       // context keys per split (multiple of kKeyTile)
 };
-VerifyKv4Plan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv);
-size_t verify_kv4_ws_bytes(const VerifyKv4Plan& p, int B, int Hkv);
+VerifyPagedPlan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv);
+size_t verify_kv4_ws_bytes(const VerifyPagedPlan& p, int B, int Hkv);
 
-struct VerifyKv4Call {
+struct VerifyPagedCall {
   const uint16_t* q;
   const uint8_t* k_codes;
   const uint8_t* k_scales;
@@ -203,6 +203,15 @@ struct VerifyKv4Call {
   float* lse;
   void* ws;
 };
-hipError_t launch_tree_verify_attn_kv4(const VerifyKv4Call& c, const VerifyKv4Plan& p, hipStream_t stream);
+hipError_t launch_tree_verify_attn_kv4(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipStream_t stream);
+
+// ------------------------------------------------------ paged 8-bit K/V cache
+hipError_t launch_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* lens_old,
+                             const int32_t* lens_new, const int32_t* page_table, int B, int n_src, int N, int Hkv,
+                             int page_size, int n_pages, int max_pages, uint8_t* k_codes, uint8_t* k_scales,
+                             uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream);
+VerifyPagedPlan plan_verify_kv8(int B, int L_max, int T_max, int Hq, int Hkv);
+size_t verify_kv8_ws_bytes(const VerifyPagedPlan& p, int B, int Hkv);
+hipError_t launch_tree_verify_attn_kv8(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipStream_t stream);
 
 }  // namespace adapld
