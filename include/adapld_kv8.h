@@ -21,6 +21,46 @@ extern "C" {
 #define ADAPLD_OP_TREE_VERIFY_ATTN_KV8 10
 
 /*
+ * adapld_qk_norm_rope -- the norm of every query and key head and the rotation
+ * by its token's position, in one pass: what makes the q and k_tree of the
+ * verify attention, and the keys that enter a cache, from a projection's rows.
+ *
+ * For token u of sequence b (u < counts[b], clamped on the device to [0, T]) and
+ * each head x of its q and k:
+ *   y = x * w / sqrt(mean(x^2) + eps)      (y = x without that weight)
+ * then, for pair i < rot_dim / 2 of dimensions (i, i + rot_dim / 2), or (2i, 2i +
+ * 1) with interleaved = 1, turned by a = 2 pi * frac(p * freqs[i] / 2^64):
+ *   (y1, y2) -> (y1 cos a - y2 sin a, y2 cos a + y1 sin a)
+ * with the position p = base[b] + offsets[b, u], or base[b] + u without offsets
+ * (the sum in 64 bits; p may be negative).  The other dimensions are y.  p * freqs
+ * is exact modulo one turn, however far the position.  All of it is computed in
+ * fp32 and rounded to bf16 once.  A row's infinities and NaN stay in it.
+ *
+ *   q, k        bf16, token u of sequence b at q + b * q_batch + u * q_token (in
+ *               elements, multiples of 8): its heads [Hq, D] or [Hkv, D], dense
+ *   q_weight, k_weight  bf16 [D], or NULL: no norm of that side
+ *   freqs       uint64 [rot_dim / 2]: turns per position in units of 2^-64 (a
+ *               negative frequency modulo 2^64); may be NULL if rot_dim is 0
+ *   base        int32 [B]
+ *   offsets     int32 [B, T] or NULL      e.g. a tree's node_depth
+ *   counts      int32 [B] or NULL (T)     e.g. node_count
+ *   rot_dim     0..D, a multiple of 16
+ *   q_out       bf16 [B, T, Hq, D]  (out) rows u >= counts[b] are not written
+ *   k_out       bf16 [B, T, Hkv, D] (out)
+ * q_out may be q itself and k_out k, where those are dense; no other overlap.
+ *
+ * Errors: NULL_ARG; INVALID_ARG for B < 0, T, Hq, Hkv < 1, rot_dim outside 0..D or
+ * no multiple of 16, interleaved outside {0, 1}, eps not finite or < 0, strides
+ * that are negative or no multiples of 8, misaligned pointers (8 bytes for
+ * freqs); UNSUPPORTED for D != 128 or B * T * (Hq + Hkv) > 2^28 - 16.
+ */
+int adapld_qk_norm_rope(const uint16_t* q, const uint16_t* k, int64_t q_batch, int64_t q_token, int64_t k_batch,
+                        int64_t k_token, const uint16_t* q_weight, const uint16_t* k_weight, const uint64_t* freqs,
+                        const int32_t* base, const int32_t* offsets, const int32_t* counts, int B, int T, int Hq,
+                        int Hkv, int D, int rot_dim, int interleaved, float eps, uint16_t* q_out, uint16_t* k_out,
+                        hipStream_t stream);
+
+/*
  * Paged 8-bit K/V cache -- the context's K/V of the verify attention in pages
  * of a pool, at 256 bytes and an eighth per token and kv head.
  *

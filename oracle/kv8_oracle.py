@@ -85,3 +85,23 @@ def kv8_rows(codes, scales, table, page, L):
         p, off = int(table[j // page]), j % page
         out[:, j] = kv8_values(codes[p, :, off], scales[p, :, off // BLOCK][:, None])
     return out
+
+
+def qk_norm_rope(x, weight, freqs, positions, eps, interleaved):
+    """x float64 [tokens, heads, D] of bf16 values, weight float64 [D] or None,
+    freqs as integers (turns per position in units of 2^-64), positions as
+    integers: the rotated rows in float64, and the largest magnitude that takes
+    part in each value."""
+    out = np.array(x, np.float64)
+    if weight is not None:
+        out = out / np.sqrt((out * out).mean(-1, keepdims=True) + eps) * weight
+    h = len(freqs)
+    size = np.abs(out)
+    for i, f in enumerate(freqs):
+        lo, hi = (2 * i, 2 * i + 1) if interleaved else (i, i + h)
+        a = np.array([2 * math.pi * (((int(p) * int(f)) % (1 << 64)) / 2.0 ** 64) for p in positions])[:, None]
+        y1, y2 = out[..., lo].copy(), out[..., hi].copy()
+        out[..., lo] = y1 * np.cos(a) - y2 * np.sin(a)
+        out[..., hi] = y2 * np.cos(a) + y1 * np.sin(a)
+        size[..., lo] = size[..., hi] = np.abs(y1) + np.abs(y2)
+    return out, size

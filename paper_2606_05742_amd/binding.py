@@ -14,6 +14,7 @@ import ctypes
 import math
 import os
 from dataclasses import dataclass
+from typing import ClassVar
 
 import torch
 
@@ -96,6 +97,8 @@ SIGNATURES = {
     "adapld_kv4_gather": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int] * 6 + [ctypes.c_void_p] * 3),
     "adapld_tree_verify_attn_kv4": (ctypes.c_int, [ctypes.c_void_p] * 11 + [ctypes.c_int] * 9 + [ctypes.c_float]
                                     + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
+    "adapld_qk_norm_rope": (ctypes.c_int, [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 4 + [ctypes.c_void_p] * 6
+                            + [ctypes.c_int] * 7 + [ctypes.c_float] + [ctypes.c_void_p] * 3),
     "adapld_kv8_append": (ctypes.c_int, [ctypes.c_void_p] * 6 + [ctypes.c_int] * 8 + [ctypes.c_void_p] * 5),
     "adapld_tree_verify_attn_kv8": (ctypes.c_int, [ctypes.c_void_p] * 11 + [ctypes.c_int] * 9 + [ctypes.c_float]
                                     + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
@@ -183,6 +186,21 @@ def _dptr(t, name, dtypes, shape, dev, nullable=False):
     if p is not None and t.get_device() != dev:
         raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
     return p
+
+
+def _rows_ptr(t, name, dev):
+    """The pointer of bf16 [B, T, heads, D] whose heads and dimensions are
+    contiguous, on the current device; tokens and sequences may be strided."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != dev:
+        raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
+    if t.dtype not in _BF16_DTYPES:
+        raise AdapldError(-2, f"{name} has dtype {t.dtype}, expected one of {_BF16_DTYPES}")
+    D = t.shape[3]
+    if t.stride(3) != 1 or (t.stride(2) != D and t.shape[2] != 1):
+        raise AdapldError(-2, f"{name} must be contiguous in its heads and dimensions, its strides are {t.stride()}")
+    return t.data_ptr()
 
 
 def _stream_on(stream, dev):
@@ -489,6 +507,54 @@ class NgramIndex:
         return outs
 
 
+def rope_frequencies(rot_dim, theta=10000.0, *, rad_per_token=None, device="cuda"):
+    """The table qk_norm_rope takes: turns per position of each of the rot_dim / 2
+    pairs, as int64 in units of 2^-64.  By default theta^(-2i / rot_dim) radians;
+    rad_per_token (a sequence of floats of any sign) gives others, e.g. scaled ones."""
+    if rot_dim % 2 or rot_dim < 0:
+        raise AdapldError(-2, f"rot_dim must be even and not negative, got {rot_dim}")
+    if rad_per_token is None:
+        rad_per_token = [theta ** (-2.0 * i / rot_dim) for i in range(rot_dim // 2)]
+    if len(rad_per_token) != rot_dim // 2 or not all(math.isfinite(f) for f in rad_per_token):
+        raise AdapldError(-2, f"rad_per_token must be {rot_dim // 2} finite numbers")
+    turns = [int(math.fmod(f / (2 * math.pi), 1.0) * 2.0 ** 64) for f in rad_per_token]
+    wrapped = [(t + (1 << 63)) % (1 << 64) - (1 << 63) for t in turns]
+    return torch.tensor(wrapped, dtype=torch.int64, device=device)
+
+
+def qk_norm_rope(q, k, freqs, base, *, offsets=None, counts=None, q_weight=None, k_weight=None, eps=1e-6,
+                 interleaved=False, q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of q (bf16 [B, T, Hq, D]) and k (bf16 [B, T, Hkv,
+    D]) with the weights (bf16 [D] each, or none: no norm), and the rotation of
+    their first 2 * len(freqs) dimensions by the token's position base[b] +
+    offsets[b, u] (offsets default to u), in one pass.  q and k may be slices of a
+    fused projection: heads and dimensions contiguous, any strides of tokens and
+    sequences that are multiples of 8.  Rows u >= counts[b] are not written.
+    Returns (q_out, k_out), contiguous."""
+    dev = _device_of(q, "q")
+    shape, kshape = q.shape, k.shape
+    if len(shape) != 4 or len(kshape) != 4 or kshape[:2] != shape[:2] or kshape[3] != shape[3]:
+        raise AdapldError(-2, f"q has shape {tuple(shape)} and k {tuple(kshape)}, expected (B, T, heads, D)")
+    B, T, Hq, D = shape
+    Hkv = kshape[2]
+    if q_out is None or k_out is None or stream is not None:
+        with _on(stream, dev):
+            q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
+            k_out = torch.empty(kshape, dtype=torch.bfloat16, device=q.device) if k_out is None else k_out
+    weight = _BF16_DTYPES, (D,), dev, True
+    st = load_library().adapld_qk_norm_rope(
+        _rows_ptr(q, "q", dev), _rows_ptr(k, "k", dev), q.stride(0), q.stride(1), k.stride(0), k.stride(1),
+        _dptr(q_weight, "q_weight", *weight), _dptr(k_weight, "k_weight", *weight),
+        _dptr(freqs, "freqs", _I64, None, dev), _dptr(base, "base", _I32, (B,), dev),
+        _dptr(offsets, "offsets", _I32, (B, T), dev, True), _dptr(counts, "counts", _I32, (B,), dev, True),
+        B, T, Hq, Hkv, D, 2 * freqs.numel(), int(bool(interleaved)), eps,
+        _dptr(q_out, "q_out", _BF16_DTYPES, shape, dev), _dptr(k_out, "k_out", _BF16_DTYPES, kshape, dev),
+        _stream_on(stream, dev))
+    if st:
+        _check(st, "adapld_qk_norm_rope")
+    return q_out, k_out
+
+
 class _PagedCache:
     """What the paged caches share: the checks of their buffers, which are made
     at the first call, and again after one of the fields is assigned or a buffer
@@ -525,8 +591,11 @@ class _PagedCache:
         return (dev, t.data_ptr(), t.shape, t.dtype, t.is_contiguous(), n.data_ptr(), n.shape, n.dtype,
                 n.is_contiguous(), None if pool is None else pool.shape)
 
-    def _marshal_pool(self, dev):
-        """(key, pointers of the four arrays, n_pages, Hkv, D)."""
+    def _marshal_pool(self, dev, bits):
+        """(key, pointers of the four arrays, n_pages, Hkv, D), for a call on rows of
+        `bits` bits a value."""
+        if self.bits != bits:
+            raise AdapldError(-2, f"the call takes a cache of {bits} bits a value, not of {self.bits}")
         pool = self._pool
         if pool is None or pool[0] != self._pool_key(dev):
             u8 = (torch.uint8,)
@@ -587,6 +656,7 @@ class Kv4Cache(_PagedCache):
     free_pages: torch.Tensor    # int32 [n_pages], the stack
     free_count: torch.Tensor    # int32 [1]
     page_size: int
+    bits: ClassVar[int] = 4
 
     @staticmethod
     def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
@@ -617,6 +687,7 @@ class Kv8Cache(_PagedCache):
     free_pages: torch.Tensor    # int32 [n_pages], the stack
     free_count: torch.Tensor    # int32 [1]
     page_size: int
+    bits: ClassVar[int] = 8
 
     @staticmethod
     def allocate(n_pages, page_size, Hkv, B, max_pages, D=HEAD_DIM, device="cuda"):
@@ -635,6 +706,7 @@ class Kv8Cache(_PagedCache):
 
 
 _I32 = (torch.int32,)
+_I64 = (torch.int64,)
 _F32 = (torch.float32,)
 _U8 = (torch.uint8,)
 _MASK = (torch.int64, torch.uint64)
@@ -671,7 +743,7 @@ def kv4_append(cache: Kv4Cache, k_new, v_new, slot_map, *, rows=None, stream=Non
     rows[b, i] (row i without rows) of sequence b at slot_map[b, i]; slots of
     -1 are padding."""
     dev = _device_of(k_new, "k_new")
-    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev, 4)
     shape = k_new.shape
     if len(shape) != 4 or shape[2] != Hkv or shape[3] != D:
         raise AdapldError(-2, f"k_new has shape {tuple(shape)}, expected (B, n_src, {Hkv}, {D})")
@@ -693,7 +765,7 @@ def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None
     returns (k_out, v_out).  Rows of slots outside the pool are left as they
     are (zero in new outputs)."""
     dev = _device_of(slot_map, "slot_map")
-    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev, 4)
     B, N = slot_map.shape
     shape = (B, N, Hkv, D)
     new = lambda: torch.zeros(shape, dtype=torch.bfloat16, device=slot_map.device)  # noqa: E731
@@ -710,50 +782,58 @@ def kv4_gather(cache: Kv4Cache, slot_map, *, k_out=None, v_out=None, stream=None
     return k_out, v_out
 
 
-def _tree_verify_attn_paged(name, op, q, cache, lens, node_count, k_tree, v_tree, tree_mask, L_max, scale, out, lse, ws,
-                            with_lse, stream):
-    fn = getattr(load_library(), name)
-    dev = _device_of(q, "q")
-    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
-    _, table, B, max_pages = cache._marshal_pages(dev)
-    shape = q.shape
-    if len(shape) != 4 or shape[0] != B or shape[3] != D:
-        raise AdapldError(-2, f"q has shape {tuple(shape)}, expected ({B}, T_max, Hq, {D})")
-    T_max, Hq = shape[1], shape[2]
-    L_max = max_pages * cache.page_size if L_max is None else L_max
-    scale = 1.0 / math.sqrt(D) if scale is None else scale
-    if out is None or lse is None or ws is None or stream is not None:
-        with _on(stream, dev):
-            out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if out is None else out
-            if lse is None and with_lse:
-                lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=q.device)
-            if ws is None:
-                need = workspace_bytes(op, B, L_max, 0, 0, T_max, Hq, Hkv, D)
-                ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-    kt = vt = mask = None
-    if k_tree is not None or v_tree is not None or tree_mask is not None:
-        tree = (B, T_max, Hkv, D)
-        kt = _dptr(k_tree, "k_tree", _BF16_DTYPES, tree, dev)
-        vt = _dptr(v_tree, "v_tree", _BF16_DTYPES, tree, dev)
-        mask = _dptr(tree_mask, "tree_mask", _MASK, (B, T_max, (T_max + 63) // 64), dev)
-    st = fn(
-        _dptr(q, "q", _BF16_DTYPES, None, dev), *pool, table, kt, vt, _dptr(lens, "lens", _I32, (B,), dev),
-        _dptr(node_count, "node_count", _I32, (B,), dev), mask, B, L_max, T_max, Hq, Hkv, D, cache.page_size, n_pages,
-        max_pages, scale, _dptr(out, "out", _BF16_DTYPES, shape, dev),
-        None if lse is None else _dptr(lse, "lse", _F32, (B, Hq, T_max), dev),
-        _dptr(ws, "ws", _U8, None, dev), ws.numel(), _stream_on(stream, dev))
-    if st:
-        _check(st, name)
-    return out, lse
+def _paged_verify(name, op, bits, doc):
+    """The verify attention over a paged cache by the entry point `name` (a
+    function of its own for each, so that a call costs the host one frame)."""
+    def verify(q, cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None, L_max=None, scale=None,
+               out=None, lse=None, ws=None, with_lse=True, stream=None):
+        fn = getattr(load_library(), name)
+        dev = _device_of(q, "q")
+        _, pool, n_pages, Hkv, D = cache._marshal_pool(dev, bits)
+        _, table, B, max_pages = cache._marshal_pages(dev)
+        shape = q.shape
+        if len(shape) != 4 or shape[0] != B or shape[3] != D:
+            raise AdapldError(-2, f"q has shape {tuple(shape)}, expected ({B}, T_max, Hq, {D})")
+        T_max, Hq = shape[1], shape[2]
+        L_max = max_pages * cache.page_size if L_max is None else L_max
+        scale = 1.0 / math.sqrt(D) if scale is None else scale
+        if out is None or lse is None or ws is None or stream is not None:
+            with _on(stream, dev):
+                out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if out is None else out
+                if lse is None and with_lse:
+                    lse = torch.empty((B, Hq, T_max), dtype=torch.float32, device=q.device)
+                if ws is None:
+                    need = workspace_bytes(op, B, L_max, 0, 0, T_max, Hq, Hkv, D)
+                    ws = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        kt = vt = mask = None
+        if k_tree is not None or v_tree is not None or tree_mask is not None:
+            tree = (B, T_max, Hkv, D)
+            kt = _dptr(k_tree, "k_tree", _BF16_DTYPES, tree, dev)
+            vt = _dptr(v_tree, "v_tree", _BF16_DTYPES, tree, dev)
+            mask = _dptr(tree_mask, "tree_mask", _MASK, (B, T_max, (T_max + 63) // 64), dev)
+        st = fn(
+            _dptr(q, "q", _BF16_DTYPES, None, dev), *pool, table, kt, vt, _dptr(lens, "lens", _I32, (B,), dev),
+            _dptr(node_count, "node_count", _I32, (B,), dev), mask, B, L_max, T_max, Hq, Hkv, D, cache.page_size, n_pages,
+            max_pages, scale, _dptr(out, "out", _BF16_DTYPES, shape, dev),
+            None if lse is None else _dptr(lse, "lse", _F32, (B, Hq, T_max), dev),
+            _dptr(ws, "ws", _U8, None, dev), ws.numel(), _stream_on(stream, dev))
+        if st:
+            _check(st, name)
+        return out, lse
+
+    verify.__name__ = verify.__qualname__ = name.removeprefix("adapld_")
+    verify.__doc__ = doc
+    return verify
 
 
-def tree_verify_attn_kv4(q, cache: Kv4Cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None,
-                         L_max=None, scale=None, out=None, lse=None, ws=None, with_lse=True, stream=None):
+tree_verify_attn_kv4 = _paged_verify(
+    "adapld_tree_verify_attn_kv4", OP_TREE_VERIFY_ATTN_KV4, 4,
     """tree_verify_attn with the context in the 4-bit cache; without k_tree,
     v_tree and tree_mask every row attends to the context alone.  L_max bounds
-    the lengths (default: what the page table holds).  Returns (out, lse)."""
-    return _tree_verify_attn_paged("adapld_tree_verify_attn_kv4", OP_TREE_VERIFY_ATTN_KV4, q, cache, lens, node_count,
-                                   k_tree, v_tree, tree_mask, L_max, scale, out, lse, ws, with_lse, stream)
+    the lengths (default: what the page table holds).  Returns (out, lse).""")
+tree_verify_attn_kv8 = _paged_verify(
+    "adapld_tree_verify_attn_kv8", OP_TREE_VERIFY_ATTN_KV8, 8,
+    """tree_verify_attn_kv4 over the 8-bit cache.  Returns (out, lse).""")
 
 
 def kv8_append(cache: Kv8Cache, k_new, v_new, lens_old, lens_new, *, rows=None, N=None, stream=None):
@@ -762,7 +842,7 @@ def kv8_append(cache: Kv8Cache, k_new, v_new, lens_old, lens_new, *, rows=None, 
     rows[b, i] (row i without rows).  N bounds the new tokens of a sequence
     (default: the width of rows, or n_src)."""
     dev = _device_of(k_new, "k_new")
-    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev)
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev, 8)
     _, table, B, max_pages = cache._marshal_pages(dev)
     shape = k_new.shape
     if len(shape) != 4 or shape[0] != B or shape[2] != Hkv or shape[3] != D:
@@ -779,13 +859,6 @@ def kv8_append(cache: Kv8Cache, k_new, v_new, lens_old, lens_new, *, rows=None, 
         Hkv, D, cache.page_size, n_pages, max_pages, *pool, _stream_on(stream, dev))
     if st:
         _check(st, "adapld_kv8_append")
-
-
-def tree_verify_attn_kv8(q, cache: Kv8Cache, lens, node_count, *, k_tree=None, v_tree=None, tree_mask=None,
-                         L_max=None, scale=None, out=None, lse=None, ws=None, with_lse=True, stream=None):
-    """tree_verify_attn_kv4 over the 8-bit cache.  Returns (out, lse)."""
-    return _tree_verify_attn_paged("adapld_tree_verify_attn_kv8", OP_TREE_VERIFY_ATTN_KV8, q, cache, lens, node_count,
-                                   k_tree, v_tree, tree_mask, L_max, scale, out, lse, ws, with_lse, stream)
 
 
 @dataclass

@@ -585,6 +585,29 @@ int check_kv8_arrays(const uint8_t* k_codes, const uint8_t* k_scales, const uint
 
 extern "C" {
 
+int adapld_qk_norm_rope(const uint16_t* q, const uint16_t* k, int64_t q_batch, int64_t q_token, int64_t k_batch,
+                        int64_t k_token, const uint16_t* q_weight, const uint16_t* k_weight, const uint64_t* freqs,
+                        const int32_t* base, const int32_t* offsets, const int32_t* counts, int B, int T, int Hq,
+                        int Hkv, int D, int rot_dim, int interleaved, float eps, uint16_t* q_out, uint16_t* k_out,
+                        hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (!q || !k || !base || !q_out || !k_out || (rot_dim > 0 && !freqs)) return ADAPLD_ERR_NULL_ARG;
+  if (T < 1 || Hq < 1 || Hkv < 1 || rot_dim < 0 || rot_dim > D || rot_dim % 16 != 0 || interleaved < 0 ||
+      interleaved > 1 || !(eps >= 0.f) || !std::isfinite(eps))
+    return ADAPLD_ERR_INVALID_ARG;
+  for (const int64_t stride : {q_batch, q_token, k_batch, k_token})
+    if (stride < 0 || stride % 8 != 0) return ADAPLD_ERR_INVALID_ARG;
+  for (const void* p : {(const void*)q, (const void*)k, (const void*)q_weight, (const void*)k_weight,
+                        (const void*)q_out, (const void*)k_out})
+    if (misaligned16(p)) return ADAPLD_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(freqs) & 7u) != 0) return ADAPLD_ERR_INVALID_ARG;
+  if (D != ADAPLD_HEAD_DIM || (double)B * T * ((double)Hq + Hkv) > kKv4MaxRows) return ADAPLD_ERR_UNSUPPORTED;
+  const adapld::NormRopeCall c{{q, k}, {q_batch, k_batch}, {q_token, k_token}, {q_weight, k_weight}, freqs, base,
+                               offsets, counts, B, T, Hq, Hkv, rot_dim, interleaved, eps, {q_out, k_out}};
+  return hip_status(adapld::launch_qk_norm_rope(c, stream));
+}
+
 int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* lens_old,
                       const int32_t* lens_new, const int32_t* page_table, int B, int n_src, int N, int Hkv, int D,
                       int page_size, int n_pages, int max_pages, uint8_t* k_codes, uint8_t* k_scales,

@@ -206,6 +206,20 @@ struct VerifyPagedCall {
 hipError_t launch_tree_verify_attn_kv4(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipStream_t stream);
 
 // ------------------------------------------------------ paged 8-bit K/V cache
+struct NormRopeCall {
+  const uint16_t* x[2];   // q and k
+  int64_t batch[2], token[2];
+  const uint16_t* weight[2];
+  const uint64_t* freqs;
+  const int32_t* base;
+  const int32_t* offsets;
+  const int32_t* counts;
+  int B, T, Hq, Hkv, rot_dim, interleaved;
+  float eps;
+  uint16_t* out[2];
+};
+hipError_t launch_qk_norm_rope(const NormRopeCall& c, hipStream_t stream);
+
 hipError_t launch_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* lens_old,
                              const int32_t* lens_new, const int32_t* page_table, int B, int n_src, int N, int Hkv,
                              int page_size, int n_pages, int max_pages, uint8_t* k_codes, uint8_t* k_scales,

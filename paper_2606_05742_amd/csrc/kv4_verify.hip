@@ -27,9 +27,8 @@ struct Kv4Format {
   static __device__ __forceinline__ uint32_t load_scale(const uint8_t* scales, size_t row, uint32_t key, int part) {
     return (scales + row * kKv4Scales)[key * kKv4Scales + part];
   }
-  static __device__ __forceinline__ uint4 dequant(const uint4 (&v)[1], int j, float X) {
-    const uint32_t w[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
-    const uint32_t c = w[j];
+  static __device__ __forceinline__ uint4 dequant(const u32x4_t (&v)[1], int j, float X) {
+    const uint32_t c = v[0][j];
     uint4 r;
     r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 0));
     r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, X, 1));

@@ -16,9 +16,8 @@ struct Kv8Format {
   static __device__ __forceinline__ uint32_t load_scale(const uint8_t* scales, size_t row, uint32_t, int) {
     return scales[row >> kKv8BlockShift];
   }
-  static __device__ __forceinline__ uint4 dequant(const uint4 (&v)[2], int j, float X) {
-    const uint4 c = v[j >> 1];
-    return kv8_values(j & 1 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), X);
+  static __device__ __forceinline__ uint4 dequant(const u32x4_t (&v)[2], int j, float X) {
+    return kv8_values(make_uint2(v[j >> 1][2 * (j & 1)], v[j >> 1][2 * (j & 1) + 1]), X);
   }
 };
 

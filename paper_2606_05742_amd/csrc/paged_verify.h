@@ -35,6 +35,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
@@ -94,14 +95,11 @@ __device__ __forceinline__ int swz16(int r) { return ((r & 7) << 1) | (((r >> 2)
 __device__ __forceinline__ bf16x8_t as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8_t, v); }
 
 // 16 bytes of codes; STREAM for data that nothing reads again.
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 template <bool STREAM>
-__device__ __forceinline__ uint4 load_codes(const uint8_t* p) {
+__device__ __forceinline__ u32x4_t load_codes(const uint8_t* p) {
   const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p);
-  u32x4_t v;
-  if constexpr (STREAM) v = __builtin_nontemporal_load(q);
-  else v = *q;
-  return make_uint4(v[0], v[1], v[2], v[3]);
+  if constexpr (STREAM) return __builtin_nontemporal_load(q);
+  else return *q;
 }
 
 // ------------------------------------------------- one 32-row block's softmax
@@ -324,7 +322,7 @@ __global__ __launch_bounds__(kThreads, 1) void paged_verify_kernel(const PagedAr
   for (int j = 0; j < 4; ++j) lpos[j] = (F::chunk(lgrp, j) ^ swz(lkey)) << 4;
 
   struct Codes {
-    uint4 c[F::kLoads];
+    u32x4_t c[F::kLoads];
     uint32_t e;
   };
   auto load = [&](int t, Codes& x) {
@@ -345,7 +343,7 @@ __global__ __launch_bounds__(kThreads, 1) void paged_verify_kernel(const PagedAr
     const size_t row = pool_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
 #pragma unroll
     for (int i = 0; i < F::kLoads; ++i)
-      x.c[i] = *reinterpret_cast<const uint4*>(codes + row * F::kCodeBytes + F::code_at(key, lgrp, i));
+      x.c[i] = load_codes<false>(codes + row * F::kCodeBytes + F::code_at(key, lgrp, i));
     x.e = F::load_scale(scales, row, key, lgrp);
   };
   auto store = [&](int t, const Codes& x) {
@@ -672,7 +670,7 @@ struct Rows16 {
     for (int j = 0; j < 4; ++j) q[j] = as_bf16x8(make_uint4(0, 0, 0, 0));
   }
   // Codes as loaded are in order: of key 16*i + col the part quad.
-  static __device__ __forceinline__ void order_codes(uint4 (&)[2][F::kLoads], uint32_t (&)[2]) {}
+  static __device__ __forceinline__ void order_codes(u32x4_t (&)[2][F::kLoads], uint32_t (&)[2]) {}
   static __device__ __forceinline__ int key_of(int i) { return 16 * i + (lane_id() & 15); }
   static __device__ __forceinline__ int part_of(int) { return lane_id() >> 4; }
 
@@ -790,20 +788,18 @@ struct Rows32 {
   }
   // From part `quad` of keys col and 16 + col to parts 2 * half + {0, 1} of key
   // lane & 31: lanes 16 apart exchange one of their two.
-  static __device__ __forceinline__ void order_codes(uint4 (&k)[2][F::kLoads], uint32_t (&e)[2]) {
-    auto swap = [](uint32_t& p, uint32_t& q) {
-      const auto t = __builtin_amdgcn_permlane16_swap(p, q, false, false);
-      p = t[0];
-      q = t[1];
-    };
+  static __device__ __forceinline__ void order_codes(u32x4_t (&k)[2][F::kLoads], uint32_t (&e)[2]) {
 #pragma unroll
-    for (int i = 0; i < F::kLoads; ++i) {
-      swap(k[0][i].x, k[1][i].x);
-      swap(k[0][i].y, k[1][i].y);
-      swap(k[0][i].z, k[1][i].z);
-      swap(k[0][i].w, k[1][i].w);
-    }
-    swap(e[0], e[1]);
+    for (int i = 0; i < F::kLoads; ++i)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const auto t = __builtin_amdgcn_permlane16_swap(k[0][i][w], k[1][i][w], false, false);
+        k[0][i][w] = t[0];
+        k[1][i][w] = t[1];
+      }
+    const auto t = __builtin_amdgcn_permlane16_swap(e[0], e[1], false, false);
+    e[0] = t[0];
+    e[1] = t[1];
   }
   template <class K>
   __device__ __forceinline__ void products_s(K&& ka, Logits& s) const {
@@ -923,7 +919,7 @@ __global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs 
   for (int j = 0; j < 4; ++j) vpos[j] = col * kRowBytes + ((F::chunk(quad, j) ^ ROWS::swizzle(col)) << 4);
 
   struct Raw {
-    uint4 k[2][F::kLoads], v[2][F::kLoads];
+    u32x4_t k[2][F::kLoads], v[2][F::kLoads];
     uint32_t ke[2], ve[2];
   };
   auto load = [&](int s, Raw& r) {

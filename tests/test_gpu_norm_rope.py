@@ -1,0 +1,178 @@
+"""The norm and rotation of queries and keys on the GPU against float64.
+
+Bounds, fixed before the first run: an output is rounded to bf16 once (2^-8 of its
+magnitude at most); before that each of the two products carries the norm's
+relative error (a sum of 128 squares, the reciprocal root, two products: below 2^-20),
+the angle's 2 pi 2^-26 and the sine's 2^-22.9, all below 2^-19 of |y1| + |y2|.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2606_05742_amd as adapld
+from test_gpu_kv4 import bf16, f64, i32
+
+pytestmark = pytest.mark.gpu
+
+
+def table(freqs):
+    """The table's entries as integers modulo 2^64."""
+    return [int(f) % (1 << 64) for f in freqs.cpu().tolist()]
+
+
+def check(q, k, freqs, base, offsets=None, counts=None, qw=None, kw=None, eps=1e-6, interleaved=False, **kw2):
+    B, T = q.shape[:2]
+    qo, ko = (torch.full(x.shape, 77.0, dtype=torch.bfloat16, device="cuda") for x in (q, k))
+    r = adapld.qk_norm_rope(q, k, freqs, i32(base), offsets=None if offsets is None else i32(offsets),
+                            counts=None if counts is None else i32(counts), q_weight=qw, k_weight=kw, eps=eps,
+                            interleaved=interleaved, q_out=qo, k_out=ko, **kw2)
+    torch.cuda.synchronize()
+    assert r[0] is qo and r[1] is ko
+    for x, o, w in ((q, qo, qw), (k, ko, kw)):
+        got, x = f64(o), f64(x)
+        for b in range(B):
+            n = T if counts is None else min(max(counts[b], 0), T)
+            p = [int(base[b]) + (int(offsets[b][u]) if offsets is not None else u) for u in range(n)]
+            want, size = oracle.qk_norm_rope(x[b, :n], None if w is None else f64(w), table(freqs), p, eps, interleaved)
+            assert (np.abs(got[b, :n] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -19 * size + 1e-38).all(), b
+            assert (got[b, n:] == 77).all()
+    return qo, ko
+
+
+def weight(rng):
+    return bf16(1 + 0.3 * rng.standard_normal(128)).cuda()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("rot", [0, 16, 48, 64, 80, 112, 128])
+@pytest.mark.parametrize("B, T, Hq, Hkv", [(1, 1, 1, 1), (2, 5, 7, 1), (3, 9, 4, 2), (1, 33, 16, 16)])
+def test_against_float64(B, T, Hq, Hkv, rot, interleaved):
+    rng = np.random.default_rng(rot + B)
+    x = bf16(rng.standard_normal((B, T, (Hq + 2 * Hkv) * 128)) * 2).cuda()
+    q, k = x[..., :Hq * 128].unflatten(-1, (Hq, 128)), x[..., Hq * 128:(Hq + Hkv) * 128].unflatten(-1, (Hkv, 128))
+    freqs = adapld.rope_frequencies(rot, 10000.0)
+    base = rng.integers(0, 9000, B).tolist()
+    check(q, k, freqs, base, qw=weight(rng), kw=weight(rng), interleaved=interleaved)
+    check(q, k, freqs, base, offsets=rng.integers(0, 20, (B, T)).tolist(), counts=[T - b for b in range(B)],
+          interleaved=interleaved)
+    check(q, k, freqs, base, counts=[-1, T + 5, 1][:B], qw=weight(rng), eps=0.0, interleaved=interleaved)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_far_positions(interleaved):
+    """Positions up to the ends of 32 bits and beyond, negative ones and frequencies
+    of any sign: the angle stays exact."""
+    rng = np.random.default_rng(3)
+    q, k = bf16(rng.standard_normal((5, 4, 4, 128))).cuda(), bf16(rng.standard_normal((5, 4, 2, 128))).cuda()
+    base = [2 ** 31 - 1, -2 ** 31, 1000003, -7, 0]
+    off = rng.integers(-2 ** 31, 2 ** 31, (5, 4))
+    off[0] = 2 ** 31 - 1
+    off[1] = -2 ** 31
+    check(q, k, adapld.rope_frequencies(128, 1e6), base, interleaved=interleaved)
+    check(q, k, adapld.rope_frequencies(128, 500.0), base, offsets=off.tolist(), interleaved=interleaved)
+    rad = np.concatenate((rng.uniform(-100, 100, 30), [0.0, math.pi], rng.uniform(-1, 1, 32))).tolist()
+    check(q, k, adapld.rope_frequencies(128, rad_per_token=rad), base, interleaved=interleaved)
+
+
+def test_frequencies_are_those_of_theta():
+    """The table against the formula: turns per position within 2^-52."""
+    for rot, theta in ((128, 10000.0), (64, 1e6), (16, 7.0)):
+        f = adapld.rope_frequencies(rot, theta).cpu().tolist()
+        want = [theta ** (-2 * i / rot) / (2 * math.pi) for i in range(rot // 2)]
+        assert max(abs(a / 2.0 ** 64 - b) for a, b in zip(f, want)) <= 2.0 ** -52
+
+
+def test_sizes_of_values():
+    """Rows of any size, rows of zeros; infinities and NaN stay in their row."""
+    rng = np.random.default_rng(9)
+    x = rng.standard_normal((1, 12, 2, 128))
+    for u, s in enumerate((2.0 ** -60, 2.0 ** -30, 1.0, 2.0 ** 30, 2.0 ** 55, 0.0)):
+        x[0, u] *= s
+    q, k = bf16(x).cuda(), bf16(x[:, :, :1]).cuda()
+    freqs = adapld.rope_frequencies(128)
+    check(q, k, freqs, [5], qw=weight(rng), kw=weight(rng))
+    check(q, k, freqs, [5])
+    good = adapld.qk_norm_rope(q, k, freqs, i32([5]), q_weight=weight(rng))[0]
+    bad = q.clone()
+    bad[0, 3, 1, 7] = math.nan
+    bad[0, 4, 0, 100] = math.inf
+    rng = np.random.default_rng(9)
+    rng.standard_normal((1, 12, 2, 128))
+    [weight(rng) for _ in range(2)]
+    o = adapld.qk_norm_rope(bad, k, freqs, i32([5]), q_weight=weight(rng))[0]
+    same = torch.ones((1, 12, 2), dtype=torch.bool)
+    same[0, 3, 1] = same[0, 4, 0] = False
+    assert torch.equal(o[same.cuda()], good[same.cuda()])
+    assert torch.isnan(o[0, 3, 1]).all() and torch.isnan(o[0, 4, 0, 100])
+    o = adapld.qk_norm_rope(bad, k, freqs, i32([5]))[0]
+    assert torch.isnan(o[0, 3, 1, [7, 71]]).all() and not torch.isnan(o[0, 3, 1, 8:71]).any()
+    assert not torch.isfinite(o[0, 4, 0, [36, 100]]).any()
+
+
+def test_strides_and_in_place():
+    rng = np.random.default_rng(13)
+    w = weight(rng), weight(rng)
+    freqs = adapld.rope_frequencies(64, 1e4)
+    whole = bf16(rng.standard_normal((3, 10, 24, 128))).cuda()
+    want = None
+    # every other token of sequences, sequences that share rows, a single head
+    for q, k in ((whole[:, ::2, :8], whole[:, ::2, 8:12]), (whole[1:2].expand(3, 10, 24, 128)[:, :, 3:7], whole[:, :, 20:21])):
+        check(q, k, freqs, [1, 2, 3], qw=w[0], kw=w[1])
+    q, k = whole[:, :, :8].contiguous(), whole[:, :, 8:12].contiguous()
+    want = adapld.qk_norm_rope(q, k, freqs, i32([4, 5, 6]), q_weight=w[0], k_weight=w[1])
+    got = adapld.qk_norm_rope(q, k, freqs, i32([4, 5, 6]), q_weight=w[0], k_weight=w[1], q_out=q, k_out=k)
+    assert got[0] is q and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_many_tokens():
+    """A prompt of a batch: every row, against float64 on the GPU."""
+    rng = np.random.default_rng(17)
+    B, T, Hq, Hkv = 3, 2011, 12, 3
+    q, k = torch.randn((B, T, Hq, 128), device="cuda").bfloat16(), torch.randn((B, T, Hkv, 128), device="cuda").bfloat16()
+    w = weight(rng), weight(rng)
+    freqs = adapld.rope_frequencies(128, 10000.0)
+    base = [0, 77, 123456]
+    out = adapld.qk_norm_rope(q, k, freqs, i32(base), q_weight=w[0], k_weight=w[1])
+    p = torch.tensor(base, device="cuda")[:, None] + torch.arange(T, device="cuda")
+    a = ((p[..., None] * freqs).double() * (2 * math.pi / 2.0 ** 64))[:, :, None]
+    for x, o, v in zip((q, k), out, w):
+        y = x.double()
+        y = y / torch.sqrt(y.square().mean(-1, keepdim=True) + 1e-6) * v.double()
+        y1, y2 = y[..., :64], y[..., 64:]
+        want = torch.cat((y1 * a.cos() - y2 * a.sin(), y2 * a.cos() + y1 * a.sin()), -1)
+        size = torch.cat((y1.abs() + y2.abs(),) * 2, -1)
+        assert ((o.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -19 * size).all()
+
+
+def test_other_stream_and_graph():
+    rng = np.random.default_rng(19)
+    q, k = bf16(rng.standard_normal((2, 6, 8, 128))).cuda(), bf16(rng.standard_normal((2, 6, 2, 128))).cuda()
+    freqs, base, counts, w = adapld.rope_frequencies(128), i32([100, 7]), i32([6, 4]), weight(rng)
+    qo, ko = torch.zeros_like(q), torch.zeros_like(k)
+    call = lambda **a: adapld.qk_norm_rope(q, k, freqs, base, counts=counts, q_weight=w, k_weight=w, q_out=qo, k_out=ko, **a)  # noqa: E731
+    call()
+    want = qo.clone(), ko.clone()
+    qo.zero_(), ko.zero_()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    call(stream=s)
+    s.synchronize()
+    assert torch.equal(qo, want[0]) and torch.equal(ko, want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s), torch.cuda.graph(graph, stream=s):
+        call()
+    torch.cuda.current_stream().wait_stream(s)
+    for rep in range(3):
+        base.add_(rep)
+        q.mul_(1.5)
+        call()
+        torch.cuda.synchronize()
+        want = qo.clone(), ko.clone()
+        qo.fill_(3.0)
+        qo[1, 4:] = want[0][1, 4:]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(qo, want[0]) and torch.equal(ko, want[1]), rep

@@ -34,13 +34,18 @@ VERIFY = [("q", P), *POOL, ("page_table", P), ("k_tree", P), ("v_tree", P), ("le
           ("tree_mask", P), ("B", 2), ("L_max", 100), ("T_max", 20), ("Hq", 8), ("Hkv", 2), ("D", 128),
           ("page_size", 16), ("n_pages", 20), ("max_pages", 8), ("scale", 0.1), ("out", P), ("lse", N), ("ws", P),
           ("ws_bytes", 1 << 30), ("stream", N)]
-CALLS = {"adapld_kv8_append": APPEND, "adapld_tree_verify_attn_kv8": VERIFY}
+ROPE = [("q", P), ("k", P), ("q_batch", 4096), ("q_token", 1024), ("k_batch", 4096), ("k_token", 1024), ("q_weight", P),
+        ("k_weight", P), ("freqs", P), ("base", P), ("offsets", N), ("counts", N), ("B", 2), ("T", 4), ("Hq", 8), ("Hkv", 2),
+        ("D", 128), ("rot_dim", 64), ("interleaved", 0), ("eps", 1e-6), ("q_out", P), ("k_out", P), ("stream", N)]
+CALLS = {"adapld_qk_norm_rope": ROPE, "adapld_kv8_append": APPEND, "adapld_tree_verify_attn_kv8": VERIFY}
 REQUIRED = {
+    "adapld_qk_norm_rope": ["q", "k", "freqs", "base", "q_out", "k_out"],
     "adapld_kv8_append": ["k_new", "v_new", "lens_old", "lens_new", "page_table", "k_codes", "k_scales", "v_codes",
                           "v_scales"],
     "adapld_tree_verify_attn_kv8": ["q", "k_codes", "k_scales", "v_codes", "v_scales", "page_table", "k_tree",
                                     "v_tree", "tree_mask", "lens", "node_count", "out"]}
-ALIGNED = {"adapld_kv8_append": ["k_new", "v_new", "k_codes", "v_codes"],
+ALIGNED = {"adapld_qk_norm_rope": ["q", "k", "q_weight", "k_weight", "q_out", "k_out"],
+           "adapld_kv8_append": ["k_new", "v_new", "k_codes", "v_codes"],
            "adapld_tree_verify_attn_kv8": ["q", "k_codes", "v_codes", "k_tree", "v_tree", "out"]}
 
 
@@ -62,9 +67,9 @@ def test_common_refusals(lib, call):
         assert f(*_args(names, **{p: N})) == NULL, p
     for p in ALIGNED[call]:
         assert f(*_args(names, **{p: ODD})) == INVALID, p
-    for size in (0, 8, 15, 24, 48, 512, -16):
-        assert not {"page_size"} & has or f(*_args(names, page_size=size)) == INVALID, size
     if "n_pages" in has:
+        for size in (0, 8, 15, 24, 48, 512, -16):
+            assert f(*_args(names, page_size=size)) == INVALID, size
         assert f(*_args(names, n_pages=0)) == INVALID
         assert f(*_args(names, max_pages=0)) == INVALID
         assert f(*_args(names, n_pages=MAX // 16 + 1)) == UNSUPPORTED
@@ -96,3 +101,13 @@ def test_verify_refusals(lib):
     assert f(*_args(VERIFY, ws_bytes=need - 1, **big)) == WS_SMALL
     assert f(*_args(VERIFY, ws=N, **big)) == NULL
     assert f(*_args(VERIFY, ws=ODD, **big)) == INVALID
+
+
+def test_norm_rope_refusals(lib):
+    f = lib.adapld_qk_norm_rope
+    for bad in (dict(T=0), dict(Hq=0), dict(rot_dim=-16), dict(rot_dim=8), dict(rot_dim=144), dict(interleaved=2),
+                dict(interleaved=-1), dict(eps=-1e-9), dict(eps=float("nan")), dict(eps=float("inf")), dict(q_batch=-8),
+                dict(q_token=1020), dict(k_batch=4), dict(k_token=-1024), dict(freqs=ctypes.c_void_p(0x10004))):
+        assert f(*_args(ROPE, **bad)) == INVALID, bad
+    assert f(*_args(ROPE, B=1 << 14, T=1 << 11)) == UNSUPPORTED
+    assert f(*_args(ROPE, B=MAX, T=MAX, Hq=MAX, Hkv=MAX)) == UNSUPPORTED
