@@ -108,7 +108,7 @@ int adapld_qk_norm_rope(const uint16_t* q, const uint16_t* k, int64_t q_batch, i
  * Errors: NULL_ARG; INVALID_ARG for B < 0, n_src, N, Hkv, n_pages, max_pages < 1,
  * a page_size other than the five, N > n_src without rows or misaligned pointers;
  * UNSUPPORTED for D != 128, n_pages * page_size or max_pages * page_size >
- * INT32_MAX, or more than 2^26 blocks of a kv head.
+ * INT32_MAX, or more than 2^26 - 4 blocks of a kv head.
  */
 int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_t* rows, const int32_t* lens_old,
                       const int32_t* lens_new, const int32_t* page_table, int B, int n_src, int N, int Hkv, int D,
@@ -130,6 +130,101 @@ int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const
                                 const int32_t* node_count, const uint64_t* tree_mask, int B, int L_max, int T_max,
                                 int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, float scale,
                                 uint16_t* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Eviction by accumulated attention weight.  A caller that bounds the cache keeps
+ * for every (sequence, kv head) the weight that each cached token has got from the
+ * rows so far and the token's position:
+ *   weights     fp32  [B, Hkv, stride]   finite, not negative
+ *   positions   int32 [B, Hkv, stride]
+ * entry j belongs to the row of that kv head at position j of the page table (its
+ * slot); after an eviction the kv heads of a sequence hold different tokens in the
+ * same slot, and a token's place is no longer its position (rotations take the
+ * position, see adapld_qk_norm_rope).  An iteration: append and attention as above,
+ * adapld_kv8_attn_weights for the rows that were kept, adapld_kv8_evict, and
+ * adapld_kv4_page_map from the old to the new lengths for the pages given back.
+ */
+
+/*
+ * adapld_kv8_attn_weights -- adds the attention weight that new rows give.
+ *
+ * Sequence b holds lens_new[b] tokens (clamped on the device to [0, L_max]), the last
+ * n = min(lens_new - lens_old, N) (0 if negative) of them those of the new rows: row
+ * i < n has query u = rows[b, i] (i itself if `rows` is NULL) and sees the slots j <=
+ * lens_old[b] + i.  For every slot j < lens_old[b] + n and kv head g:
+ *   weights_out[b, g, j] = (weights[b, g, j] if j < lens_old[b], else 0)
+ *     + sum over the rows i that see j, and over the Hq / Hkv heads h of g, of
+ *       exp(scale * q[b, u, h] . k[b, g, j] - lse[b, h, u])
+ * and positions[b, g, lens_old[b] + i] = first_position[b] + i.  Other entries are
+ * left as they are.  A row whose u is outside [0, T_max) and a head whose lse is -inf
+ * (a row without any key) give nothing.
+ *
+ *   q           bf16 [B, T_max, Hq, D]  as the attention took it
+ *   lse         fp32 [B, Hq, T_max]     as the attention wrote it
+ *   rows        int32 [B, N] or NULL    e.g. accept_nodes (NULL: N <= T_max)
+ *   k_codes, k_scales, page_table       the cache, with the new rows' keys
+ *   lens_old, lens_new, first_position  int32 [B]
+ *   L_max       an upper bound of the lengths, at most max_pages * page_size and
+ *               at most stride
+ *   weights_out fp32 [B, Hkv, stride] (out); weights itself, or no overlap
+ * Sums are fp32, in an order that the sizes fix.  q, the keys and scale * q.k *
+ * log2(e) are finite, lse finite or -inf.
+ *
+ * Errors: NULL_ARG; INVALID_ARG for B < 0, Hq % Hkv != 0, non-positive sizes, N > T_max
+ * without rows, L_max > max_pages * page_size or stride, a page_size other than the
+ * five, scale as in the attention, or misaligned pointers; UNSUPPORTED for D != 128,
+ * T_max or N > ADAPLD_MAX_TREE_NODES, n_pages * page_size or max_pages * page_size >
+ * INT32_MAX, L_max > 2^30, or B * Hkv * (L_max / 128 + 1) > 2^24 - 1.
+ */
+int adapld_kv8_attn_weights(const uint16_t* q, const float* lse, const int32_t* rows, const uint8_t* k_codes,
+                            const uint8_t* k_scales, const int32_t* page_table, const int32_t* lens_old,
+                            const int32_t* lens_new, const int32_t* first_position, int B, int L_max, int T_max,
+                            int N, int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, int stride,
+                            float scale, const float* weights, float* weights_out, int32_t* positions,
+                            hipStream_t stream);
+
+/*
+ * adapld_kv8_evict -- keeps `budget` tokens of every kv head.
+ *
+ * For each sequence b with L = lens[b] tokens (clamped on the device to [0, L_max])
+ * and kv head: where L > budget, the tokens are ranked, those with positions[j] >=
+ * next_position[b] - recent (in 64 bits) before the others, then by weight, largest
+ * first, then by slot, lowest first; the first `budget` stay.  Those of them in
+ * slots >= budget move into the slots < budget that the others leave, both in
+ * ascending order of slots, with their rows of K and V, weight and position; the
+ * rest stay where they are.  A block of the cache that rows move into takes the
+ * largest scale of the rows that it then holds, and rows of smaller scales are
+ * rounded again to it (exactly, but for values below 2^-6 of the scale).
+ * lens_out[b] = min(L, budget), and weights_out and positions_out hold the entries
+ * of the slots below that; other entries are left as they are, and so are the
+ * cache's rows at or behind it.  (Made again with the same weights, positions and
+ * lens, the call leaves the same cache.)
+ *
+ *   budget      a multiple of ADAPLD_KV8_BLOCK, >= ADAPLD_KV8_BLOCK
+ *   recent      >= 0
+ *   weights_out, positions_out  weights and positions themselves, or no overlap
+ *   lens_out    int32 [B] (out); lens itself, or no overlap
+ *   L_max       an upper bound of the lengths, at most max_pages * page_size and
+ *               at most stride
+ *   ws          adapld_kv8_evict_workspace_bytes(B, Hkv, L_max, budget) bytes (may
+ *               be NULL if 0), 16-byte aligned
+ * The pages of slots below min(L, budget) are in the table of no other sequence.  A
+ * page id outside the pool is read as the nearest page, and never written.
+ * Weights are compared as numbers, -0 before 0 as the smaller, a NaN by its sign as
+ * the largest or the smallest.
+ *
+ * Errors: NULL_ARG; INVALID_ARG for B < 0, non-positive sizes, a budget as above,
+ * recent < 0, L_max > max_pages * page_size or stride, a page_size other than the
+ * five, or misaligned pointers; UNSUPPORTED for D != 128, n_pages * page_size or
+ * max_pages * page_size > INT32_MAX, L_max > 2^30, B * Hkv > 2^22 - 1, or (where
+ * L_max > budget) more than 2^26 - 4 blocks to keep of a kv head; WORKSPACE_TOO_SMALL.
+ */
+size_t adapld_kv8_evict_workspace_bytes(int B, int Hkv, int L_max, int budget);
+int adapld_kv8_evict(const float* weights, const int32_t* positions, const int32_t* lens,
+                     const int32_t* next_position, const int32_t* page_table, int B, int L_max, int budget, int recent,
+                     int Hkv, int D, int page_size, int n_pages, int max_pages, int stride, uint8_t* k_codes,
+                     uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, float* weights_out,
+                     int32_t* positions_out, int32_t* lens_out, void* ws, size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

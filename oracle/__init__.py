@@ -8,4 +8,4 @@ from .adapld_oracle import (  # noqa: F401
     semantic_topk, embedding_fallback, build_draft_tree, build_draft_tree_paper, tree_verify_attn, accept_greedy, compact_kv, step,
 )
 from .kv4_oracle import kv4_pack, kv4_page_map, kv4_quantise, kv4_values, kv4_verify  # noqa: F401
-from .kv8_oracle import kv8_append, kv8_codes, kv8_exponent, kv8_rows, kv8_values, qk_norm_rope  # noqa: F401
+from .kv8_oracle import kv8_append, kv8_attn_weights, kv8_codes, kv8_evict, kv8_exponent, kv8_rows, kv8_values, qk_norm_rope  # noqa: F401

@@ -105,3 +105,71 @@ def qk_norm_rope(x, weight, freqs, positions, eps, interleaved):
         out[..., hi] = y2 * np.cos(a) + y1 * np.sin(a)
         size[..., lo] = size[..., hi] = np.abs(y1) + np.abs(y2)
     return out, size
+
+
+def kv8_attn_weights(q, lse, keys, lens_old, lens_new, first_position, weights, positions, rows=None, N=None, scale=None):
+    """q float64 [B, T, Hq, D], lse [B, Hq, T], keys a list of float64 [Hkv, L, D]
+    (the values of each sequence's slots); weights float64 and positions int
+    [B, Hkv, stride]: (weights, positions, reach) after the rows, reach the largest
+    sum |q||k| * scale of each kv head, which bounds the rounding of a computation
+    in fewer bits."""
+    B, T, Hq, D = q.shape
+    Hkv = weights.shape[1]
+    G = Hq // Hkv
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    N = (T if rows is None else len(rows[0])) if N is None else N
+    w, p, reach = np.array(weights, np.float64), np.array(positions), np.zeros((B, Hkv))
+    for b in range(B):
+        old = int(lens_old[b])
+        n = min(max(int(lens_new[b]) - old, 0), N)
+        w[b, :, old:old + n] = 0.0
+        p[b, :, old:old + n] = int(first_position[b]) + np.arange(n)
+        for i in range(n):
+            u = i if rows is None else int(rows[b][i])
+            if not 0 <= u < T:
+                continue
+            for h in range(Hq):
+                if lse[b, h, u] == -math.inf:
+                    continue
+                k = keys[b][h // G, :old + i + 1]
+                w[b, h // G, :old + i + 1] += np.exp(k @ q[b, u, h] * scale - lse[b, h, u])
+                reach[b, h // G] = max(reach[b, h // G], (np.abs(k) @ np.abs(q[b, u, h])).max() * scale)
+    return w, p, reach
+
+
+def kv8_evict(weights, positions, lens, next_position, budget, recent, table, page, cache):
+    """One kv head after another; `cache` (the arrays k_codes, k_scales, v_codes,
+    v_scales) is changed in place.  Returns (weights, positions, lens) of the
+    tokens that stay, a list for each sequence and kv head, and the lengths."""
+    B, Hkv = weights.shape[:2]
+    n_pages = cache[0].shape[0]
+    wo, po, lo = [], [], [min(max(int(n), 0), budget) for n in lens]
+    for b in range(B):
+        L, since = max(int(lens[b]), 0), int(next_position[b]) - recent
+        for g in range(Hkv):
+            w, p = weights[b, g, :L], positions[b, g, :L]
+            src = list(range(min(L, budget)))
+            if L > budget:
+                # -0 is smaller than 0
+                rank = sorted(range(L), key=lambda j: (int(p[j]) < since, -float(w[j]),
+                                                       bool(np.signbit(w[j])), j))
+                kept = set(rank[:budget])
+                free = [j for j in range(budget) if j not in kept]
+                for to, j in zip(free, sorted(j for j in kept if j >= budget)):
+                    src[to] = j
+                at = lambda j: (int(table[b][j // page]), g, j % page)  # noqa: E731
+                near = lambda a: (min(max(a[0], 0), n_pages - 1), a[1], a[2])  # noqa: E731
+                for codes, scales in ((cache[0], cache[1]), (cache[2], cache[3])):
+                    for start in sorted({j // BLOCK * BLOCK for j in free}):
+                        if not 0 <= at(start)[0] < n_pages:
+                            continue
+                        places = [near(at(src[j])) for j in range(start, start + BLOCK)]
+                        es = [int(scales[x, g, y // BLOCK]) for x, _, y in places]
+                        e = max(es)
+                        got = [codes[x] if f == e else kv8_codes(kv8_values(codes[x], f), e) for x, f in zip(places, es)]
+                        for i, c in enumerate(got):
+                            codes[at(start + i)] = c
+                        scales[at(start)[0], g, at(start)[2] // BLOCK] = e
+            wo.append([w[j] for j in src])
+            po.append([int(p[j]) for j in src])
+    return wo, po, lo

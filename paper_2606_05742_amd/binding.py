@@ -100,6 +100,11 @@ SIGNATURES = {
     "adapld_qk_norm_rope": (ctypes.c_int, [ctypes.c_void_p] * 2 + [ctypes.c_int64] * 4 + [ctypes.c_void_p] * 6
                             + [ctypes.c_int] * 7 + [ctypes.c_float] + [ctypes.c_void_p] * 3),
     "adapld_kv8_append": (ctypes.c_int, [ctypes.c_void_p] * 6 + [ctypes.c_int] * 8 + [ctypes.c_void_p] * 5),
+    "adapld_kv8_attn_weights": (ctypes.c_int, [ctypes.c_void_p] * 9 + [ctypes.c_int] * 11 + [ctypes.c_float]
+                                + [ctypes.c_void_p] * 4),
+    "adapld_kv8_evict_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int] * 4),
+    "adapld_kv8_evict": (ctypes.c_int, [ctypes.c_void_p] * 5 + [ctypes.c_int] * 10 + [ctypes.c_void_p] * 8
+                         + [ctypes.c_size_t, ctypes.c_void_p]),
     "adapld_tree_verify_attn_kv8": (ctypes.c_int, [ctypes.c_void_p] * 11 + [ctypes.c_int] * 9 + [ctypes.c_float]
                                     + [ctypes.c_void_p] * 3 + [ctypes.c_size_t, ctypes.c_void_p]),
 }
@@ -859,6 +864,85 @@ def kv8_append(cache: Kv8Cache, k_new, v_new, lens_old, lens_new, *, rows=None, 
         Hkv, D, cache.page_size, n_pages, max_pages, *pool, _stream_on(stream, dev))
     if st:
         _check(st, "adapld_kv8_append")
+
+
+def kv8_attn_weights(cache: Kv8Cache, q, lse, lens_old, lens_new, first_position, weights, positions, *, rows=None,
+                     N=None, L_max=None, scale=None, weights_out=None, stream=None):
+    """Adds to the weight of each cached token (fp32 [B, Hkv, stride]) what it
+    gets from the rows that took sequence b from lens_old[b] to lens_new[b]
+    tokens: the i-th is row rows[b, i] (row i without rows) of q (bf16 [B, T_max,
+    Hq, D]) and lse, as the attention took and wrote them.  The new tokens'
+    positions (int32, like weights) are first_position[b] + i.  N bounds the rows
+    of a sequence (default: the width of rows, or T_max), L_max the lengths
+    (default: what table and weights hold).  Returns (weights_out, positions);
+    weights_out is weights if not given."""
+    dev = _device_of(q, "q")
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev, 8)
+    _, table, B, max_pages = cache._marshal_pages(dev)
+    shape, wshape = q.shape, weights.shape
+    if len(shape) != 4 or shape[0] != B or shape[3] != D:
+        raise AdapldError(-2, f"q has shape {tuple(shape)}, expected ({B}, T_max, Hq, {D})")
+    if len(wshape) != 3 or wshape[0] != B or wshape[1] != Hkv:
+        raise AdapldError(-2, f"weights has shape {tuple(wshape)}, expected ({B}, {Hkv}, stride)")
+    T_max, Hq = shape[1], shape[2]
+    if N is None:
+        N = T_max if rows is None else rows.shape[1]
+    if L_max is None:
+        L_max = min(max_pages * cache.page_size, wshape[2])
+    weights_out = weights if weights_out is None else weights_out
+    if stream is not None:
+        _on(stream, dev)
+    st = load_library().adapld_kv8_attn_weights(
+        _dptr(q, "q", _BF16_DTYPES, None, dev), _dptr(lse, "lse", _F32, (B, Hq, T_max), dev),
+        None if rows is None else _dptr(rows, "rows", _I32, (B, N), dev), pool[0], pool[1], table,
+        _dptr(lens_old, "lens_old", _I32, (B,), dev), _dptr(lens_new, "lens_new", _I32, (B,), dev),
+        _dptr(first_position, "first_position", _I32, (B,), dev), B, L_max, T_max, N, Hq, Hkv, D, cache.page_size,
+        n_pages, max_pages, wshape[2], 1.0 / math.sqrt(D) if scale is None else scale,
+        _dptr(weights, "weights", _F32, None, dev), _dptr(weights_out, "weights_out", _F32, wshape, dev),
+        _dptr(positions, "positions", _I32, wshape, dev), _stream_on(stream, dev))
+    if st:
+        _check(st, "adapld_kv8_attn_weights")
+    return weights_out, positions
+
+
+def kv8_evict_workspace_bytes(B, Hkv, L_max, budget) -> int:
+    return int(load_library().adapld_kv8_evict_workspace_bytes(B, Hkv, L_max, budget))
+
+
+def kv8_evict(cache: Kv8Cache, weights, positions, lens, next_position, budget, recent=0, *, L_max=None,
+              weights_out=None, positions_out=None, lens_out=None, ws=None, stream=None):
+    """Keeps `budget` tokens of every kv head: those at positions of the last
+    `recent` before next_position[b] and then those with the most weight; the
+    kept rows behind the budget move into the slots that others leave.  Returns
+    (weights_out, positions_out, lens_out): weights and positions in place and a
+    new lens_out if not given.  page_map from lens to lens_out gives the pages
+    back."""
+    dev = _device_of(weights, "weights")
+    _, pool, n_pages, Hkv, D = cache._marshal_pool(dev, 8)
+    _, table, B, max_pages = cache._marshal_pages(dev)
+    shape = weights.shape
+    if len(shape) != 3 or shape[0] != B or shape[1] != Hkv:
+        raise AdapldError(-2, f"weights has shape {tuple(shape)}, expected ({B}, {Hkv}, stride)")
+    if L_max is None:
+        L_max = min(max_pages * cache.page_size, shape[2])
+    if lens_out is None or ws is None or stream is not None:
+        with _on(stream, dev):
+            lens_out = _i32(B, weights.device) if lens_out is None else lens_out
+            if ws is None:
+                need = kv8_evict_workspace_bytes(B, Hkv, L_max, budget)
+                ws = torch.empty(max(need, 16), dtype=torch.uint8, device=weights.device)
+    weights_out = weights if weights_out is None else weights_out
+    positions_out = positions if positions_out is None else positions_out
+    st = load_library().adapld_kv8_evict(
+        _dptr(weights, "weights", _F32, None, dev), _dptr(positions, "positions", _I32, shape, dev),
+        _dptr(lens, "lens", _I32, (B,), dev), _dptr(next_position, "next_position", _I32, (B,), dev), table, B, L_max,
+        budget, recent, Hkv, D, cache.page_size, n_pages, max_pages, shape[2], *pool,
+        _dptr(weights_out, "weights_out", _F32, shape, dev), _dptr(positions_out, "positions_out", _I32, shape, dev),
+        _dptr(lens_out, "lens_out", _I32, (B,), dev), _dptr(ws, "ws", _U8, None, dev), ws.numel(),
+        _stream_on(stream, dev))
+    if st:
+        _check(st, "adapld_kv8_evict")
+    return weights_out, positions_out, lens_out
 
 
 @dataclass

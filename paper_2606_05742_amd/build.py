@@ -21,7 +21,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libadapld.so")
 
 SOURCES = ["lexical.hip", "semantic.hip", "tree.hip", "paper_tree.hip", "verify.hip", "accept.hip", "embed.hip", "ngram.hip", "noalloc.hip", "kv4.hip",
-           "kv4_verify.hip", "kv8.hip", "kv8_verify.hip", "norm_rope.hip", "abi.cpp"]
+           "kv4_verify.hip", "kv8.hip", "kv8_verify.hip", "norm_rope.hip", "kv8_weights.hip", "kv8_evict.hip", "abi.cpp"]
 ARCH = "gfx950"
 
 # -packed-fp32-ops keeps the compiler from emitting packed fp32 VALU ops.

@@ -33,7 +33,10 @@ size_t step_sem_part(int B, int L_stride, int k) { return (semantic_ws(B, L_stri
 constexpr int64_t kKv4MaxRows = (1 << 28) - 16;
 constexpr int64_t kKv4MaxOutRows = (1 << 27) - 8;
 constexpr int64_t kKv4MaxGroups = (1 << 23) - 8;
+// 64 threads a block, 256 a workgroup of the weights, 1024 a kv head of the eviction.
 constexpr int64_t kKv8MaxBlocks = (1 << 26) - 4;
+constexpr int64_t kKv8MaxWeightGroups = (1 << 24) - 1;
+constexpr int64_t kKv8MaxPairs = (1 << 22) - 1;
 
 // The embedding fallback's own part (16-byte aligned), then the scan's lists.
 size_t embed_head_ws(int B, int L_stride) { return (adapld::embed_ws_bytes(B, L_stride) + 15) / 16 * 16; }
@@ -627,6 +630,66 @@ int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_
   return hip_status(adapld::launch_kv8_append(k_new, v_new, rows, lens_old, lens_new, page_table, B, n_src, N, Hkv,
                                               page_size, n_pages, max_pages, k_codes, k_scales, v_codes, v_scales,
                                               stream));
+}
+
+int adapld_kv8_attn_weights(const uint16_t* q, const float* lse, const int32_t* rows, const uint8_t* k_codes,
+                            const uint8_t* k_scales, const int32_t* page_table, const int32_t* lens_old,
+                            const int32_t* lens_new, const int32_t* first_position, int B, int L_max, int T_max,
+                            int N, int Hq, int Hkv, int D, int page_size, int n_pages, int max_pages, int stride,
+                            float scale, const float* weights, float* weights_out, int32_t* positions,
+                            hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (!q || !lse || !k_codes || !k_scales || !page_table || !lens_old || !lens_new || !first_position || !weights ||
+      !weights_out || !positions)
+    return ADAPLD_ERR_NULL_ARG;
+  if (L_max < 1 || T_max < 1 || N < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_pages < 1 || L_max > stride ||
+      (!rows && N > T_max) || !(scale > 0.f) || !std::isfinite(scale * 1.4426950408889634f))
+    return ADAPLD_ERR_INVALID_ARG;
+  if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
+  if (D != ADAPLD_HEAD_DIM || T_max > ADAPLD_MAX_TREE_NODES || N > ADAPLD_MAX_TREE_NODES ||
+      (int64_t)max_pages * page_size > INT32_MAX || L_max > (1 << 30) ||
+      (double)B * Hkv * (L_max / 128 + 1) > kKv8MaxWeightGroups)
+    return ADAPLD_ERR_UNSUPPORTED;
+  if (L_max > max_pages * page_size || misaligned16(q) || misaligned16(k_codes)) return ADAPLD_ERR_INVALID_ARG;
+  const adapld::AttnWeightsCall c{q, lse, rows, k_codes, k_scales, page_table, lens_old, lens_new, first_position,
+                                  B, L_max, T_max, N, Hq, Hkv, page_size, n_pages, max_pages, stride, scale, weights,
+                                  weights_out, positions};
+  return hip_status(adapld::launch_kv8_attn_weights(c, stream));
+}
+
+size_t adapld_kv8_evict_workspace_bytes(int B, int Hkv, int L_max, int budget) {
+  if (B < 1 || Hkv < 1 || L_max < 1 || budget < ADAPLD_KV8_BLOCK || (double)B * Hkv > kKv8MaxPairs) return 0;
+  return adapld::evict_ws_bytes(B, Hkv, L_max, budget);
+}
+
+int adapld_kv8_evict(const float* weights, const int32_t* positions, const int32_t* lens,
+                     const int32_t* next_position, const int32_t* page_table, int B, int L_max, int budget, int recent,
+                     int Hkv, int D, int page_size, int n_pages, int max_pages, int stride, uint8_t* k_codes,
+                     uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, float* weights_out,
+                     int32_t* positions_out, int32_t* lens_out, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (B < 0) return ADAPLD_ERR_INVALID_ARG;
+  if (B == 0) return ADAPLD_OK;
+  if (!weights || !positions || !lens || !next_position || !page_table || !weights_out || !positions_out || !lens_out)
+    return ADAPLD_ERR_NULL_ARG;
+  if (const int st = check_kv8_arrays(k_codes, k_scales, v_codes, v_scales); st != ADAPLD_OK) return st;
+  if (L_max < 1 || Hkv < 1 || max_pages < 1 || L_max > stride || budget < ADAPLD_KV8_BLOCK ||
+      budget % ADAPLD_KV8_BLOCK != 0 || recent < 0)
+    return ADAPLD_ERR_INVALID_ARG;
+  if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
+  if (D != ADAPLD_HEAD_DIM || (int64_t)max_pages * page_size > INT32_MAX || L_max > (1 << 30) ||
+      (double)B * Hkv > kKv8MaxPairs ||
+      (L_max > budget && (double)B * Hkv * (budget / ADAPLD_KV8_BLOCK) > kKv8MaxBlocks))
+    return ADAPLD_ERR_UNSUPPORTED;
+  if (L_max > max_pages * page_size) return ADAPLD_ERR_INVALID_ARG;
+  const size_t need = adapld::evict_ws_bytes(B, Hkv, L_max, budget);
+  if (need > 0 && !ws) return ADAPLD_ERR_NULL_ARG;
+  if (ws_bytes < need) return ADAPLD_ERR_WORKSPACE_TOO_SMALL;
+  if (need > 0 && misaligned16(ws)) return ADAPLD_ERR_INVALID_ARG;
+  const adapld::EvictCall c{weights, positions, lens, next_position, page_table, B, L_max, budget, recent, Hkv,
+                            page_size, n_pages, max_pages, stride, {k_codes, v_codes}, {k_scales, v_scales},
+                            weights_out, positions_out, lens_out, ws};
+  return hip_status(adapld::launch_kv8_evict(c, stream));
 }
 
 int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,

@@ -228,4 +228,39 @@ VerifyPagedPlan plan_verify_kv8(int B, int L_max, int T_max, int Hq, int Hkv);
 size_t verify_kv8_ws_bytes(const VerifyPagedPlan& p, int B, int Hkv);
 hipError_t launch_tree_verify_attn_kv8(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipStream_t stream);
 
+struct AttnWeightsCall {
+  const uint16_t* q;
+  const float* lse;
+  const int32_t* rows;
+  const uint8_t* k_codes;
+  const uint8_t* k_scales;
+  const int32_t* page_table;
+  const int32_t* lens_old;
+  const int32_t* lens_new;
+  const int32_t* first_position;
+  int B, L_max, T_max, N, Hq, Hkv, page_size, n_pages, max_pages, stride;
+  float scale;
+  const float* weights;
+  float* weights_out;
+  int32_t* positions;
+};
+hipError_t launch_kv8_attn_weights(const AttnWeightsCall& c, hipStream_t stream);
+
+struct EvictCall {
+  const float* weights;
+  const int32_t* positions;
+  const int32_t* lens;
+  const int32_t* next_position;
+  const int32_t* page_table;
+  int B, L_max, budget, recent, Hkv, page_size, n_pages, max_pages, stride;
+  uint8_t* codes[2];    // K and V
+  uint8_t* scales[2];
+  float* weights_out;
+  int32_t* positions_out;
+  int32_t* lens_out;
+  void* ws;
+};
+size_t evict_ws_bytes(int B, int Hkv, int L_max, int budget);
+hipError_t launch_kv8_evict(const EvictCall& c, hipStream_t stream);
+
 }  // namespace adapld

@@ -37,14 +37,28 @@ VERIFY = [("q", P), *POOL, ("page_table", P), ("k_tree", P), ("v_tree", P), ("le
 ROPE = [("q", P), ("k", P), ("q_batch", 4096), ("q_token", 1024), ("k_batch", 4096), ("k_token", 1024), ("q_weight", P),
         ("k_weight", P), ("freqs", P), ("base", P), ("offsets", N), ("counts", N), ("B", 2), ("T", 4), ("Hq", 8), ("Hkv", 2),
         ("D", 128), ("rot_dim", 64), ("interleaved", 0), ("eps", 1e-6), ("q_out", P), ("k_out", P), ("stream", N)]
-CALLS = {"adapld_qk_norm_rope": ROPE, "adapld_kv8_append": APPEND, "adapld_tree_verify_attn_kv8": VERIFY}
+WEIGHTS = [("q", P), ("lse", P), ("rows", N), ("k_codes", P), ("k_scales", P), ("page_table", P), ("lens_old", P),
+           ("lens_new", P), ("first_position", P), ("B", 2), ("L_max", 100), ("T_max", 20), ("N", 20), ("Hq", 8),
+           ("Hkv", 2), ("D", 128), ("page_size", 16), ("n_pages", 20), ("max_pages", 8), ("stride", 128), ("scale", 0.1),
+           ("weights", P), ("weights_out", P), ("positions", P), ("stream", N)]
+EVICT = [("weights", P), ("positions", P), ("lens", P), ("next_position", P), ("page_table", P), ("B", 2), ("L_max", 100),
+         ("budget", 64), ("recent", 8), ("Hkv", 2), ("D", 128), ("page_size", 16), ("n_pages", 20), ("max_pages", 8),
+         ("stride", 128), *POOL, ("weights_out", P), ("positions_out", P), ("lens_out", P), ("ws", P),
+         ("ws_bytes", 1 << 30), ("stream", N)]
+CALLS = {"adapld_qk_norm_rope": ROPE, "adapld_kv8_attn_weights": WEIGHTS, "adapld_kv8_evict": EVICT,
+         "adapld_kv8_append": APPEND, "adapld_tree_verify_attn_kv8": VERIFY}
 REQUIRED = {
     "adapld_qk_norm_rope": ["q", "k", "freqs", "base", "q_out", "k_out"],
+    "adapld_kv8_attn_weights": ["q", "lse", "k_codes", "k_scales", "page_table", "lens_old", "lens_new",
+                                "first_position", "weights", "weights_out", "positions"],
+    "adapld_kv8_evict": ["weights", "positions", "lens", "next_position", "page_table", "k_codes", "k_scales",
+                         "v_codes", "v_scales", "weights_out", "positions_out", "lens_out"],
     "adapld_kv8_append": ["k_new", "v_new", "lens_old", "lens_new", "page_table", "k_codes", "k_scales", "v_codes",
                           "v_scales"],
     "adapld_tree_verify_attn_kv8": ["q", "k_codes", "k_scales", "v_codes", "v_scales", "page_table", "k_tree",
                                     "v_tree", "tree_mask", "lens", "node_count", "out"]}
-ALIGNED = {"adapld_qk_norm_rope": ["q", "k", "q_weight", "k_weight", "q_out", "k_out"],
+ALIGNED = {"adapld_kv8_attn_weights": ["q", "k_codes"], "adapld_kv8_evict": ["k_codes", "v_codes", "ws"],
+           "adapld_qk_norm_rope": ["q", "k", "q_weight", "k_weight", "q_out", "k_out"],
            "adapld_kv8_append": ["k_new", "v_new", "k_codes", "v_codes"],
            "adapld_tree_verify_attn_kv8": ["q", "k_codes", "v_codes", "k_tree", "v_tree", "out"]}
 
@@ -111,3 +125,25 @@ def test_norm_rope_refusals(lib):
         assert f(*_args(ROPE, **bad)) == INVALID, bad
     assert f(*_args(ROPE, B=1 << 14, T=1 << 11)) == UNSUPPORTED
     assert f(*_args(ROPE, B=MAX, T=MAX, Hq=MAX, Hkv=MAX)) == UNSUPPORTED
+
+
+def test_attn_weights_refusals(lib):
+    f = lib.adapld_kv8_attn_weights
+    for bad in (dict(L_max=0), dict(T_max=0), dict(N=0), dict(N=21), dict(Hq=0), dict(Hq=7), dict(L_max=129, stride=1000),
+                dict(stride=99), dict(scale=0.0), dict(scale=float("nan")), dict(scale=3.4e38)):
+        assert f(*_args(WEIGHTS, **bad)) == INVALID, bad
+    assert f(*_args(WEIGHTS, T_max=257)) == UNSUPPORTED
+    assert f(*_args(WEIGHTS, N=257, rows=P)) == UNSUPPORTED
+    assert f(*_args(WEIGHTS, B=1 << 16, Hkv=8, L_max=1 << 13, max_pages=1 << 9, stride=1 << 13)) == UNSUPPORTED
+
+
+def test_evict_refusals(lib):
+    f, need = lib.adapld_kv8_evict, lib.adapld_kv8_evict_workspace_bytes
+    for bad in (dict(L_max=0), dict(L_max=129, stride=1000), dict(stride=99), dict(budget=0), dict(budget=-16), dict(budget=24),
+                dict(recent=-1)):
+        assert f(*_args(EVICT, **bad)) == INVALID, bad
+    assert need(2, 2, 100, 64) == 4 * (64 + 36 + 1) * 4 and need(2, 2, 64, 64) == 0 and need(0, 2, 100, 64) == 0
+    assert f(*_args(EVICT, ws_bytes=need(2, 2, 100, 64) - 1)) == WS_SMALL
+    assert f(*_args(EVICT, ws=N)) == NULL
+    assert f(*_args(EVICT, B=1 << 22, Hkv=1)) == UNSUPPORTED
+    assert f(*_args(EVICT, B=1 << 16, Hkv=8, L_max=4096, budget=2048, max_pages=256, stride=4096)) == UNSUPPORTED

@@ -17,10 +17,12 @@ def cache_of(bits=8, n_pages=4, page_size=32, Hkv=2, B=1, max_pages=3):
 
 def test_caches_of_the_other_width_are_refused(lib):  # noqa: F811
     q, kv, n = bf16(1, 2, 4, 128), bf16(1, 3, 2, 128), i32([1])
-    four, eight = cache_of(4), cache_of(8)
+    four, eight, w = cache_of(4), cache_of(8), torch.zeros((1, 2, 96))
     for call in (lambda: adapld.kv8_append(four, kv, kv, n, n), lambda: adapld.tree_verify_attn_kv8(q, four, n, n),
                  lambda: adapld.kv4_append(eight, kv, kv, i32([[0, 1, 2]])), lambda: adapld.kv4_gather(eight, i32([[0]])),
-                 lambda: adapld.tree_verify_attn_kv4(q, eight, n, n)):
+                 lambda: adapld.tree_verify_attn_kv4(q, eight, n, n),
+                 lambda: adapld.kv8_attn_weights(four, q, w, n, n, n, w, i32([[[0]]])),
+                 lambda: adapld.kv8_evict(four, w, i32([[[0]]]), n, n, 16)):
         with pytest.raises(AdapldError, match="bits a value"):
             call()
     assert not lib.calls
@@ -73,3 +75,27 @@ def test_frequencies():
                 dict(rot_dim=2, rad_per_token=[math.inf])):
         with pytest.raises(AdapldError):
             adapld.rope_frequencies(**bad, device="cpu")
+
+
+def test_weights_and_eviction_pass_the_sizes(lib):  # noqa: F811
+    c, n = cache_of(), i32([4])
+    w, p = torch.zeros((1, 2, 80)), torch.zeros((1, 2, 80), dtype=torch.int32)
+    q, lse = bf16(1, 5, 4, 128), torch.zeros((1, 4, 5))
+    assert adapld.kv8_attn_weights(c, q, lse, n, n, n, w, p)[0] is w
+    adapld.kv8_attn_weights(c, q, lse, n, n, n, w, p, rows=i32([[1, 2]]), L_max=70, weights_out=w.clone())
+    assert [a[9:20] for _, a in lib.calls] == [(1, 80, 5, 5, 4, 2, 128, 32, 4, 3, 80), (1, 70, 5, 2, 4, 2, 128, 32, 4, 3, 80)]
+    lib.calls.clear()
+    wo, po, lo = adapld.kv8_evict(c, w, p, n, n, 32, 7, ws=torch.zeros(4096, dtype=torch.uint8))
+    assert wo is w and po is p and lo.shape == (1,)
+    assert lib.calls[0][1][5:15] == (1, 80, 32, 7, 2, 128, 32, 4, 3, 80)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    for bad in (dict(weights=w[:, :1]), dict(weights=w.double()), dict(positions=p[..., :79]), dict(lens=i32([1, 2])),
+                dict(positions_out=p[..., :79])):
+        with pytest.raises(AdapldError):
+            adapld.kv8_evict(**(dict(cache=c, weights=w, positions=p, lens=n, next_position=n, budget=32, ws=ws) | bad))
+    for bad in (dict(q=bf16(1, 5, 4, 64)), dict(lse=lse[..., :4]), dict(weights=w[0]), dict(rows=i32([[1]]), N=2),
+                dict(positions=p.long())):
+        with pytest.raises(AdapldError):
+            adapld.kv8_attn_weights(**(dict(cache=c, q=q, lse=lse, lens_old=n, lens_new=n, first_position=n, weights=w,
+                                            positions=p) | bad))
+    assert len(lib.calls) == 1
