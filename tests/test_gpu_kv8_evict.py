@@ -113,6 +113,27 @@ def test_weights_with_large_logits():
     check_weights([400, 20], [403, 23], 4, 1, 3, 16, wide=8.0)
 
 
+@pytest.mark.parametrize("T, Hq, Hkv", [(5, 4, 2), (20, 8, 1), (70, 4, 2)])
+def test_weights_ignore_what_is_no_row(T, Hq, Hkv):
+    """NaN in the queries and log-sum-exps that no row picks, in keys behind the length
+    and in weights behind the old one changes nothing."""
+    rng = np.random.default_rng(T)
+    new, old = [200, 90], [200 - (T - 2), 90]
+    cache, _, _ = filled(new, 16, Hkv, rng)
+    rows = i32([[T - 1 - i for i in range(T - 2)], [0] * (T - 2)])
+    q = bf16(rng.standard_normal((2, T, Hq, 128))).cuda()
+    lse = torch.full((2, Hq, T), 6.0, device="cuda")
+    w, p = torch.rand((2, Hkv, 224), device="cuda"), torch.zeros((2, Hkv, 224), dtype=torch.int32, device="cuda")
+    call = lambda: adapld.kv8_attn_weights(cache, q, lse, i32(old), i32(new), i32([0, 0]), w, p, rows=rows,  # noqa: E731
+                                           weights_out=torch.zeros_like(w))[0]
+    want = call()
+    assert torch.isfinite(want).all() and torch.equal(want[1, :, :90], w[1, :, :90])
+    q[0, :2], q[1] = math.nan, math.nan
+    lse[0, :, :2], lse[1] = math.nan, math.nan
+    w[0, :, old[0]:] = math.nan
+    assert torch.equal(call(), want)
+
+
 def test_weights_long_and_clamped():
     """Longer than one workgroup takes, several sequences; lengths outside are clamped."""
     rng = np.random.default_rng(5)
