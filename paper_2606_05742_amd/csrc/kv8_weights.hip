@@ -7,6 +7,7 @@
 // workgroup's waves in a fixed order) sums up all that a key gets, so the order of a
 // sum does not depend on the launch.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "adapld_internal.h"
@@ -57,12 +58,7 @@ __device__ __forceinline__ const uint16_t* query_of(const WeightsArgs& a, int b,
 __device__ __forceinline__ bf16x8_t operand(uint32_t lo, uint32_t hi, float X) {
   return __builtin_bit_cast(bf16x8_t, kv8_values(make_uint2(lo, hi), X));
 }
-template <bool STREAM>
-__device__ __forceinline__ u32x4_t load16(const uint8_t* p) {
-  const u32x4_t* q = reinterpret_cast<const u32x4_t*>(p);
-  if constexpr (STREAM) return __builtin_nontemporal_load(q);
-  else return *q;
-}
+__device__ __forceinline__ u32x4_t load16(const uint8_t* p) { return *reinterpret_cast<const u32x4_t*>(p); }
 __device__ __forceinline__ float add_lane_xor32(float v) {
   const auto t = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
   return __int_as_float(t[0]) + __int_as_float(t[1]);
@@ -77,12 +73,14 @@ __device__ __forceinline__ float add_lane_xor16(float v) {
 // One pass over the keys: a wave takes steps of 32, alone, the queries stay in its
 // registers.  On v_mfma_f32_16x16x32_bf16 with the rows as A and 16 keys as B a lane
 // has 4 rows of one key, so a key's sum is its lane's own but for two exchanges.
-// Codes of two steps are in flight.
+// Codes of three steps are in flight.
 constexpr int kNarrowThreads = 256;
 constexpr int kNarrowWaves = kNarrowThreads / kWave;
 constexpr int kStep = 32;
+constexpr int kMaxSteps = 8;   // of a wave
+static_assert(kMaxSteps <= kWave, "a lane for each step's page ids");
 
-template <int RB, bool STREAM>
+template <int RB>
 __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(const WeightsArgs a) {
   const AttnWeightsCall& c = a.c;
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
@@ -90,17 +88,14 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lane = lane_id(), col = lane & 15, quad = lane >> 4;
   const int c0 = split * a.chunk;
-  // Lane j holds the page ids of the two halves of the wave's step first + j.
+  // Lane j holds the page ids of the two halves of the wave's step j (kMaxSteps at most).
   const int32_t* const table = c.page_table + (size_t)b * c.max_pages;
   int ids[2];
-  auto load_ids = [&](int first) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int pos = c0 + (wave + (first + lane) * kNarrowWaves) * kStep + 16 * i;
-      ids[i] = page_in_pool(table[min(pos >> a.page_shift, c.max_pages - 1)], c.n_pages);
-    }
-  };
-  load_ids(0);
+  for (int i = 0; i < 2; ++i) {
+    const int pos = c0 + (wave + lane * kNarrowWaves) * kStep + 16 * i;
+    ids[i] = page_in_pool(table[min(pos >> a.page_shift, c.max_pages - 1)], c.n_pages);
+  }
   const int old = min(max(c.lens_old[b], 0), c.L_max);
   const int n = min(max(min(max(c.lens_new[b], 0), c.L_max) - old, 0), c.N);
   const int c1 = min(c0 + a.chunk, old + n);
@@ -115,7 +110,7 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
     float w;   // of key k0 + lane, lanes 0..31
   };
   auto load = [&](int s, Raw& r) {
-    const int k0 = c0 + s * kStep, at = ((s - wave) / kNarrowWaves) & 63;
+    const int k0 = c0 + s * kStep, at = (s - wave) / kNarrowWaves;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       // Keys behind the last read the last one again; their sums are not stored.
@@ -131,23 +126,19 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
       }
       const size_t row = pool_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
       const uint8_t* const p = c.k_codes + row * kKv8RowBytes;
-      r.k[i][0] = load16<STREAM>(p + key * kKv8RowBytes + quad * 16);
-      r.k[i][1] = load16<STREAM>(p + key * kKv8RowBytes + quad * 16 + 64);
+      r.k[i][0] = load16(p + key * kKv8RowBytes + quad * 16);
+      r.k[i][1] = load16(p + key * kKv8RowBytes + quad * 16 + 64);
       r.e[i] = c.k_scales[row >> kKv8BlockShift];
     }
     r.w = w_in[min(k0 + (lane & 31), max(old - 1, 0))];
   };
-  // Codes of the second next step; behind the wave's last step that one again, so that
+  // Codes of the third next step; behind the wave's last step that one again, so that
   // the number of loads in flight does not depend on a branch.
   const int last = wave + (steps - 1 - wave) / kNarrowWaves * kNarrowWaves;
-  auto load_later = [&](int s, Raw& r) {
-    const int later = min(s + 2 * kNarrowWaves, last);
-    if ((later - wave) / kNarrowWaves % 64 == 0) load_ids((later - wave) / kNarrowWaves);
-    load(later, r);
-  };
-  Raw r[2];
+  Raw r[3];
   load(wave, r[0]);
   load(min(wave + kNarrowWaves, last), r[1]);
+  load(min(wave + 2 * kNarrowWaves, last), r[2]);
 
   bf16x8_t q[RB][4];
   float lse2[RB][4];
@@ -191,7 +182,7 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
         }
       sum[i] = (p[0] + p[1]) + (p[2] + p[3]);
     }
-    load_later(s, x);
+    load(min(s + 3 * kNarrowWaves, last), x);
     // lanes 0..15 and 16..31 take the sums of either half
     const float v0 = add_lane_xor32(add_lane_xor16(sum[0])), v1 = add_lane_xor32(add_lane_xor16(sum[1]));
     const float v = n == 0 ? 0.f : quad & 1 ? v1 : v0;   // without rows nothing is known of the keys
@@ -202,140 +193,239 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
     }
   };
   int s = wave;
-  for (; s + kNarrowWaves < steps; s += 2 * kNarrowWaves) {
+  for (; s + 2 * kNarrowWaves < steps; s += 3 * kNarrowWaves) {
     step(s, r[0]);
     step(s + kNarrowWaves, r[1]);
+    step(s + 2 * kNarrowWaves, r[2]);
   }
   if (s < steps) step(s, r[0]);
+  if (s + kNarrowWaves < steps) step(s + kNarrowWaves, r[1]);
 }
 
 // ---------------------------------------------------------- more than 64 rows
 //
 // A wave keeps 64 keys as A operands in registers and the rows pass by, 32 a block on
 // v_mfma_f32_32x32x16_bf16: a lane then has one row, so one log-sum-exp, and 32 sums
-// of keys that stay its own until the end.  Of a workgroup's 8 waves two share the
-// keys, each with every other block of rows; blocks come through LDS, the next pair
-// while the current one is multiplied.
-constexpr int kWideThreads = 512;
-constexpr int kWideKeys = 64;                         // of a wave
-constexpr int kWideGroups = kWideThreads / kWave / 2; // of waves with the same keys
-constexpr int kRowsBytes = 32 * kD * 2;               // a block of rows in LDS
+// of keys that stay its own until the end.  Of a workgroup's 8 waves 8 / KG share the
+// keys, each with every (8 / KG)-th block of rows.  A round is a block for each of
+// them; rounds come straight to a ring of four in LDS, two ahead, and the exponentials
+// of one round run beside the products of the next.
+constexpr int kWideKeys = 64;            // of a wave
+constexpr int kRowBytes = kD * 2;
+constexpr int kStages = 4;               // rounds in the ring
+constexpr int kMaxRows = 2048;           // rows whose places and log-sum-exps LDS holds at a time
 
 // Physical 16-byte chunk of logical chunk ch in row r: lanes that read one chunk of 16
 // consecutive rows hit every bank once.
-__device__ __forceinline__ int swizzled(int r, int ch) { return (r << 8) + ((ch ^ (r & 15)) << 4); }
+__device__ __forceinline__ int swizzled(int r, int ch) { return r * kRowBytes + ((ch ^ (r & 15)) << 4); }
 
-__global__ __launch_bounds__(kWideThreads, 2) void kv8_weights_wide_kernel(const WeightsArgs a) {
-  __shared__ __attribute__((aligned(1024))) uint8_t s_rows[2][2][kRowsBytes];
-  __shared__ float s_lse2[2][2][32];
+template <int KG, int kParts>
+__global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kernel(const WeightsArgs a) {
+  constexpr int kWideThreads = KG * kParts * kWave;
+  constexpr int kRows = 32 * kParts;               // rows of a round
+  constexpr int kLoads = 8 / KG;                   // of a wave for a round
+  __shared__ __attribute__((aligned(1024))) uint8_t s_rows[kStages][kRows * kRowBytes];
+  __shared__ int s_at[kMaxRows];       // query of a row, in rows of q behind the sequence's first; -1: none
+  __shared__ float s_lse2[kMaxRows];
+  __shared__ int s_any;
   const AttnWeightsCall& c = a.c;
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
   const int b = bg / c.Hkv, g = bg - b * c.Hkv;
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int kg = wave % kWideGroups, part = wave / kWideGroups;
+  const int kg = wave % KG, part = wave / KG;
   const int lane = lane_id(), col = lane & 31, half = lane >> 5;
   const int old = min(max(c.lens_old[b], 0), c.L_max);
   const int n = min(max(min(max(c.lens_new[b], 0), c.L_max) - old, 0), c.N);
-  const int end = old + n, c0 = split * (kWideGroups * kWideKeys);
+  const int end = old + n, c0 = split * (KG * kWideKeys);
   if (c0 >= end) return;
   const int k0 = c0 + kg * kWideKeys;
   const int rows = n * a.G;
 
   // Keys: lane (half, col) the dimensions [64 * half, +64) of keys col and 32 + col;
   // keys behind the last read the last one again, their sums are not stored.
-  bf16x8_t kf[2][8];
+  u32x4_t codes[2][4];
+  uint32_t exponent[2];
 #pragma unroll
   for (int m = 0; m < 2; ++m) {
     const int j = min(k0 + 32 * m + col, end - 1);
     const int page = page_in_pool(c.page_table[(size_t)b * c.max_pages + (j >> a.page_shift)], c.n_pages);
     const size_t row = pool_row(page, g, j & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
-    const float X = kv8_scale(c.k_scales[row >> kKv8BlockShift]);
     const u32x4_t* p = reinterpret_cast<const u32x4_t*>(c.k_codes + row * kKv8RowBytes + 64 * half);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x4_t w = p[i];
-      kf[m][2 * i] = operand(w[0], w[1], X);
-      kf[m][2 * i + 1] = operand(w[2], w[3], X);
-    }
+    for (int i = 0; i < 4; ++i) codes[m][i] = p[i];
+    exponent[m] = c.k_scales[row >> kKv8BlockShift];
   }
 
-  // Loader: 512 threads bring 64 rows, a thread two 16-byte chunks of one row.
-  const int lrow = tid >> 3, lch = tid & 7;
-  uint4 next[2];
-  float next_lse2 = 0.f;
-  auto fetch = [&](int r0) {
-    const RowAt x = row_at(a, b, g, n, r0 + lrow);
-    const uint4* const p = reinterpret_cast<const uint4*>(query_of(a, b, x));
-    next[0] = x.in ? p[lch] : make_uint4(0, 0, 0, 0);   // a row that is none must not bring a NaN
-    next[1] = x.in ? p[lch + 8] : make_uint4(0, 0, 0, 0);
-    if (lch == 0) next_lse2 = lse2_of(a, b, x);
-  };
-  auto store = [&](int buf) {
-    uint8_t* const p = s_rows[buf][lrow >> 5];
-    *reinterpret_cast<uint4*>(p + swizzled(lrow & 31, lch)) = next[0];
-    *reinterpret_cast<uint4*>(p + swizzled(lrow & 31, lch + 8)) = next[1];
-    if (lch == 0) s_lse2[buf][lrow >> 5][lrow & 31] = next_lse2;
-  };
-  fetch(0);
-  store(0);
-  __syncthreads();
   float sum[2][16] = {};
-  const bool plain = k0 + kWideKeys <= old + 1;   // every row sees all the wave's keys
-  int buf = 0;
-  for (int r0 = 0; r0 < rows; r0 += 64, buf ^= 1) {
-    if (r0 + 64 < rows) fetch(r0 + 64);
-    const uint8_t* const p = s_rows[buf][part];
-    const float lse2 = s_lse2[buf][part][col];
-    f32x16_t z[2] = {};
+  bf16x8_t kf[2][8];
+  const uint16_t* const q0 = c.q + (size_t)b * c.T_max * c.Hq * kD;
+  for (int first = 0; first < rows; first += kMaxRows) {
+    const int some = min(rows - first, kMaxRows), rounds = (some + kRows - 1) / kRows;
+    if (tid == 0) s_any = -1;
+    __syncthreads();
+    // all in flight together
+    RowAt x[kMaxRows / kWideThreads];
+    float lse2[kMaxRows / kWideThreads];
 #pragma unroll
-    for (int d = 0; d < 8; ++d) {
-      const bf16x8_t q = *reinterpret_cast<const bf16x8_t*>(p + swizzled(col, 8 * half + d));
+    for (int i = 0; i < kMaxRows / kWideThreads; ++i) x[i] = row_at(a, b, g, n, first + min(tid + i * kWideThreads, rounds * kRows - 1));
 #pragma unroll
-      for (int m = 0; m < 2; ++m) z[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[m][d], q, z[m], 0, 0, 0);
+    for (int i = 0; i < kMaxRows / kWideThreads; ++i) lse2[i] = lse2_of(a, b, x[i]);
+#pragma unroll
+    for (int i = 0; i < kMaxRows / kWideThreads; ++i) {
+      const int r = tid + i * kWideThreads;
+      if (r < rounds * kRows) {
+        s_at[r] = x[i].in ? x[i].u * c.Hq + x[i].h : -1;
+        s_lse2[r] = lse2[i];
+        if (x[i].in) s_any = x[i].u * c.Hq + x[i].h;
+      }
     }
-    if (plain) {
+    __syncthreads();
+    // A row that is none takes the place of one that is some, with an infinite log-sum-
+    // exp: what its own place in q holds may be no number.
+    const int any = s_any;
+    // A wave brings kLoads KiB of a round, four rows a load; behind the last round that
+    // one again, so that the number of loads in flight is the same in every round.
+    // Places are read from LDS a round before they are used.
+    const int r4 = wave * kLoads * 4;
+    int at[kLoads];
+    auto places = [&](int round) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) at[i] = s_at[min(round, rounds - 1) * kRows + r4 + 4 * i + lane / 16];
+    };
+    auto load = [&](int round) {
+      const uint32_t to = lds_addr(s_rows[round % kStages]) + r4 * kRowBytes;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        dma16(q0 + (size_t)(at[i] < 0 ? any : at[i]) * kD + ((lane ^ (r4 + 4 * i + lane / 16)) & 15) * 8,
+              __builtin_amdgcn_readfirstlane(to + 4 * i * kRowBytes));
+    };
+#pragma unroll
+    for (int i = 0; i + 1 < kStages; ++i) {
+      places(i);
+      if (any >= 0) load(i);
+    }
+    places(kStages - 1);
+    if (first == 0) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int t = 0; t < 16; ++t) sum[m][t] += __builtin_amdgcn_exp2f(fmaf(z[m][t], a.sl2, -lse2));
-    } else {
-      const int sees = old + (r0 + 32 * part + col) / a.G;
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int t = 0; t < 16; ++t) {
-          const float e = __builtin_amdgcn_exp2f(fmaf(z[m][t], a.sl2, -lse2));
-          sum[m][t] += k0 + 32 * m + 8 * (t >> 2) + (t & 3) + 4 * half <= sees ? e : 0.f;
+        for (int i = 0; i < 4; ++i) {
+          const float X = kv8_scale((int)exponent[m]);
+          kf[m][2 * i] = operand(codes[m][i][0], codes[m][i][1], X);
+          kf[m][2 * i + 1] = operand(codes[m][i][2], codes[m][i][3], X);
         }
     }
-    if (r0 + 64 < rows) store(buf ^ 1);
-    __syncthreads();
+    if (any < 0) continue;
+    // Eight chunks of a round: two products and four exponentials of the round before,
+    // kept together by scheduling barriers (left alone, the compiler sets the products
+    // behind each other, every one behind its operand's way through LDS).
+    auto operand_of = [&](int round, int d) {
+      return *reinterpret_cast<const bf16x8_t*>(s_rows[round % kStages] + 32 * part * kRowBytes + swizzled(col, 8 * half + d));
+    };
+    auto add4 = [&](const f32x16_t (&z)[2], int n4, float lse2, int sees, auto plain) {
+      const int m = n4 / 4;
+#pragma unroll
+      for (int t = 4 * (n4 % 4); t < 4 * (n4 % 4) + 4; ++t) {
+        const float w = __builtin_amdgcn_exp2f(fmaf(z[m][t], a.sl2, -lse2));
+        if constexpr (decltype(plain)::value) sum[m][t] += w;
+        else sum[m][t] += 32 * m + 8 * (t >> 2) + (t & 3) <= sees ? w : 0.f;
+      }
+    };
+    // With NEXT the products of the next round, with ADD the exponentials of this one.
+    auto round_of = [&](int i, f32x16_t (&z)[2], f32x16_t (&z_next)[2], auto plain, auto NEXT, auto ADD) {
+      constexpr bool kNext = decltype(NEXT)::value, kAdd = decltype(ADD)::value;
+      bf16x8_t q[8];
+      if constexpr (kNext) {
+#pragma unroll
+        for (int d = 0; d < 3; ++d) q[d] = operand_of(i + 1, d);
+        z_next[0] = z_next[1] = f32x16_t{};
+      }
+      const int r = i * kRows + 32 * part + col;
+      float lse2 = 0.f;
+      int sees = 0;
+      if constexpr (kAdd) {
+        lse2 = s_lse2[r];
+        // the last key that the row sees, counted from the lane's first
+        if constexpr (!decltype(plain)::value) sees = old + (first + r) / a.G - k0 - 4 * half;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        if constexpr (kNext) {
+          if (d + 3 < 8) q[d + 3] = operand_of(i + 1, d + 3);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) z_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[m][d], q[d], z_next[m], 0, 0, 0);
+        }
+        if constexpr (kAdd) add4(z, d, lse2, sees, plain);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto run = [&](auto plain) {
+      using Yes = std::true_type;
+      using No = std::false_type;
+      f32x16_t za[2], zb[2];
+      waitcnt_vm<(kStages - 2) * kLoads>();
+      __syncthreads();
+      round_of(-1, zb, za, plain, Yes{}, No{});
+      waitcnt_vm<(kStages - 3) * kLoads>();
+      __syncthreads();
+      // Round i + 1, whose products are formed, has landed; round i + kStages - 1 takes the
+      // place of round i - 1.
+      auto body = [&](int i, f32x16_t (&z)[2], f32x16_t (&z_next)[2]) {
+        load(i + kStages - 1);
+        places(i + kStages);
+        round_of(i, z, z_next, plain, Yes{}, Yes{});
+        waitcnt_vm<(kStages - 3) * kLoads>();
+        __syncthreads();
+      };
+      int i = 0;
+      for (; i + 2 < rounds; i += 2) {
+        body(i, za, zb);
+        body(i + 1, zb, za);
+      }
+      if (i + 1 < rounds) {
+        body(i, za, zb);
+        round_of(i + 1, zb, za, plain, No{}, Yes{});
+      } else {
+        round_of(i, za, zb, plain, No{}, Yes{});
+      }
+    };
+    if (k0 + kWideKeys <= old + 1) run(std::true_type{});   // every row sees all the wave's keys
+    else run(std::false_type{});
+    waitcnt_vm<0>();
   }
-  // Sums over the 32 lanes of a half, then of the two waves of the same keys.
+  // Sums over the 32 lanes of a half, then of the waves of the same keys.  Values 16
+  // lanes apart and 8 apart are added in pairs, each half of the lanes keeping one.
   float* const s_sum = reinterpret_cast<float*>(s_rows);   // [waves][64 keys]
   __syncthreads();
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int t = 0; t < 16; ++t) {
-      float v = sum[m][t];
-      v += __shfl_xor(v, 16, kWave);
-      v += __shfl_xor(v, 8, kWave);
-      v += __shfl_xor(v, 4, kWave);
-      v += __shfl_xor(v, 2, kWave);
-      v += __shfl_xor(v, 1, kWave);
-      if (col == t) s_sum[wave * kWideKeys + 32 * m + 8 * (t >> 2) + (t & 3) + 4 * half] = v;
+    for (int t = 0; t < 4; ++t) {
+      float h[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {   // values t + 4 i and t + 4 i + 8, the latter where bit 4 of the lane is set
+        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_int(sum[m][t + 4 * i]), __float_as_int(sum[m][t + 4 * i + 8]), false, false);
+        h[i] = __int_as_float(w[0]) + __int_as_float(w[1]);
+      }
+      const bool up = lane & 8;       // h[1] where bit 3 is set
+      float v = (up ? h[1] : h[0]) + dpp_f32<0x128>(up ? h[0] : h[1]);   // row_ror:8
+      v += dpp_f32<0x141>(v);             // row_half_mirror
+      v += dpp_f32<0xb1>(v);              // quad_perm 1 0 3 2
+      v += dpp_f32<0x4e>(v);              // quad_perm 2 3 0 1
+      const int value = t + 4 * ((lane >> 3) & 1) + 8 * ((lane >> 4) & 1);
+      if ((lane & 7) == 0) s_sum[wave * kWideKeys + 32 * m + 8 * (value >> 2) + (value & 3) + 4 * half] = v;
     }
   __syncthreads();
-  if (tid < kWideGroups * kWideKeys) {
-    const int key = c0 + tid;
-    if (key < end) {
-      const float v = s_sum[tid] + s_sum[kWideGroups * kWideKeys + tid];
-      const size_t at = (size_t)bg * c.stride + key;
-      c.weights_out[at] = key < old ? c.weights[at] + v : v;
-      if (key >= old) c.positions[at] = c.first_position[b] + (key - old);
-    }
+  const int key = c0 + tid;
+  if (tid < KG * kWideKeys && key < end) {
+    float v = s_sum[tid];
+#pragma unroll
+    for (int p = 1; p < kParts; ++p) v += s_sum[p * KG * kWideKeys + tid];
+    const size_t at = (size_t)bg * c.stride + key;
+    c.weights_out[at] = key < old ? c.weights[at] + v : v;
+    if (key >= old) c.positions[at] = c.first_position[b] + (key - old);
   }
 }
 
@@ -350,24 +440,38 @@ hipError_t launch_kv8_attn_weights(const AttnWeightsCall& c, hipStream_t stream)
   const int64_t pairs = (int64_t)c.B * c.Hkv;
   const int64_t rows = (int64_t)c.N * a.G;
   if (rows > 64) {
-    a.chunk = kWideGroups * kWideKeys;
-    a.nsplit = (c.L_max + a.chunk - 1) / a.chunk;
-    hipLaunchKernelGGL(kv8_weights_wide_kernel, dim3((unsigned)(pairs * a.nsplit)), dim3(kWideThreads), 0, stream, a);
+    // A workgroup of 256 keys passes 64 rows a round, one of 128 keys 128 rows; a round
+    // takes 1.2 to 1.3 us, the rest of a workgroup 4, and 256 of them run at once.  us a
+    // call, 256 / 128 keys: 4 x 4096 keys of 4 heads, 256 rows of 7 heads 41.2 / 49.9, 32
+    // of them 13.2 / 18.8; 4 x 2048, 256 rows 37.3 / 27.3, 32 13.2 / 10.0.
+    auto cost = [&](int keys, int round) {
+      const double groups = (double)(pairs * ((c.L_max + keys - 1) / keys));
+      return std::ceil(groups / 256) * (4 + 1.25 * (double)((rows + round - 1) / round));
+    };
+    auto wide = [&](auto KG, auto parts) {
+      constexpr int kg = decltype(KG)::value, kp = decltype(parts)::value;
+      a.chunk = kg * kWideKeys;
+      a.nsplit = (c.L_max + a.chunk - 1) / a.chunk;
+      hipLaunchKernelGGL((kv8_weights_wide_kernel<kg, kp>), dim3((unsigned)(pairs * a.nsplit)), dim3(kg * kp * kWave), 0,
+                         stream, a);
+    };
+    using Two = std::integral_constant<int, 2>;
+    using Four = std::integral_constant<int, 4>;
+    if (cost(256, 64) <= cost(128, 128)) wide(Four{}, Two{});
+    else wide(Two{}, Four{});
     return hipGetLastError();
   }
-  // Steps of a wave: up to 16, fewer while there are not 1024 workgroups.
+  // Steps of a wave: up to 8, fewer while there are not 1024 workgroups (32 x 8192 keys of
+  // 8 heads, single tokens: 58 us with 8 to 32 steps, 62 to 65 with two steps in flight
+  // or non-temporal loads).
   constexpr int kUnit = kNarrowWaves * kStep;
   const int units = (c.L_max + kUnit - 1) / kUnit;
-  const int per = (int)std::min<int64_t>(16, std::max<int64_t>(1, pairs * units / 1024));
+  const int per = (int)std::min<int64_t>(kMaxSteps, std::max<int64_t>(1, pairs * units / 1024));
   a.chunk = per * kUnit;
   a.nsplit = (units + per - 1) / per;
-  constexpr size_t kPlainBytes = (size_t)64 << 20;
-  const bool stream_k = (size_t)pairs * c.L_max * kKv8RowBytes >= kPlainBytes;
   auto narrow = [&](auto rb) {
     constexpr int RB = decltype(rb)::value;
-    const dim3 grid((unsigned)(pairs * a.nsplit));
-    if (stream_k) hipLaunchKernelGGL((kv8_weights_narrow_kernel<RB, true>), grid, dim3(kNarrowThreads), 0, stream, a);
-    else hipLaunchKernelGGL((kv8_weights_narrow_kernel<RB, false>), grid, dim3(kNarrowThreads), 0, stream, a);
+    hipLaunchKernelGGL(kv8_weights_narrow_kernel<RB>, dim3((unsigned)(pairs * a.nsplit)), dim3(kNarrowThreads), 0, stream, a);
   };
   if (rows <= 16) narrow(std::integral_constant<int, 1>{});
   else if (rows <= 32) narrow(std::integral_constant<int, 2>{});
