@@ -250,6 +250,15 @@ def test_evict_pages_outside_the_pool():
     check_evict([300, 300], 128, 8, 16, 2, bad=[(0, 1, -1), (0, 3, 1 << 30), (0, 12, -5), (0, 17, 999)])
 
 
+@pytest.mark.parametrize("lens, budget", [([5000, 4200], 4096), ([9000], 8192), ([8192], 8160), ([20000, 17000], 16400),
+                                          ([33000], 800), ([80, 127, 64], 64)])
+def test_evict_lengths(lens, budget):
+    """Slots held a few, several or many a thread, more than a workgroup holds; many
+    and few moves."""
+    check_evict(lens, budget, 20, 64, 1)
+    check_evict(lens, budget, 20, 64, 1, weights=lambda r, s: r.integers(0, 3, s))
+
+
 def test_evict_many():
     check_evict([64 + 5 * b for b in range(40)], 64, 7, 16, 4)
 
