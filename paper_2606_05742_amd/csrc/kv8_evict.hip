@@ -76,7 +76,10 @@ __device__ __forceinline__ void move_block(const EvictCall& c, int b, int g, int
   for (int t = 0; t < 4; ++t) {
     from_r[t] = __shfl(from, 4 * t + sub, kWave);
 #pragma unroll
-    for (int n = 0; n < 2; ++n) x[n][t] = *reinterpret_cast<const uint2*>(c.codes[n] + from_r[t] * kKv8RowBytes + part * 8);
+    for (int n = 0; n < 2; ++n) {
+      x[n][t] = make_uint2(0, 0);
+      if (from_r[t] != to + 4 * t + sub) x[n][t] = *reinterpret_cast<const uint2*>(c.codes[n] + from_r[t] * kKv8RowBytes + part * 8);
+    }
   }
 #pragma unroll
   for (int n = 0; n < 2; ++n) {
@@ -84,9 +87,10 @@ __device__ __forceinline__ void move_block(const EvictCall& c, int b, int g, int
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int r = 4 * t + sub, e_r = __shfl(e[n], r, kWave);
-      if (from_r[t] != to + r || e_r != most)
-        *reinterpret_cast<uint2*>(c.codes[n] + (to + r) * kKv8RowBytes + part * 8) =
-            e_r == most ? x[n][t] : kv8_rescale(x[n][t], e_r, most);
+      const bool comes = from_r[t] != to + r;
+      uint2* const at = reinterpret_cast<uint2*>(c.codes[n] + (to + r) * kKv8RowBytes + part * 8);
+      if (e_r != most) *at = kv8_rescale(comes ? x[n][t] : *at, e_r, most);
+      else if (comes) *at = x[n][t];
     }
     if (lane == 0) c.scales[n][to >> kKv8BlockShift] = (uint8_t)most;
   }
@@ -193,6 +197,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
     known |= digit << shift;
     want = s_pick[1];
     equal = s_pick[2];
+    if (want == equal) break;   // all of them stay: the other digits do not matter
   }
 
   // In order of slots: the first `want` of the equal ones stay.  A slot's rank is the
