@@ -193,19 +193,20 @@ def _dptr(t, name, dtypes, shape, dev, nullable=False):
     return p
 
 
-def _rows_ptr(t, name, dev):
-    """The pointer of bf16 [B, T, heads, D] whose heads and dimensions are
-    contiguous, on the current device; tokens and sequences may be strided."""
-    if not isinstance(t, torch.Tensor):
+def _rows(t, name, shape, dev):
+    """(pointer, strides of sequences and tokens) of bf16 [B, T, heads, D] on the
+    current device whose heads and dimensions are contiguous; tokens and sequences
+    may be strided."""
+    if type(t) is not _Tensor and not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.get_device() != dev:
         raise AdapldError(-2, f"{name} is on {t.device}, the current device is cuda:{dev}")
     if t.dtype not in _BF16_DTYPES:
         raise AdapldError(-2, f"{name} has dtype {t.dtype}, expected one of {_BF16_DTYPES}")
-    D = t.shape[3]
-    if t.stride(3) != 1 or (t.stride(2) != D and t.shape[2] != 1):
+    batch, token, head, dim = t.stride()
+    if dim != 1 or (head != shape[3] and shape[2] != 1):
         raise AdapldError(-2, f"{name} must be contiguous in its heads and dimensions, its strides are {t.stride()}")
-    return t.data_ptr()
+    return t.data_ptr(), batch, token
 
 
 def _stream_on(stream, dev):
@@ -546,12 +547,15 @@ def qk_norm_rope(q, k, freqs, base, *, offsets=None, counts=None, q_weight=None,
         with _on(stream, dev):
             q_out = torch.empty(shape, dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
             k_out = torch.empty(kshape, dtype=torch.bfloat16, device=q.device) if k_out is None else k_out
-    weight = _BF16_DTYPES, (D,), dev, True
+    qp, q_batch, q_token = _rows(q, "q", shape, dev)
+    kp, k_batch, k_token = _rows(k, "k", kshape, dev)
     st = load_library().adapld_qk_norm_rope(
-        _rows_ptr(q, "q", dev), _rows_ptr(k, "k", dev), q.stride(0), q.stride(1), k.stride(0), k.stride(1),
-        _dptr(q_weight, "q_weight", *weight), _dptr(k_weight, "k_weight", *weight),
+        qp, kp, q_batch, q_token, k_batch, k_token,
+        None if q_weight is None else _dptr(q_weight, "q_weight", _BF16_DTYPES, (D,), dev),
+        None if k_weight is None else _dptr(k_weight, "k_weight", _BF16_DTYPES, (D,), dev),
         _dptr(freqs, "freqs", _I64, None, dev), _dptr(base, "base", _I32, (B,), dev),
-        _dptr(offsets, "offsets", _I32, (B, T), dev, True), _dptr(counts, "counts", _I32, (B,), dev, True),
+        None if offsets is None else _dptr(offsets, "offsets", _I32, (B, T), dev),
+        None if counts is None else _dptr(counts, "counts", _I32, (B,), dev),
         B, T, Hq, Hkv, D, 2 * freqs.numel(), int(bool(interleaved)), eps,
         _dptr(q_out, "q_out", _BF16_DTYPES, shape, dev), _dptr(k_out, "k_out", _BF16_DTYPES, kshape, dev),
         _stream_on(stream, dev))

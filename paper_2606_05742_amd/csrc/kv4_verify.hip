@@ -22,6 +22,15 @@ namespace {
 // A part is a group of 32 dimensions: 16 bytes of codes and a scale of its own.
 struct Kv4Format {
   static constexpr int kLoads = 1, kCodeBytes = kKv4RowBytes;
+  // A model's layers each bring their own cache, so a call finds its codes in
+  // HBM; where one wave reads each of them, large ones are streamed past the
+  // caches.  us a call over rotating caches, plain / non-temporal: single tokens,
+  // 32 x 8192 keys of 8 kv heads (256 MiB of codes) 58.5 / 54.5, 4 x 30000 (117)
+  // 35.4 / 32.5; 8 nodes, 16 x 4096 (64) 29.4 / 27.9; 8 x 2048 (16) 12.9 / 12.9.
+  // Called again on the same cache, plain loads find it in the last-level cache:
+  // 49.4 / 54.4, 29.4 / 30.8, 25.4 / 27.3, 10.8 / 11.3; so small ones load plainly.
+  // Two row blocks read the codes twice: chains of 16 nodes, 32 x 4096 62.5 / 63.5.
+  static constexpr size_t kStreamBytes = (size_t)64 << 20;
   static __device__ __forceinline__ uint32_t code_at(uint32_t key, int part, int) { return key * kKv4RowBytes + part * 16; }
   static __device__ __forceinline__ int chunk(int part, int j) { return 4 * part + j; }
   static __device__ __forceinline__ uint32_t load_scale(const uint8_t* scales, size_t row, uint32_t key, int part) {
@@ -66,16 +75,7 @@ VerifyPagedPlan plan_verify_kv4(int B, int L_max, int T_max, int Hq, int Hkv) {
 size_t verify_kv4_ws_bytes(const VerifyPagedPlan& p, int B, int Hkv) { return paged_ws_bytes(p, B, Hkv); }
 
 hipError_t launch_tree_verify_attn_kv4(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipStream_t stream) {
-  // A model's layers each bring their own cache, so a call finds its codes in
-  // HBM; where one wave reads each of them, large ones are streamed past the
-  // caches.  us a call over rotating caches, plain / non-temporal: single tokens,
-  // 32 x 8192 keys of 8 kv heads (256 MiB of codes) 58.5 / 54.5, 4 x 30000 (117)
-  // 35.4 / 32.5; 8 nodes, 16 x 4096 (64) 29.4 / 27.9; 8 x 2048 (16) 12.9 / 12.9.
-  // Called again on the same cache, plain loads find it in the last-level cache:
-  // 49.4 / 54.4, 29.4 / 30.8, 25.4 / 27.3, 10.8 / 11.3; so small ones load plainly.
-  // Two row blocks read the codes twice: chains of 16 nodes, 32 x 4096 62.5 / 63.5.
-  constexpr size_t kPlainBytes = (size_t)64 << 20;
-  return launch_paged<Kv4Format>(c, p, kPlainBytes, stream);
+  return launch_paged<Kv4Format>(c, p, stream);
 }
 
 }  // namespace adapld

@@ -9,8 +9,18 @@ namespace adapld {
 
 constexpr int kKv8RowLanes = ADAPLD_HEAD_DIM / 8;
 
-// The largest magnitude of 8 bf16 values as bits, infinities and NaN left out.
-__device__ __forceinline__ uint32_t kv8_amax(uint4 x) {
+// The largest magnitude of 8 bf16 values as bits.
+typedef uint16_t kv8_u16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t kv8_max2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(kv8_u16x2_t, a), __builtin_bit_cast(kv8_u16x2_t, b)));
+}
+__device__ __forceinline__ uint32_t kv8_amax2(uint4 x) {   // of either half of the words
+  const uint32_t m = 0x7fff7fffu;
+  return kv8_max2(kv8_max2(x.x & m, x.y & m), kv8_max2(x.z & m, x.w & m));
+}
+__device__ __forceinline__ uint32_t kv8_halves_max(uint32_t m) { return max(m & 0xffffu, m >> 16); }
+// The same with infinities and NaN left out.
+__device__ __forceinline__ uint32_t kv8_finite_amax(uint4 x) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t m = 0;
 #pragma unroll
@@ -31,14 +41,22 @@ __device__ __forceinline__ float kv8_scale(int e) { return __uint_as_float((uint
 
 typedef short kv8_s16x2_t __attribute__((ext_vector_type(2)));
 
-// 8 bf16 values as codes: rounded once, to the nearest, ties to even; magnitudes above
-// 448 X (infinities, and what 2^(kKv8MaxExp - 127) does not reach) as 448 X, NaN as
-// 0x7f (the conversion gives 0xff, whatever the NaN's sign).
+// 8 bf16 values of magnitudes up to 448 X as codes: rounded once, to the nearest, ties
+// to even.
+__device__ __forceinline__ uint2 kv8_round(uint4 x, float X) {
+  kv8_s16x2_t a{}, b{};
+  a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(bf16x2_t, x.x), X, false);
+  a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(bf16x2_t, x.y), X, true);
+  b = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(b, __builtin_bit_cast(bf16x2_t, x.z), X, false);
+  b = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(b, __builtin_bit_cast(bf16x2_t, x.w), X, true);
+  return make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+}
+// Any 8 values: magnitudes above 448 X (infinities, and what 2^(kKv8MaxExp - 127) does
+// not reach) as 448 X, NaN as 0x7f (the conversion gives 0xff, whatever the NaN's sign).
 __device__ __forceinline__ uint32_t kv8_plain_nan(uint32_t c) {
   return c & ~(((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u);
 }
 __device__ __forceinline__ uint2 kv8_quantise(uint4 x, int e) {
-  const float X = kv8_scale(e);
   const uint32_t most = (uint32_t)(e + 8) << 7 | 0x60u;
   uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -47,12 +65,8 @@ __device__ __forceinline__ uint2 kv8_quantise(uint4 x, int e) {
     const uint32_t lo2 = lo <= 0x7f80u ? min(lo, most) : lo, hi2 = hi <= 0x7f80u ? min(hi, most) : hi;
     w[i] = (w[i] & 0x80008000u) | lo2 | (hi2 << 16);
   }
-  kv8_s16x2_t a{}, b{};
-  a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(bf16x2_t, w[0]), X, false);
-  a = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(a, __builtin_bit_cast(bf16x2_t, w[1]), X, true);
-  b = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(b, __builtin_bit_cast(bf16x2_t, w[2]), X, false);
-  b = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(b, __builtin_bit_cast(bf16x2_t, w[3]), X, true);
-  return make_uint2(kv8_plain_nan(__builtin_bit_cast(uint32_t, a)), kv8_plain_nan(__builtin_bit_cast(uint32_t, b)));
+  const uint2 c = kv8_round(make_uint4(w[0], w[1], w[2], w[3]), kv8_scale(e));
+  return make_uint2(kv8_plain_nan(c.x), kv8_plain_nan(c.y));
 }
 
 // 8 codes as bf16 values, exact.

@@ -18,6 +18,8 @@
 //                          j = 0..3 of the part is
 //   dequant(c, j, X)       that group as 8 bf16 values, scale X
 //   load_scale(...)        the part's scale byte
+//   kStreamBytes           bytes of codes from which on a cache that one wave reads is
+//                          loaded with the non-temporal hint; 0: never
 #pragma once
 
 #include <algorithm>
@@ -1218,10 +1220,8 @@ inline size_t paged_ws_bytes(const VerifyPagedPlan& p, int B, int Hkv) {
   return (size_t)B * Hkv * p.nsplit * p.rows_max * (kD * sizeof(float) + sizeof(float2));
 }
 
-// stream_min: bytes of codes from which on a cache that one wave reads is streamed
-// past the caches.
 template <class F>
-hipError_t launch_paged(const VerifyPagedCall& c, const VerifyPagedPlan& p, size_t stream_min, hipStream_t stream) {
+hipError_t launch_paged(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipStream_t stream) {
   PagedArgs a{};
   a.c = c;
   a.G = c.Hq / c.Hkv; a.rows_max = p.rows_max; a.nw = (c.T_max + 63) / 64;
@@ -1234,22 +1234,21 @@ hipError_t launch_paged(const VerifyPagedCall& c, const VerifyPagedPlan& p, size
   a.ws_ml = c.ws ? reinterpret_cast<float2*>(static_cast<float*>(c.ws) + slots * kD) : nullptr;
   const int units = c.B * c.Hkv * p.nsplit;
   const dim3 grid((unsigned)((units + 7) / 8 * 8 * p.rowgroups));
-  const bool stream_kv = (size_t)c.B * c.L_max * c.Hkv * 2 * F::kCodeBytes >= stream_min;
   auto narrow = [&](auto rows, auto rb, auto st) {
     hipLaunchKernelGGL((paged_narrow_kernel<F, decltype(rows), decltype(rb)::value, decltype(st)::value>),
                        dim3((unsigned)units), dim3(kThreads), 0, stream, a);
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;
+  auto one_block = [&](auto rows) {
+    if constexpr (F::kStreamBytes > 0) {
+      if ((size_t)c.B * c.L_max * c.Hkv * 2 * F::kCodeBytes >= F::kStreamBytes) return narrow(rows, One{}, std::true_type{});
+    }
+    narrow(rows, One{}, std::false_type{});
+  };
   switch (p.rows) {
-    case 16:
-      if (stream_kv) narrow(Rows16<F>{}, One{}, std::true_type{});
-      else narrow(Rows16<F>{}, One{}, std::false_type{});
-      break;
-    case 32:
-      if (stream_kv) narrow(Rows32<F>{}, One{}, std::true_type{});
-      else narrow(Rows32<F>{}, One{}, std::false_type{});
-      break;
+    case 16: one_block(Rows16<F>{}); break;
+    case 32: one_block(Rows32<F>{}); break;
     case 64: narrow(Rows32<F>{}, Two{}, std::false_type{}); break;
     case 128: hipLaunchKernelGGL((paged_verify_kernel<F, 4>), grid, dim3(kThreads), 0, stream, a); break;
     default: hipLaunchKernelGGL((paged_verify_kernel<F, 8>), grid, dim3(kThreads), 0, stream, a); break;
