@@ -52,7 +52,8 @@ extern "C" {
  * Errors: NULL_ARG; INVALID_ARG for B < 0, T, Hq, Hkv < 1, rot_dim outside 0..D or
  * no multiple of 16, interleaved outside {0, 1}, eps not finite or < 0, strides
  * that are negative or no multiples of 8, misaligned pointers (8 bytes for
- * freqs); UNSUPPORTED for D != 128 or B * T * (Hq + Hkv) > 2^28 - 16.
+ * freqs); UNSUPPORTED for D != 128, B * T * (Hq + Hkv) > 2^28 - 16 or B * T *
+ * ceil((Hq + Hkv) / 16) > 2^26 - 4.
  */
 int adapld_qk_norm_rope(const uint16_t* q, const uint16_t* k, int64_t q_batch, int64_t q_token, int64_t k_batch,
                         int64_t k_token, const uint16_t* q_weight, const uint16_t* k_weight, const uint64_t* freqs,
@@ -174,7 +175,8 @@ int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const
  * without rows, L_max > max_pages * page_size or stride, a page_size other than the
  * five, scale as in the attention, or misaligned pointers; UNSUPPORTED for D != 128,
  * T_max or N > ADAPLD_MAX_TREE_NODES, n_pages * page_size or max_pages * page_size >
- * INT32_MAX, L_max > 2^30, or B * Hkv * (L_max / 128 + 1) > 2^24 - 1.
+ * INT32_MAX, L_max > 2^30, B * max(T_max, N) * Hq > 2^27 - 8, or B * Hkv * (L_max / 128 +
+ * 1) > 2^23 - 1.
  */
 int adapld_kv8_attn_weights(const uint16_t* q, const float* lse, const int32_t* rows, const uint8_t* k_codes,
                             const uint8_t* k_scales, const int32_t* page_table, const int32_t* lens_old,

@@ -206,7 +206,8 @@ def _rows(t, name, shape, dev):
     batch, token, head, dim = t.stride()
     if dim != 1 or (head != shape[3] and shape[2] != 1):
         raise AdapldError(-2, f"{name} must be contiguous in its heads and dimensions, its strides are {t.stride()}")
-    return t.data_ptr(), batch, token
+    # the stride of a single entry is whatever made the tensor
+    return t.data_ptr(), batch if shape[0] > 1 else 0, token if shape[1] > 1 else 0
 
 
 def _stream_on(stream, dev):

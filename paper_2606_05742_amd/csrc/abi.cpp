@@ -33,9 +33,10 @@ size_t step_sem_part(int B, int L_stride, int k) { return (semantic_ws(B, L_stri
 constexpr int64_t kKv4MaxRows = (1 << 28) - 16;
 constexpr int64_t kKv4MaxOutRows = (1 << 27) - 8;
 constexpr int64_t kKv4MaxGroups = (1 << 23) - 8;
-// 64 threads a block, 256 a workgroup of the weights, 1024 a kv head of the eviction.
-constexpr int64_t kKv8MaxBlocks = (1 << 26) - 4;
-constexpr int64_t kKv8MaxWeightGroups = (1 << 24) - 1;
+// A wave of 64 a block or a token's heads, 512 a workgroup of the weights, 1024 a kv head
+// of the eviction.
+constexpr int64_t kMaxWaves = (1 << 26) - 4;
+constexpr int64_t kKv8MaxWeightGroups = (1 << 23) - 1;
 constexpr int64_t kKv8MaxPairs = (1 << 22) - 1;
 
 // The embedding fallback's own part (16-byte aligned), then the scan's lists.
@@ -605,7 +606,10 @@ int adapld_qk_norm_rope(const uint16_t* q, const uint16_t* k, int64_t q_batch, i
                         (const void*)q_out, (const void*)k_out})
     if (misaligned16(p)) return ADAPLD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(freqs) & 7u) != 0) return ADAPLD_ERR_INVALID_ARG;
-  if (D != ADAPLD_HEAD_DIM || (double)B * T * ((double)Hq + Hkv) > kKv4MaxRows) return ADAPLD_ERR_UNSUPPORTED;
+  // at least 4 heads of a token a wave, and 16 where there are more rows than 2^18
+  if (D != ADAPLD_HEAD_DIM || (double)B * T * ((double)Hq + Hkv) > kKv4MaxRows ||
+      (double)B * T * (((int64_t)Hq + Hkv + 15) / 16) > kMaxWaves)
+    return ADAPLD_ERR_UNSUPPORTED;
   const adapld::NormRopeCall c{{q, k}, {q_batch, k_batch}, {q_token, k_token}, {q_weight, k_weight}, freqs, base,
                                offsets, counts, B, T, Hq, Hkv, rot_dim, interleaved, eps, {q_out, k_out}};
   return hip_status(adapld::launch_qk_norm_rope(c, stream));
@@ -625,7 +629,7 @@ int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_
   if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
   // a wave of 64 threads a block of a kv head, below 2^32 threads a launch
   if (D != ADAPLD_HEAD_DIM || (int64_t)max_pages * page_size > INT32_MAX ||
-      (double)B * adapld::kv8_blocks_touched(N) * Hkv > kKv8MaxBlocks)
+      (double)B * adapld::kv8_blocks_touched(N) * Hkv > kMaxWaves)
     return ADAPLD_ERR_UNSUPPORTED;
   return hip_status(adapld::launch_kv8_append(k_new, v_new, rows, lens_old, lens_new, page_table, B, n_src, N, Hkv,
                                               page_size, n_pages, max_pages, k_codes, k_scales, v_codes, v_scales,
@@ -649,6 +653,7 @@ int adapld_kv8_attn_weights(const uint16_t* q, const float* lse, const int32_t* 
   if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
   if (D != ADAPLD_HEAD_DIM || T_max > ADAPLD_MAX_TREE_NODES || N > ADAPLD_MAX_TREE_NODES ||
       (int64_t)max_pages * page_size > INT32_MAX || L_max > (1 << 30) ||
+      (double)B * (T_max > N ? T_max : N) * Hq > kKv4MaxOutRows ||
       (double)B * Hkv * (L_max / 128 + 1) > kKv8MaxWeightGroups)
     return ADAPLD_ERR_UNSUPPORTED;
   if (L_max > max_pages * page_size || misaligned16(q) || misaligned16(k_codes)) return ADAPLD_ERR_INVALID_ARG;
@@ -679,7 +684,7 @@ int adapld_kv8_evict(const float* weights, const int32_t* positions, const int32
   if (const int st = check_kv4_pool(page_size, n_pages); st != ADAPLD_OK) return st;
   if (D != ADAPLD_HEAD_DIM || (int64_t)max_pages * page_size > INT32_MAX || L_max > (1 << 30) ||
       (double)B * Hkv > kKv8MaxPairs ||
-      (L_max > budget && (double)B * Hkv * (budget / ADAPLD_KV8_BLOCK) > kKv8MaxBlocks))
+      (L_max > budget && (double)B * Hkv * (budget / ADAPLD_KV8_BLOCK) > kMaxWaves))
     return ADAPLD_ERR_UNSUPPORTED;
   if (L_max > max_pages * page_size) return ADAPLD_ERR_INVALID_ARG;
   const size_t need = adapld::evict_ws_bytes(B, Hkv, L_max, budget);

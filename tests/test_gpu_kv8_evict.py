@@ -228,6 +228,22 @@ def test_evict_sizes_of_weights():
     check_evict([300, 200], 32, 0, 32, 3, weights=lambda r, s: -np.exp2(r.uniform(-140, 120, s)))
 
 
+def test_evict_not_a_number():
+    """Infinities are ranked like other numbers, NaN as the largest or the smallest by
+    its sign."""
+    cache, _ = make_cache([64], 16, 1, np.random.default_rng(1))
+    adapld.kv8_append(cache, *(bf16(np.ones((1, 64, 1, 128))).cuda() for _ in range(2)), i32([0]), i32([64]))
+    w = torch.ones((1, 1, 64))
+    w[0, 0, [3, 5]] = torch.tensor([math.nan, -math.nan])
+    w[0, 0, [7, 9]] = torch.tensor([-math.inf, math.inf])
+    w[0, 0, 48:] = torch.tensor([2.0, math.nan, math.inf, -math.inf] + [0.5] * 12)
+    p = torch.arange(64, dtype=torch.int32, device="cuda").view(1, 1, 64)
+    _, po, lo = adapld.kv8_evict(cache, w.cuda(), p, i32([64]), i32([64]), 48, 0)
+    want = list(range(48))
+    want[5], want[7], want[47] = 48, 49, 50      # -NaN, -inf and the last of the ones go
+    assert lo.tolist() == [48] and po[0, 0, :48].tolist() == want
+
+
 def test_evict_protection():
     """More protected tokens than the budget, all, none, positions at the ends of 32 bits."""
     check_evict([500, 480], 64, 700, 16, 2)

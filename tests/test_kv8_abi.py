@@ -125,6 +125,7 @@ def test_norm_rope_refusals(lib):
         assert f(*_args(ROPE, **bad)) == INVALID, bad
     assert f(*_args(ROPE, B=1 << 14, T=1 << 11)) == UNSUPPORTED
     assert f(*_args(ROPE, B=MAX, T=MAX, Hq=MAX, Hkv=MAX)) == UNSUPPORTED
+    assert f(*_args(ROPE, B=1 << 13, T=1 << 13, Hq=1, Hkv=1)) == UNSUPPORTED   # a wave a token
 
 
 def test_attn_weights_refusals(lib):
@@ -134,6 +135,9 @@ def test_attn_weights_refusals(lib):
         assert f(*_args(WEIGHTS, **bad)) == INVALID, bad
     assert f(*_args(WEIGHTS, T_max=257)) == UNSUPPORTED
     assert f(*_args(WEIGHTS, N=257, rows=P)) == UNSUPPORTED
+    assert f(*_args(WEIGHTS, N=256, rows=P, Hq=1 << 20, Hkv=1)) == UNSUPPORTED
+    assert f(*_args(WEIGHTS, T_max=256, N=1, Hq=1 << 20, Hkv=1)) == UNSUPPORTED
+    assert f(*_args(WEIGHTS, B=1 << 22, L_max=16)) == UNSUPPORTED                # a workgroup a kv head
     assert f(*_args(WEIGHTS, B=1 << 16, Hkv=8, L_max=1 << 13, max_pages=1 << 9, stride=1 << 13)) == UNSUPPORTED
 
 

@@ -59,6 +59,9 @@ def test_norm_rope_strides(lib):  # noqa: F811
     adapld.qk_norm_rope(q[:, ::2], k[:, ::2], f, i32([0, 1]))
     assert [a[2:6] for _, a in lib.calls] == [(5 * 768, 768, 5 * 768, 768), (5 * 768, 2 * 768, 5 * 768, 2 * 768)]
     assert lib.calls[0][1][12:19] == (2, 5, 4, 1, 128, 64, 0)
+    one = torch.empty_strided((1, 1, 4, 128), (3, 5, 128, 1), dtype=torch.bfloat16)
+    adapld.qk_norm_rope(one, one[:, :, :1], f, i32([0]))
+    assert lib.calls.pop()[1][2:6] == (0, 0, 0, 0)          # strides of single entries mean nothing
     for bad in (dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), dict(k=bf16(2, 4, 1, 128)), dict(q=q.float()),
                 dict(freqs=f.int()), dict(q_weight=bf16(64)), dict(offsets=i32([[0, 1]])), dict(base=i32([1]))):
         with pytest.raises(AdapldError):
