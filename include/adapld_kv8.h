@@ -34,7 +34,9 @@ extern "C" {
  * with the position p = base[b] + offsets[b, u], or base[b] + u without offsets
  * (the sum in 64 bits; p may be negative).  The other dimensions are y.  p * freqs
  * is exact modulo one turn, however far the position.  All of it is computed in
- * fp32 and rounded to bf16 once.  A row's infinities and NaN stay in it.
+ * fp32 and rounded to bf16 once (a mean of squares that leaves fp32's range, as with
+ * magnitudes above 2^60, or below 2^-60 where eps is 0, makes no norm).  A row's
+ * infinities and NaN stay in it.
  *
  *   q, k        bf16, token u of sequence b at q + b * q_batch + u * q_token (in
  *               elements, multiples of 8): its heads [Hq, D] or [Hkv, D], dense
@@ -158,7 +160,7 @@ int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const
  *       exp(scale * q[b, u, h] . k[b, g, j] - lse[b, h, u])
  * and positions[b, g, lens_old[b] + i] = first_position[b] + i.  Other entries are
  * left as they are.  A row whose u is outside [0, T_max) and a head whose lse is -inf
- * (a row without any key) give nothing.
+ * (a row without any key) or NaN give nothing, whatever q holds there.
  *
  *   q           bf16 [B, T_max, Hq, D]  as the attention took it
  *   lse         fp32 [B, Hq, T_max]     as the attention wrote it
@@ -168,8 +170,8 @@ int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const
  *   L_max       an upper bound of the lengths, at most max_pages * page_size and
  *               at most stride
  *   weights_out fp32 [B, Hkv, stride] (out); weights itself, or no overlap
- * Sums are fp32, in an order that the sizes fix.  q, the keys and scale * q.k *
- * log2(e) are finite, lse finite or -inf.
+ * Sums are fp32, in an order that the sizes fix.  Of the heads that give, q, the keys
+ * and scale * q.k * log2(e) are finite.
  *
  * Errors: NULL_ARG; INVALID_ARG for B < 0, Hq % Hkv != 0, non-positive sizes, N > T_max
  * without rows, L_max > max_pages * page_size or stride, a page_size other than the

@@ -146,9 +146,10 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
   for (int rb = 0; rb < RB; ++rb) {
     const RowAt x = row_at(a, b, g, n, 16 * rb + col);
     const uint4* const p = reinterpret_cast<const uint4*>(query_of(a, b, x));
+    const bool gives = lse2_of(a, b, x) < INFINITY;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)   // a row that is none must not bring a NaN
-      q[rb][j] = __builtin_bit_cast(bf16x8_t, x.in ? p[8 * (j >> 1) + 2 * quad + (j & 1)] : make_uint4(0, 0, 0, 0));
+    for (int j = 0; j < 4; ++j)   // a row that gives nothing must not bring a NaN
+      q[rb][j] = __builtin_bit_cast(bf16x8_t, gives ? p[8 * (j >> 1) + 2 * quad + (j & 1)] : make_uint4(0, 0, 0, 0));
 #pragma unroll
     for (int t = 0; t < 4; ++t) lse2[rb][t] = lse2_of(a, b, row_at(a, b, g, n, 16 * rb + 4 * quad + t));
   }
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
   constexpr int kRows = 32 * kParts;               // rows of a round
   constexpr int kLoads = 8 / KG;                   // of a wave for a round
   __shared__ __attribute__((aligned(1024))) uint8_t s_rows[kStages][kRows * kRowBytes];
-  __shared__ int s_at[kMaxRows];       // query of a row, in rows of q behind the sequence's first; -1: none
+  __shared__ int s_at[kMaxRows];       // query of a row, in rows of q behind the sequence's first; -1: it gives nothing
   __shared__ float s_lse2[kMaxRows];
   __shared__ int s_any;
   const AttnWeightsCall& c = a.c;
@@ -275,13 +276,14 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
     for (int i = 0; i < kMaxRows / kWideThreads; ++i) {
       const int r = tid + i * kWideThreads;
       if (r < rounds * kRows) {
-        s_at[r] = x[i].in ? x[i].u * c.Hq + x[i].h : -1;
+        const bool gives = lse2[i] < INFINITY;
+        s_at[r] = gives ? x[i].u * c.Hq + x[i].h : -1;
         s_lse2[r] = lse2[i];
-        if (x[i].in) s_any = x[i].u * c.Hq + x[i].h;
+        if (gives) s_any = x[i].u * c.Hq + x[i].h;
       }
     }
     __syncthreads();
-    // A row that is none takes the place of one that is some, with an infinite log-sum-
+    // A row that gives nothing takes the place of one that does, with an infinite log-sum-
     // exp: what its own place in q holds may be no number.
     const int any = s_any;
     // A wave brings kLoads KiB of a round, four rows a load; behind the last round that

@@ -134,6 +134,31 @@ def test_weights_ignore_what_is_no_row(T, Hq, Hkv):
     assert torch.equal(call(), want)
 
 
+@pytest.mark.parametrize("T, Hq, Hkv", [(4, 4, 4), (5, 4, 2), (20, 8, 1), (70, 4, 2), (256, 2, 2)])
+def test_weights_ignore_rows_without_keys(T, Hq, Hkv):
+    """Heads whose log-sum-exp is -inf, or no number, give nothing, whatever their queries
+    hold; a sequence may have no others."""
+    rng = np.random.default_rng(T)
+    new, old = [300, 300], [300 - T, 300 - T]
+    cache, _, _ = filled(new, 16, Hkv, rng)
+    q = bf16(rng.standard_normal((2, T, Hq, 128))).cuda()
+    lse = torch.full((2, Hq, T), 6.0, device="cuda")
+    off = torch.from_numpy(rng.random((Hq, T)) < 0.4).cuda()
+    lse[0][off] = -math.inf
+    lse[1] = -math.inf
+    w, p = torch.rand((2, Hkv, 304), device="cuda"), torch.zeros((2, Hkv, 304), dtype=torch.int32, device="cuda")
+    call = lambda: adapld.kv8_attn_weights(cache, q, lse, i32(old), i32(new), i32([0, 0]), w, p,  # noqa: E731
+                                           weights_out=torch.zeros_like(w))[0]
+    want = call()
+    assert torch.isfinite(want).all()
+    assert torch.equal(want[1, :, :old[1]], w[1, :, :old[1]]) and (want[1, :, old[1]:] == 0).all()
+    q[0][off.T] = math.nan
+    q[1] = math.inf
+    assert torch.equal(call(), want)
+    lse[lse == -math.inf] = math.nan
+    assert torch.equal(call(), want)
+
+
 def test_weights_long_and_clamped():
     """Longer than one workgroup takes, several sequences; lengths outside are clamped."""
     rng = np.random.default_rng(5)
