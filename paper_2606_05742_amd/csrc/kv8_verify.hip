@@ -1,5 +1,14 @@
 // Tree-masked verify attention over the paged 8-bit K/V cache: the kernels of
 // paged_verify.h for rows of E4M3 codes with a scale for each 16 tokens.
+//
+// Where it stands, us a call: single tokens, 32 x 8192 keys of 8 heads, 93 (538 MB, 5.8
+// TB/s: the reads).  16 x 8192, 52 nodes, 32 heads over 8, 142 (0.79 PFLOP/s, of which the
+// merge 9), some 8 % behind 4-bit rows: twice the bytes and the same products beside the
+// same vector instructions.  Left out there one at a time (of 146): the codes' loads 123,
+// the exponentials 133, the conversions 146.  Four tiles of codes in flight, and products
+// and exponentials in chunks kept apart by scheduling barriers, changed nothing.  One
+// sequence, 32 heads, 517 keys: 9.2, of which 4.7 a launch with a step of keys; a CU
+// brings the rest at 31 bytes a ns.
 #include "kv8_device.h"
 #include "paged_verify.h"
 
@@ -27,6 +36,11 @@ struct Kv8Format {
 
 }  // namespace
 
+// The units of the 4-bit cache's plan, whose choices are the best here too, us a call:
+// 24 x 6007 keys of 4 heads at most, 56 nodes of 28 heads, 256 rows in 2 splits 93, in 3
+// 100, 128 rows unsplit 103; 16 x 8192 keys of 8 heads, 52 nodes of 32, 256 rows in 2 splits
+// 143, in 3 168, 128 rows unsplit 154; single tokens, 1 x 4096 keys of 8 heads, as planned
+// 13.9, 8 splits 14.8, 16 13.6; 44 nodes there, 13 splits 21.5, 12 24.2.
 VerifyPagedPlan plan_verify_kv8(int B, int L_max, int T_max, int Hq, int Hkv) {
   static const PagedShape shapes[] = {{16, true, kWaves * kStep, 5.5, 1.3, 1.3},
                                       {32, true, kWaves * kStep, 5.5, 2.0, 2.0},

@@ -6,6 +6,11 @@
 // matrix products, and a weight 2^(s scale log2(e) - lse log2(e)).  One wave (or one
 // workgroup's waves in a fixed order) sums up all that a key gets, so the order of a
 // sum does not depend on the launch.
+//
+// Where it stands: single tokens, 32 x 8192 keys of 8 heads, read 286 MB in 57 us, 5.0
+// TB/s.  256 new rows of 28 heads over 4: 4 x 4096 keys 41 us, 0.73 PFLOP/s, the
+// exponentials beside the products; 4 x 6007 at most, two thirds of
+// it tokens, 64 us, in part-filled rounds of workgroups over the CUs.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
