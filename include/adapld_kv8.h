@@ -125,7 +125,9 @@ int adapld_kv8_append(const uint16_t* k_new, const uint16_t* v_new, const int32_
  * Everything is as in adapld_tree_verify_attn_kv4 (arguments, single tokens without
  * a tree, rows without any key, which entries and rows may hold anything, what has
  * to be finite, how weights are rounded, limits and errors), but for the cache's
- * format; the workspace is that of ADAPLD_OP_TREE_VERIFY_ATTN_KV8.
+ * format; the workspace is that of ADAPLD_OP_TREE_VERIFY_ATTN_KV8.  Where a sequence's
+ * kv head holds a NaN below its length, the results of that head are unspecified, and
+ * no other's.
  */
 int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const uint8_t* k_scales,
                                 const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* page_table,
