@@ -36,15 +36,19 @@ struct Kv8Format {
 
 }  // namespace
 
-// The units of the 4-bit cache's plan, whose choices are the best here too, us a call:
-// 24 x 6007 keys of 4 heads at most, 56 nodes of 28 heads, 256 rows in 2 splits 93, in 3
-// 100, 128 rows unsplit 103; 16 x 8192 keys of 8 heads, 52 nodes of 32, 256 rows in 2 splits
-// 143, in 3 168, 128 rows unsplit 154; single tokens, 1 x 4096 keys of 8 heads, as planned
-// 13.9, 8 splits 14.8, 16 13.6; 44 nodes there, 13 splits 21.5, 12 24.2.
+// What the constants were fitted to, us a call in a graph at the choice / at others, 32
+// heads over 8 unless said: single tokens, 1 x 517 keys unsplit 9.1 / in 3 9.2 (and a
+// launch more for the host); 1 x 1024 in 4 9.1 / unsplit 12.6; 8 x 1024 in 4 11.0 /
+// unsplit 13.6; 1 x 8192 in 16 14.1 / in 32 15.4; 16 x 8192 in 2 53 / unsplit 66, in 4
+// 57.  8 nodes: 1 x 768 in 3 12.9 / unsplit 15.5; 16 nodes: 1 x 384 in 3 12.7 / unsplit
+// 15.8, 1 x 4096 in 16 18.2 / in 32 20.8.  Over 175 sizes the choice is 0.5 % behind the
+// best on average (16 at most); over 87 of tiles 1.5 (13).  Tiles, with the 4-bit cache's constants: 16 x 8192, 52
+// nodes 256 rows in 2 143 / in 4 156, 128 rows unsplit 164; 24 x 6007 at most, 28 over 4,
+// 35 nodes 256 in 2 93 / in 3 100, 128 unsplit 103; 1 x 4096 128 in 13 25.9 / in 8 24.6.
 VerifyPagedPlan plan_verify_kv8(int B, int L_max, int T_max, int Hq, int Hkv) {
-  static const PagedShape shapes[] = {{16, true, kWaves * kStep, 5.5, 1.3, 1.3},
-                                      {32, true, kWaves * kStep, 5.5, 2.0, 2.0},
-                                      {64, true, kWaves / 2 * kStep, 5.5, 1.7, 1.7},
+  static const PagedShape shapes[] = {{16, true, kWaves * kStep, 5.3, 1.75, 1.75, 2.7, 0.2, true},
+                                      {32, true, kWaves * kStep, 8.9, 1.8, 1.8, 2.7, 0.2, true},
+                                      {64, true, kWaves / 2 * kStep, 10.4, 1.77, 1.77, 2.5, 0.25, true},
                                       {128, false, kKeyTile, 10.0, 1.12, 1.12},
                                       {256, false, kKeyTile, 10.0, 1.9, 1.12}};
   return plan_paged(shapes, B, L_max, T_max, Hq, Hkv);

@@ -924,13 +924,14 @@ __global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs 
     u32x4_t k[2][F::kLoads], v[2][F::kLoads];
     uint32_t ke[2], ve[2];
   };
-  auto load = [&](int s, Raw& r) {
+  auto load = [&](int s, Raw& r, bool used = true) {
     const int k0 = c0 + s * kStep, at = ((s - slice) / kSlices) & 63;
+    const int part = used ? quad : 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       // Keys behind the last read the last one again; their logits are masked.
       int pos = k0 + 16 * i;
-      uint32_t key = col;
+      uint32_t key = used ? col : 0;
       int page = __builtin_amdgcn_readlane(ids[i], at);
       if (pos + 16 > c1) {
         if (pos >= c1) {
@@ -941,21 +942,21 @@ __global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs 
       }
       const size_t row = pool_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
 #pragma unroll
-      for (int n = 0; n < F::kLoads; ++n) r.k[i][n] = load_codes<STREAM>(c.k_codes + row * F::kCodeBytes + F::code_at(key, quad, n));
+      for (int n = 0; n < F::kLoads; ++n) r.k[i][n] = load_codes<STREAM>(c.k_codes + row * F::kCodeBytes + F::code_at(key, part, n));
 #pragma unroll
-      for (int n = 0; n < F::kLoads; ++n) r.v[i][n] = load_codes<STREAM>(c.v_codes + row * F::kCodeBytes + F::code_at(key, quad, n));
-      r.ke[i] = F::load_scale(c.k_scales, row, key, quad);
-      r.ve[i] = F::load_scale(c.v_scales, row, key, quad);
+      for (int n = 0; n < F::kLoads; ++n) r.v[i][n] = load_codes<STREAM>(c.v_codes + row * F::kCodeBytes + F::code_at(key, part, n));
+      r.ke[i] = F::load_scale(c.k_scales, row, key, part);
+      r.ve[i] = F::load_scale(c.v_scales, row, key, part);
     }
   };
   // Codes of step s + 2 * kSlices, once r's are used; behind the wave's last step
-  // that one again, so that the number of loads in flight does not depend on
+  // a line of that one, so that the number of loads in flight does not depend on
   // a branch (the wait for a step's codes would then be one for all).
   const int last = slice + (n_ctx - 1 - slice) / kSlices * kSlices;
   auto load_later = [&](int s, Raw& r) {
     const int later = min(s + 2 * kSlices, last);
     if ((later - slice) / kSlices % 64 == 0) load_ids((later - slice) / kSlices);
-    load(later, r);
+    load(later, r, s + 2 * kSlices <= last);
   };
   // V rows of a context step to buffer `buf`, and its S.
   auto begin_ctx = [&](Raw& r, int buf, typename ROWS::Logits& s) {
@@ -1163,12 +1164,16 @@ __global__ __launch_bounds__(kCombineThreads) void paged_combine_kernel(const Pa
 
 // A shape of the kernels and its cost in us: a workgroup (one a CU) takes a
 // start-up and a time per unit of keys, which for the 256-row shape depends on
-// whether some SIMD has two row blocks.
+// whether some SIMD has two row blocks; the merge of a split context a time of its own
+// and one for each split.  With `parts` a whole context is charged for the part of its
+// last unit that it fills.
 struct PagedShape {
   int rows;       // stacked rows per workgroup
   bool narrow;    // up to 64 rows: the shape that just holds them
   int unit;       // keys of a step of the workgroup
   double start, per_unit, per_unit_half;   // the latter where at most half the rows live
+  double merge = 5.0, per_split = 0.0;
+  bool parts = false;
 };
 
 // The shape and the number of context splits with the least estimated time.  A call
@@ -1177,7 +1182,7 @@ struct PagedShape {
 template <int N>
 VerifyPagedPlan plan_paged(const PagedShape (&shapes)[N], int B, int L_max, int T_max, int Hq, int Hkv) {
   constexpr int kCUs = 256;
-  constexpr double kCombine = 5.0, kPartialBytesPerUs = 6e6;
+  constexpr double kPartialBytesPerUs = 6e6;
   const int rows_max = T_max * (Hq / Hkv);
   const int64_t pairs = (int64_t)B * Hkv;
   VerifyPagedPlan best{};
@@ -1203,9 +1208,10 @@ VerifyPagedPlan plan_paged(const PagedShape (&shapes)[N], int B, int L_max, int 
       if (nsplit != want && want > least) continue;   // the same split as a smaller count
       const int64_t wgs = pairs * rowgroups * nsplit;
       const double rounds = (double)((wgs + kCUs - 1) / kCUs);
-      double cost = std::max(rounds * (s.start + mean * (per + beside)), s.start + longest * (per + beside));
+      const double taken = (s.parts && nsplit == 1 ? (double)L_max / s.unit : per) + beside;
+      double cost = std::max(rounds * (s.start + mean * taken), s.start + longest * taken);
       if (nsplit > 1)
-        cost += kCombine + (double)(pairs * nsplit) * rows_max * 2 * (kD * 4 + 8) / kPartialBytesPerUs;
+        cost += s.merge + s.per_split * nsplit + (double)(pairs * nsplit) * rows_max * 2 * (kD * 4 + 8) / kPartialBytesPerUs;
       if (best.rows == 0 || cost < best_cost) {
         best_cost = cost;
         best = VerifyPagedPlan{rows_max, s.rows, rowgroups, nsplit, per * s.unit};
