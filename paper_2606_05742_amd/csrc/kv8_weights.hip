@@ -56,10 +56,6 @@ __device__ __forceinline__ float lse2_of(const WeightsArgs& a, int b, const RowA
   const float lse = a.c.lse[((size_t)b * a.c.Hq + x.h) * a.c.T_max + x.u];
   return x.in && lse > -INFINITY ? lse * kLog2e : INFINITY;
 }
-__device__ __forceinline__ const uint16_t* query_of(const WeightsArgs& a, int b, const RowAt& x) {
-  return a.c.q + (((size_t)b * a.c.T_max + x.u) * a.c.Hq + x.h) * kD;
-}
-
 __device__ __forceinline__ bf16x8_t operand(uint32_t lo, uint32_t hi, float X) {
   return __builtin_bit_cast(bf16x8_t, kv8_values(make_uint2(lo, hi), X));
 }
@@ -82,11 +78,11 @@ __device__ __forceinline__ float add_lane_xor16(float v) {
 constexpr int kNarrowThreads = 256;
 constexpr int kNarrowWaves = kNarrowThreads / kWave;
 constexpr int kStep = 32;
-constexpr int kMaxSteps = 8;   // of a wave
+constexpr int kMaxSteps = 16;   // of a wave
 static_assert(kMaxSteps <= kWave, "a lane for each step's page ids");
 
 template <int RB>
-__global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(const WeightsArgs a) {
+__global__ __launch_bounds__(kNarrowThreads, RB == 1 ? 4 : RB == 2 ? 3 : 2) void kv8_weights_narrow_kernel(const WeightsArgs a) {
   const AttnWeightsCall& c = a.c;
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
   const int b = bg / c.Hkv, g = bg - b * c.Hkv;
@@ -114,13 +110,18 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
     uint32_t e[2];
     float w;   // of key k0 + lane, lanes 0..31
   };
+  // Step s; behind the wave's last step a line of that one, so that the number of loads in
+  // flight does not depend on a branch.
+  const int last = wave + (steps - 1 - wave) / kNarrowWaves * kNarrowWaves;
   auto load = [&](int s, Raw& r) {
-    const int k0 = c0 + s * kStep, at = (s - wave) / kNarrowWaves;
+    const bool used = s <= last;
+    s = min(s, last);
+    const int k0 = c0 + s * kStep, at = (s - wave) / kNarrowWaves, part = used ? quad : 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       // Keys behind the last read the last one again; their sums are not stored.
       int pos = k0 + 16 * i;
-      uint32_t key = col;
+      uint32_t key = used ? col : 0;
       int page = __builtin_amdgcn_readlane(ids[i], at);
       if (pos + 16 > c1) {
         if (pos >= c1) {
@@ -131,36 +132,37 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
       }
       const size_t row = pool_row(page, g, pos & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
       const uint8_t* const p = c.k_codes + row * kKv8RowBytes;
-      r.k[i][0] = load16(p + key * kKv8RowBytes + quad * 16);
-      r.k[i][1] = load16(p + key * kKv8RowBytes + quad * 16 + 64);
+      r.k[i][0] = load16(p + key * kKv8RowBytes + part * 16);
+      r.k[i][1] = load16(p + key * kKv8RowBytes + part * 16 + 64);
       r.e[i] = c.k_scales[row >> kKv8BlockShift];
     }
     r.w = w_in[min(k0 + (lane & 31), max(old - 1, 0))];
   };
-  // Codes of the third next step; behind the wave's last step that one again, so that
-  // the number of loads in flight does not depend on a branch.
-  const int last = wave + (steps - 1 - wave) / kNarrowWaves * kNarrowWaves;
   Raw r[3];
   load(wave, r[0]);
-  load(min(wave + kNarrowWaves, last), r[1]);
-  load(min(wave + 2 * kNarrowWaves, last), r[2]);
+  load(wave + kNarrowWaves, r[1]);
+  load(wave + 2 * kNarrowWaves, r[2]);
 
+  // Lane r looks row r up for all.
+  const RowAt mine = row_at(a, b, g, n, lane);
+  const float my_lse2 = lse2_of(a, b, mine);
+  const int my_place = my_lse2 < INFINITY ? mine.u * c.Hq + mine.h : -1;
   bf16x8_t q[RB][4];
   float lse2[RB][4];
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const RowAt x = row_at(a, b, g, n, 16 * rb + col);
-    const uint4* const p = reinterpret_cast<const uint4*>(query_of(a, b, x));
-    const bool gives = lse2_of(a, b, x) < INFINITY;
+    const int place = __shfl(my_place, 16 * rb + col, kWave);
+    const uint4* const p = reinterpret_cast<const uint4*>(c.q + ((size_t)b * c.T_max * c.Hq + max(place, 0)) * kD);
 #pragma unroll
     for (int j = 0; j < 4; ++j)   // a row that gives nothing must not bring a NaN
-      q[rb][j] = __builtin_bit_cast(bf16x8_t, gives ? p[8 * (j >> 1) + 2 * quad + (j & 1)] : make_uint4(0, 0, 0, 0));
+      q[rb][j] = __builtin_bit_cast(bf16x8_t, place >= 0 ? p[8 * (j >> 1) + 2 * quad + (j & 1)] : make_uint4(0, 0, 0, 0));
 #pragma unroll
-    for (int t = 0; t < 4; ++t) lse2[rb][t] = lse2_of(a, b, row_at(a, b, g, n, 16 * rb + 4 * quad + t));
+    for (int t = 0; t < 4; ++t) lse2[rb][t] = __shfl(my_lse2, 16 * rb + 4 * quad + t, kWave);
   }
 
   auto step = [&](int s, Raw& x) {
     const int k0 = c0 + s * kStep;
+    const bool plain = k0 + kStep <= old;
     float sum[2];
     const float w = x.w;
 #pragma unroll
@@ -182,13 +184,13 @@ __global__ __launch_bounds__(kNarrowThreads) void kv8_weights_narrow_kernel(cons
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           float e = __builtin_amdgcn_exp2f(fmaf(z[rb][t], a.sl2, -lse2[rb][t]));
-          if (k0 + kStep > old)   // a new row sees no later one
-            e = k0 + 16 * i + col <= old + (16 * rb + 4 * quad + t) / a.G ? e : 0.f;
+          if (!plain)   // a new row sees no later one
+            e = k0 + 16 * i + col <= old + __shfl(mine.i, 16 * rb + 4 * quad + t, kWave) ? e : 0.f;
           p[t] += e;
         }
       sum[i] = (p[0] + p[1]) + (p[2] + p[3]);
     }
-    load(min(s + 3 * kNarrowWaves, last), x);
+    load(s + 3 * kNarrowWaves, x);
     // lanes 0..15 and 16..31 take the sums of either half
     const float v0 = add_lane_xor32(add_lane_xor16(sum[0])), v1 = add_lane_xor32(add_lane_xor16(sum[1]));
     const float v = n == 0 ? 0.f : quad & 1 ? v1 : v0;   // without rows nothing is known of the keys
@@ -468,12 +470,33 @@ hipError_t launch_kv8_attn_weights(const AttnWeightsCall& c, hipStream_t stream)
     else wide(Two{}, Four{});
     return hipGetLastError();
   }
-  // Steps of a wave: up to 8, fewer while there are not 1024 workgroups (32 x 8192 keys of
-  // 8 heads, single tokens: 58 us with 8 to 32 steps, 62 to 65 with two steps in flight
-  // or non-temporal loads).
+  // Steps of a wave by the least estimated time in us: at least a wave's own latency, start
+  // and steps, and at least what all workgroups take, `at_once` of them at a time.  us a
+  // call at the choice / with steps for 1024 workgroups, 8 at most: single tokens of 32
+  // heads over 8, 32 x 8192 56.7 / 57.8, 4 x 12000 14.4 / 16.0, 13 x 4087 14.9 / 18.0; 28
+  // rows, 13 x 4087 12.8 / 17.1; 42 rows, 13 x 4087 16.1 / 25.0; 52 rows, 32 x 4087 36.7 /
+  // 47.2.  Over 80 sizes it is 2 % behind the best number of steps on average (15 on these
+  // sizes by the other rule).
+  struct Cost {
+    double start, step, base, group, group_step;
+    int at_once, most;
+  };
+  static const Cost costs[] = {{4.0, 0.65, 2.3, 2.2, 1.75, 1024, 8},        // up to 16 rows
+                               {4.7, 0.95, 3.3, 2.5, 1.7, 768, kMaxSteps},   // 32
+                               {5.7, 1.2, 5.6, 2.9, 1.9, 512, kMaxSteps}};   // 64
+  const Cost& k = costs[rows <= 16 ? 0 : rows <= 32 ? 1 : 2];
   constexpr int kUnit = kNarrowWaves * kStep;
   const int units = (c.L_max + kUnit - 1) / kUnit;
-  const int per = (int)std::min<int64_t>(kMaxSteps, std::max<int64_t>(1, pairs * units / 1024));
+  int per = 1;
+  double least = 0.0;
+  for (int p = 1; p <= k.most; ++p) {
+    const double groups = (double)(pairs * ((units + p - 1) / p));
+    const double t = std::max(k.start + k.step * p, k.base + groups / k.at_once * (k.group + k.group_step * p));
+    if (p == 1 || t < least) {
+      least = t;
+      per = p;
+    }
+  }
   a.chunk = per * kUnit;
   a.nsplit = (units + per - 1) / per;
   auto narrow = [&](auto rb) {
