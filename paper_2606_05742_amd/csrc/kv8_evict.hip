@@ -27,7 +27,7 @@ namespace {
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectWaves = kSelectThreads / kWave;
 constexpr int kBins = 2048;
-constexpr int kCopies = 4;             // of the histogram: weights crowd in few bins
+constexpr int kCopies = 4;             // of a histogram: weights crowd in few bins
 constexpr int kFewMoves = 64;          // moved beside the selection
 constexpr int kMoveThreads = 256;
 constexpr int kMoveWaves = kMoveThreads / kWave;
@@ -53,25 +53,22 @@ __device__ __forceinline__ uint32_t ordered_bits(float w) {
 }
 __device__ __forceinline__ float weight_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-// Exclusive prefix sum over the workgroup; `total` is the sum.
-__device__ __forceinline__ int block_excl_scan(int v, int* s_wave, int& total) {
-  const int in = wave_incl_scan_i32(v);
-  if (lane_id() == kWave - 1) s_wave[threadIdx.x / kWave] = in;
-  __syncthreads();
-  int before = 0, sum = 0;
-#pragma unroll
-  for (int w = 0; w < kSelectWaves; ++w) {
-    before += w < (int)(threadIdx.x / kWave) ? s_wave[w] : 0;
-    sum += s_wave[w];
-  }
-  __syncthreads();
-  total = sum;
-  return in - v + before;
+// The sum of the first n counts of the waves, on every lane.
+__device__ __forceinline__ int sum_of_waves(const int* counts, int n) {
+  static_assert(kSelectWaves == 16, "a row of lanes");
+  int v = lane_id() % 16 < n ? counts[lane_id() % 16] : 0;
+  v += __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, false);   // row_ror:8, 4, 2, 1
+  v += __builtin_amdgcn_mov_dpp(v, 0x124, 0xf, 0xf, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x122, 0xf, 0xf, false);
+  v += __builtin_amdgcn_mov_dpp(v, 0x121, 0xf, 0xf, false);
+  return __builtin_amdgcn_readfirstlane(v);
 }
 
 // One block of kept slots takes its rows: lane r < 16 (and those 16, 32, 48 behind it)
 // gives the slot that row r comes from, the row itself where it stays.  16 lanes a row,
 // four rows at a time.  Rows of a smaller scale than the largest are rounded again.
+// EAGER: rows that stay are read with the others, not when their scale asks for it.
+template <bool EAGER>
 __device__ __forceinline__ void move_block(const EvictCall& c, int b, int g, int slot0, int src, int page_shift) {
   const int lane = lane_id(), part = lane % kKv8RowLanes, sub = lane / kKv8RowLanes;
   const int32_t* const table = c.page_table + (size_t)b * c.max_pages;
@@ -89,7 +86,7 @@ __device__ __forceinline__ void move_block(const EvictCall& c, int b, int g, int
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       x[n][t] = make_uint2(0, 0);
-      if (from_r[t] != to + 4 * t + sub) x[n][t] = *reinterpret_cast<const uint2*>(c.codes[n] + from_r[t] * kKv8RowBytes + part * 8);
+      if (EAGER || from_r[t] != to + 4 * t + sub) x[n][t] = *reinterpret_cast<const uint2*>(c.codes[n] + from_r[t] * kKv8RowBytes + part * 8);
     }
   }
 #pragma unroll
@@ -100,7 +97,7 @@ __device__ __forceinline__ void move_block(const EvictCall& c, int b, int g, int
       const int r = 4 * t + sub, e_r = __shfl(e[n], r, kWave);
       const bool comes = from_r[t] != to + r;
       uint2* const at = reinterpret_cast<uint2*>(c.codes[n] + (to + r) * kKv8RowBytes + part * 8);
-      if (e_r != most) *at = kv8_rescale(comes ? x[n][t] : *at, e_r, most);
+      if (e_r != most) *at = kv8_rescale(EAGER || comes ? x[n][t] : *at, e_r, most);
       else if (comes) *at = x[n][t];
     }
     if (lane == 0) c.scales[n][to >> kKv8BlockShift] = (uint8_t)most;
@@ -112,8 +109,8 @@ __device__ __forceinline__ void move_block(const EvictCall& c, int b, int g, int
 // workspace.
 template <int R, bool FEW>
 __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const EvictCall c, int page_shift) {
-  __shared__ int s_hist[kCopies][kBins];
-  __shared__ int s_wave[kSelectWaves];
+  __shared__ __attribute__((aligned(16))) int s_hist[2][kCopies][kBins];
+  __shared__ int s_wave[kSelectWaves], s_protects[kSelectWaves];
   __shared__ int s_count[R][kSelectWaves];
   __shared__ int s_pick[3];
   __shared__ int s_free[FEW ? kFewMoves : 1], s_from[FEW ? kFewMoves : 1];
@@ -137,7 +134,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
     }
     return;
   }
-  const int64_t since = (int64_t)c.next_position[b] - c.recent;
+  const int since = (int)max((int64_t)c.next_position[b] - c.recent, (int64_t)INT32_MIN);
 
   constexpr int kChunk = R * kSelectThreads;
   uint32_t key[R];
@@ -151,12 +148,15 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
       pos[i] = p_in[j];
     }
   };
+  // Whether any lane of the wave has an i-th slot.
+  auto live = [&](int j0, int i) { return j0 + i * kSelectThreads + wave * kWave < L; };
   // f(slot, i) for the thread's slots.
   auto each = [&](bool reload, auto&& f) {
     for (int j0 = 0; j0 < L; j0 += kChunk) {
       if (reload) load(j0);
 #pragma unroll
       for (int i = 0; i < R; ++i) {
+        if (!live(j0, i)) break;
         const int j = j0 + i * kSelectThreads + tid;
         if (j < L) f(j, i);
       }
@@ -164,39 +164,51 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
   };
 
   // The protected tokens stay, and of the others as many as there is room for; where
-  // they alone are too many, as many of them.
-  for (int i = tid; i < kCopies * kBins; i += kSelectThreads) s_hist[0][i] = 0;
-  int mine = 0, protects;
-  each(true, [&](int, int i) { mine += pos[i] >= since; });
-  block_excl_scan(mine, s_wave, protects);
-  const bool among = protects >= c.budget;   // the choice is among the protected ones
-  int want = among ? c.budget : c.budget - protects;
-
-  // The want-th largest weight of those, by digits of 11, 11 and 10 bits.
+  // they alone are too many, as many of them.  The want-th largest weight of those, by
+  // digits of 11, 11 and 10 bits: the first one's histogram is made for both kinds,
+  // before it is known which is asked for.
+  if (resident) load(0);
+  for (int i = tid; i < 2 * kCopies * kBins / 4; i += kSelectThreads) reinterpret_cast<int4*>(s_hist)[i] = make_int4(0, 0, 0, 0);
+  __syncthreads();
+  bool among = false;   // the choice is among the protected ones
+  int want = 0;
   uint32_t found = 0, known = 0;   // its leading bits, and which those are
   int equal = 0;
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const uint32_t digit = pass == 2 ? kBins / 2 - 1 : kBins - 1;
+    int mine = 0;
     each(!resident, [&](int, int i) {
-      if ((pos[i] >= since) == among && (key[i] & known) == found)
-        atomicAdd(&s_hist[tid % kCopies][(key[i] >> shift) & digit], 1);
+      const bool kept = pos[i] >= since;
+      mine += kept;
+      if (pass == 0 || (kept == among && (key[i] & known) == found))
+        atomicAdd(&s_hist[pass == 0 && kept][tid % kCopies][(key[i] >> shift) & digit], 1);
     });
+    if (pass == 0) {
+      mine = wave_incl_scan_i32(mine);
+      if (lane == kWave - 1) s_protects[wave] = mine;
+    }
     __syncthreads();
-    // two bins a thread, the largest first; they are cleared for the next pass
+    if (pass == 0) {
+      const int protects = sum_of_waves(s_protects, kSelectWaves);
+      among = protects >= c.budget;
+      want = among ? c.budget : c.budget - protects;
+    }
+    // two bins a thread, the largest first; the first kind's are cleared for the next pass
     const int hi = kBins - 1 - 2 * tid;
     int n1 = 0, n0 = 0;
 #pragma unroll
     for (int k = 0; k < kCopies; ++k) {
-      int2* const at = reinterpret_cast<int2*>(&s_hist[k][hi - 1]);
-      const int2 n = *at;
+      const int2 n = *reinterpret_cast<const int2*>(&s_hist[pass == 0 && among][k][hi - 1]);
       n0 += n.x;
       n1 += n.y;
-      *at = make_int2(0, 0);
+      *reinterpret_cast<int2*>(&s_hist[0][k][hi - 1]) = make_int2(0, 0);
     }
-    int total;
-    const int above = block_excl_scan(n1 + n0, s_wave, total);
+    const int in = wave_incl_scan_i32(n1 + n0);
+    if (lane == kWave - 1) s_wave[wave] = in;
+    __syncthreads();
+    const int above = in - n1 - n0 + sum_of_waves(s_wave, wave);
     if (above < want && above + n1 + n0 >= want) {
       const bool first = above + n1 >= want;
       s_pick[0] = first ? hi : hi - 1;
@@ -246,6 +258,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
     if (want == equal) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
+        if (!live(j0, i)) break;
         const bool chosen = (pos[i] >= since) == among;
         if (chosen ? key[i] >= found : !among) kept |= 1u << i;
       }
@@ -253,6 +266,11 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
       uint32_t ranks[R];
 #pragma unroll
       for (int i = 0; i < R; ++i) {
+        ranks[i] = ~0u;
+        if (!live(j0, i)) {
+          if (lane == 0) s_count[i][wave] = 0;
+          continue;
+        }
         const int j = j0 + i * kSelectThreads + tid;
         const bool eq = j < L && (pos[i] >= since) == among && key[i] == found;
         const uint64_t m = __ballot(eq);
@@ -263,6 +281,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
       scan_counts(total);
 #pragma unroll
       for (int i = 0; i < R; ++i) {
+        if (!live(j0, i)) break;
         const bool chosen = (pos[i] >= since) == among;
         bool stays = chosen ? key[i] > found : !among;
         if (ranks[i] != ~0u) stays = equals + s_count[i][wave] + (int)ranks[i] < want;
@@ -275,6 +294,11 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
     int at[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
+      at[i] = 0;
+      if (!live(j0, i)) {
+        if (lane == 0) s_count[i][wave] = 0;
+        continue;
+      }
       const int j = j0 + i * kSelectThreads + tid;
       const bool in = j < L, stays = kept >> i & 1;
       const uint64_t f = __ballot(in && !stays && j < c.budget), m = __ballot(in && stays && j >= c.budget);
@@ -285,6 +309,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
     scan_counts(total);
 #pragma unroll
     for (int i = 0; i < R; ++i) {
+      if (!live(j0, i)) break;
       const int j = j0 + i * kSelectThreads + tid;
       if (j >= L) continue;
       const int before = s_count[i][wave];
@@ -303,6 +328,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < R; ++i) {
+      if (!live(j0, i)) break;
       const int j = j0 + i * kSelectThreads + tid;
       if (j >= L || j < c.budget || !(kept >> i & 1)) continue;
       const int k = moves + (s_count[i][wave] >> 16) + at[i];
@@ -327,7 +353,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv8_evict_select_kernel(const 
       int src = (block << kKv8BlockShift) + row;
       for (int m = k; m < moves && s_free[m] >> kKv8BlockShift == block; ++m)
         if (s_free[m] % ADAPLD_KV8_BLOCK == row) src = s_from[m];
-      move_block(c, b, g, block << kKv8BlockShift, src, page_shift);
+      move_block<true>(c, b, g, block << kKv8BlockShift, src, page_shift);
     }
   }
 }
@@ -346,7 +372,7 @@ __global__ __launch_bounds__(kMoveThreads) void kv8_evict_move_kernel(const Evic
   const int moved = *ws.moved, src = ws.src[slot0 + row];
   // without moves src holds anything
   if (moved == 0 || !__any(src != slot0 + row)) return;
-  move_block(c, b, g, slot0, src, page_shift);
+  move_block<false>(c, b, g, slot0, src, page_shift);
 }
 
 }  // namespace
