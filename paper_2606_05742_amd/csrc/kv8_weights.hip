@@ -35,27 +35,22 @@ struct WeightsArgs {
   float sl2;
 };
 
-// The stacked row's query, or none: rows behind the last, and those whose entry of
-// `rows` is no query.
+// Stacked row r of at most N * G: its new row i, the place of its query among the
+// sequence's, and its log-sum-exp in units of log2, infinite where the row gives nothing
+// (but for what the lengths say, which these loads do not wait for).
 struct RowAt {
-  int i, h, u;
-  bool in;
+  int i, place;
+  float lse2;
 };
-__device__ __forceinline__ RowAt row_at(const WeightsArgs& a, int b, int g, int n, int r) {
-  RowAt x;
-  const int rows = n * a.G, rr = max(min(r, rows - 1), 0);
-  x.i = rr / a.G;
-  x.h = g * a.G + (rr - x.i * a.G);
-  x.u = a.c.rows ? a.c.rows[(size_t)b * a.c.N + x.i] : x.i;
-  x.in = r < rows && x.u >= 0 && x.u < a.c.T_max;
-  x.u = x.in ? x.u : 0;
-  return x;
+__device__ __forceinline__ RowAt row_at(const WeightsArgs& a, int b, int g, int r) {
+  const AttnWeightsCall& c = a.c;
+  const int most = c.N * a.G, rr = min(r, most - 1), i = rr / a.G, h = g * a.G + (rr - i * a.G);
+  const int u = c.rows ? c.rows[(size_t)b * c.N + i] : i;
+  const bool in = u >= 0 && u < c.T_max;
+  const float lse = c.lse[((size_t)b * c.Hq + h) * c.T_max + (in ? u : 0)];
+  return {i, (in ? u : 0) * c.Hq + h, in && r < most && lse > -INFINITY ? lse * kLog2e : INFINITY};
 }
-// Its log-sum-exp in units of log2; infinite where the row gives nothing.
-__device__ __forceinline__ float lse2_of(const WeightsArgs& a, int b, const RowAt& x) {
-  const float lse = a.c.lse[((size_t)b * a.c.Hq + x.h) * a.c.T_max + x.u];
-  return x.in && lse > -INFINITY ? lse * kLog2e : INFINITY;
-}
+
 __device__ __forceinline__ bf16x8_t operand(uint32_t lo, uint32_t hi, float X) {
   return __builtin_bit_cast(bf16x8_t, kv8_values(make_uint2(lo, hi), X));
 }
@@ -97,6 +92,7 @@ __global__ __launch_bounds__(kNarrowThreads, RB == 1 ? 4 : RB == 2 ? 3 : 2) void
     const int pos = c0 + (wave + lane * kNarrowWaves) * kStep + 16 * i;
     ids[i] = page_in_pool(table[min(pos >> a.page_shift, c.max_pages - 1)], c.n_pages);
   }
+  const RowAt mine = row_at(a, b, g, lane);   // lane r looks row r up for all
   const int old = min(max(c.lens_old[b], 0), c.L_max);
   const int n = min(max(min(max(c.lens_new[b], 0), c.L_max) - old, 0), c.N);
   const int c1 = min(c0 + a.chunk, old + n);
@@ -143,10 +139,8 @@ __global__ __launch_bounds__(kNarrowThreads, RB == 1 ? 4 : RB == 2 ? 3 : 2) void
   load(wave + kNarrowWaves, r[1]);
   load(wave + 2 * kNarrowWaves, r[2]);
 
-  // Lane r looks row r up for all.
-  const RowAt mine = row_at(a, b, g, n, lane);
-  const float my_lse2 = lse2_of(a, b, mine);
-  const int my_place = my_lse2 < INFINITY ? mine.u * c.Hq + mine.h : -1;
+  const float my_lse2 = lane < n * a.G ? mine.lse2 : INFINITY;
+  const int my_place = my_lse2 < INFINITY ? mine.place : -1;
   bf16x8_t q[RB][4];
   float lse2[RB][4];
 #pragma unroll
@@ -274,19 +268,16 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
     __syncthreads();
     // all in flight together
     RowAt x[kMaxRows / kWideThreads];
-    float lse2[kMaxRows / kWideThreads];
 #pragma unroll
-    for (int i = 0; i < kMaxRows / kWideThreads; ++i) x[i] = row_at(a, b, g, n, first + min(tid + i * kWideThreads, rounds * kRows - 1));
-#pragma unroll
-    for (int i = 0; i < kMaxRows / kWideThreads; ++i) lse2[i] = lse2_of(a, b, x[i]);
+    for (int i = 0; i < kMaxRows / kWideThreads; ++i) x[i] = row_at(a, b, g, first + min(tid + i * kWideThreads, some - 1));
 #pragma unroll
     for (int i = 0; i < kMaxRows / kWideThreads; ++i) {
       const int r = tid + i * kWideThreads;
       if (r < rounds * kRows) {
-        const bool gives = lse2[i] < INFINITY;
-        s_at[r] = gives ? x[i].u * c.Hq + x[i].h : -1;
-        s_lse2[r] = lse2[i];
-        if (gives) s_any = x[i].u * c.Hq + x[i].h;
+        const bool gives = first + r < rows && x[i].lse2 < INFINITY;
+        s_at[r] = gives ? x[i].place : -1;
+        s_lse2[r] = gives ? x[i].lse2 : INFINITY;
+        if (gives) s_any = x[i].place;
       }
     }
     __syncthreads();
