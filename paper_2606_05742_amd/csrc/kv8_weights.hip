@@ -7,10 +7,11 @@
 // workgroup's waves in a fixed order) sums up all that a key gets, so the order of a
 // sum does not depend on the launch.
 //
-// Where it stands: single tokens, 32 x 8192 keys of 8 heads, read 286 MB in 57 us, 5.0
-// TB/s.  256 new rows of 28 heads over 4: 4 x 4096 keys 41 us, 0.73 PFLOP/s, the
-// exponentials beside the products; 4 x 6007 at most, two thirds of
-// it tokens, 64 us, in part-filled rounds of workgroups over the CUs.
+// Where it stands: single tokens, 32 x 8192 keys of 8 heads, read 286 MB in 54 us, 5.3
+// TB/s.  196 rows (28 new ones, 28 heads over 4), 16 x 8192 keys 38 us, 0.69 PFLOP/s; 1792
+// rows, 4 x 4096 keys 41 us, 0.73 PFLOP/s, the exponentials beside the products; 4 x 6007
+// at most, two thirds of it tokens, 64 us, in part-filled rounds of workgroups over the
+// CUs.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -221,6 +222,44 @@ constexpr int kMaxRows = 2048;           // rows whose places and log-sum-exps L
 // consecutive rows hit every bank once.
 __device__ __forceinline__ int swizzled(int r, int ch) { return r * kRowBytes + ((ch ^ (r & 15)) << 4); }
 
+// Four weights of 64 keys and 32 rows, value n4 of 8: to the sums of the lane's keys; rows
+// see the first `sees` + 1 keys, or with `plain` all.
+template <class PLAIN>
+__device__ __forceinline__ void add4(const WeightsArgs& a, float (&sum)[2][16], const f32x16_t (&z)[2], int n4, float lse2,
+                                     int sees, PLAIN) {
+  const int m = n4 / 4;
+#pragma unroll
+  for (int t = 4 * (n4 % 4); t < 4 * (n4 % 4) + 4; ++t) {
+    const float w = __builtin_amdgcn_exp2f(fmaf(z[m][t], a.sl2, -lse2));
+    if constexpr (PLAIN::value) sum[m][t] += w;
+    else sum[m][t] += 32 * m + 8 * (t >> 2) + (t & 3) <= sees ? w : 0.f;
+  }
+}
+
+// Sums over the 32 lanes of a half: out[key] of the 64 keys.  Values 16 lanes apart and 8
+// apart are added in pairs, each half of the lanes keeping one.
+__device__ __forceinline__ void sums_of_keys(const float (&sum)[2][16], float* out) {
+  const int lane = lane_id(), half = lane >> 5;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      float h[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {   // values t + 4 i and t + 4 i + 8, the latter where bit 4 of the lane is set
+        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_int(sum[m][t + 4 * i]), __float_as_int(sum[m][t + 4 * i + 8]), false, false);
+        h[i] = __int_as_float(w[0]) + __int_as_float(w[1]);
+      }
+      const bool up = lane & 8;       // h[1] where bit 3 is set
+      float v = (up ? h[1] : h[0]) + dpp_f32<0x128>(up ? h[0] : h[1]);   // row_ror:8
+      v += dpp_f32<0x141>(v);             // row_half_mirror
+      v += dpp_f32<0xb1>(v);              // quad_perm 1 0 3 2
+      v += dpp_f32<0x4e>(v);              // quad_perm 2 3 0 1
+      const int value = t + 4 * ((lane >> 3) & 1) + 8 * ((lane >> 4) & 1);
+      if ((lane & 7) == 0) out[32 * m + 8 * (value >> 2) + (value & 3) + 4 * half] = v;
+    }
+}
+
 template <int KG, int kParts>
 __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kernel(const WeightsArgs a) {
   constexpr int kWideThreads = KG * kParts * kWave;
@@ -323,15 +362,6 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
     auto operand_of = [&](int round, int d) {
       return *reinterpret_cast<const bf16x8_t*>(s_rows[round % kStages] + 32 * part * kRowBytes + swizzled(col, 8 * half + d));
     };
-    auto add4 = [&](const f32x16_t (&z)[2], int n4, float lse2, int sees, auto plain) {
-      const int m = n4 / 4;
-#pragma unroll
-      for (int t = 4 * (n4 % 4); t < 4 * (n4 % 4) + 4; ++t) {
-        const float w = __builtin_amdgcn_exp2f(fmaf(z[m][t], a.sl2, -lse2));
-        if constexpr (decltype(plain)::value) sum[m][t] += w;
-        else sum[m][t] += 32 * m + 8 * (t >> 2) + (t & 3) <= sees ? w : 0.f;
-      }
-    };
     // With NEXT the products of the next round, with ADD the exponentials of this one.
     auto round_of = [&](int i, f32x16_t (&z)[2], f32x16_t (&z_next)[2], auto plain, auto NEXT, auto ADD) {
       constexpr bool kNext = decltype(NEXT)::value, kAdd = decltype(ADD)::value;
@@ -357,7 +387,7 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
 #pragma unroll
           for (int m = 0; m < 2; ++m) z_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[m][d], q[d], z_next[m], 0, 0, 0);
         }
-        if constexpr (kAdd) add4(z, d, lse2, sees, plain);
+        if constexpr (kAdd) add4(a, sum, z, d, lse2, sees, plain);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -395,28 +425,9 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
     else run(std::false_type{});
     waitcnt_vm<0>();
   }
-  // Sums over the 32 lanes of a half, then of the waves of the same keys.  Values 16
-  // lanes apart and 8 apart are added in pairs, each half of the lanes keeping one.
   float* const s_sum = reinterpret_cast<float*>(s_rows);   // [waves][64 keys]
   __syncthreads();
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      float h[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {   // values t + 4 i and t + 4 i + 8, the latter where bit 4 of the lane is set
-        const auto w = __builtin_amdgcn_permlane16_swap(__float_as_int(sum[m][t + 4 * i]), __float_as_int(sum[m][t + 4 * i + 8]), false, false);
-        h[i] = __int_as_float(w[0]) + __int_as_float(w[1]);
-      }
-      const bool up = lane & 8;       // h[1] where bit 3 is set
-      float v = (up ? h[1] : h[0]) + dpp_f32<0x128>(up ? h[0] : h[1]);   // row_ror:8
-      v += dpp_f32<0x141>(v);             // row_half_mirror
-      v += dpp_f32<0xb1>(v);              // quad_perm 1 0 3 2
-      v += dpp_f32<0x4e>(v);              // quad_perm 2 3 0 1
-      const int value = t + 4 * ((lane >> 3) & 1) + 8 * ((lane >> 4) & 1);
-      if ((lane & 7) == 0) s_sum[wave * kWideKeys + 32 * m + 8 * (value >> 2) + (value & 3) + 4 * half] = v;
-    }
+  sums_of_keys(sum, s_sum + wave * kWideKeys);
   __syncthreads();
   const int key = c0 + tid;
   if (tid < KG * kWideKeys && key < end) {
@@ -426,6 +437,173 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
     const size_t at = (size_t)bg * c.stride + key;
     c.weights_out[at] = key < old ? c.weights[at] + v : v;
     if (key >= old) c.positions[at] = c.first_position[b] + (key - old);
+  }
+}
+
+// ----------------------------------------------------- 65 to 256 rows, many keys
+//
+// So few rows fit LDS together with the codes of the keys to come, so a workgroup brings
+// them once and its waves take blocks of 64 keys, alone, without a barrier: as above a
+// block is A operands in registers and the rows pass by, 32 at a time, the exponentials
+// of 32 beside the products of the next.  The codes of a wave's next block come straight
+// from memory to LDS meanwhile.
+constexpr int kMidThreads = 512;
+constexpr int kMidWaves = kMidThreads / kWave;
+constexpr int kMidRows = 256;
+constexpr int kMidBlocks = 16;   // of a workgroup, at most
+
+__global__ __launch_bounds__(kMidThreads, 2) void kv8_weights_mid_kernel(const WeightsArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t s_rows[kMidRows * kRowBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_codes[kMidWaves][kWideKeys * kKv8RowBytes];
+  __shared__ int s_at[kMidRows];       // as in the wide kernel
+  __shared__ float s_lse2[kMidRows];
+  __shared__ float s_sum[kMidWaves][kWideKeys];
+  __shared__ int s_any;
+  const AttnWeightsCall& c = a.c;
+  const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
+  const int b = bg / c.Hkv, g = bg - b * c.Hkv;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int lane = lane_id(), col = lane & 31, half = lane >> 5;
+  const RowAt mine = row_at(a, b, g, tid % kMidRows);
+  const int old = min(max(c.lens_old[b], 0), c.L_max);
+  const int n = min(max(min(max(c.lens_new[b], 0), c.L_max) - old, 0), c.N);
+  const int end = old + n, chunk0 = split * a.chunk, c1 = min(chunk0 + a.chunk, end);
+  if (chunk0 >= end) return;
+  const int rows = n * a.G, blocks = (rows + 31) / 32;
+  const float* const w_in = c.weights + (size_t)bg * c.stride;
+  float* const w_out = c.weights_out + (size_t)bg * c.stride;
+
+  // Of the wave's block at k0: lane j the page of key j, the codes to LDS (chunk p of key
+  // j lies at p ^ (j & 7)), the scales of the lane's two keys, the older weight of key
+  // `lane`.  Keys behind the last read the last one again; their sums are not stored.
+  const int32_t* const table = c.page_table + (size_t)b * c.max_pages;
+  auto pages_of = [&](int k0) { return page_in_pool(table[min(k0 + lane, end - 1) >> a.page_shift], c.n_pages); };
+  uint32_t exponent[2];
+  float w;
+  auto load_keys = [&](int k0, int pages) {
+    auto row_of = [&](int key) {
+      return pool_row(__shfl(pages, key, kWave), g, min(k0 + key, end - 1) & ((1 << a.page_shift) - 1), c.Hkv, a.page_shift);
+    };
+    const uint32_t to = lds_addr(s_codes[wave]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      dma16(c.k_codes + row_of(8 * i + lane / 8) * kKv8RowBytes + ((lane ^ (lane / 8)) & 7) * 16,
+            __builtin_amdgcn_readfirstlane(to + i * 1024));
+#pragma unroll
+    for (int m = 0; m < 2; ++m) exponent[m] = c.k_scales[row_of(32 * m + col) >> kKv8BlockShift];
+    w = w_in[min(k0 + lane, max(old - 1, 0))];
+  };
+  int k0 = chunk0 + wave * kWideKeys;
+  constexpr int kNext = kMidWaves * kWideKeys;
+  int pages = pages_of(k0);
+  load_keys(k0, pages);
+  pages = pages_of(k0 + kNext);
+
+  if (tid == 0) s_any = -1;
+  __syncthreads();
+  if (tid < blocks * 32) {
+    const bool gives = tid < rows && mine.lse2 < INFINITY;
+    s_at[tid] = gives ? mine.place : -1;
+    s_lse2[tid] = gives ? mine.lse2 : INFINITY;
+    if (gives) s_any = mine.place;
+  }
+  __syncthreads();
+  const int any = s_any;
+  if (any >= 0) {
+    const uint16_t* const q0 = c.q + (size_t)b * c.T_max * c.Hq * kD;
+    for (int i = 0; i < blocks; ++i) {
+      const int r4 = 32 * i + 4 * wave, row = r4 + lane / 16, at = s_at[row];
+      dma16(q0 + (size_t)(at < 0 ? any : at) * kD + ((lane ^ row) & 15) * 8,
+            __builtin_amdgcn_readfirstlane(lds_addr(s_rows) + r4 * kRowBytes));
+    }
+  }
+  waitcnt_vm<0>();
+  __syncthreads();
+
+  for (; k0 < c1; k0 += kNext) {
+    waitcnt_vm<0>();
+    asm volatile("" ::: "memory");   // the codes have landed
+    bf16x8_t kf[2][8];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      const float X = kv8_scale((int)exponent[m]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x4_t x = *reinterpret_cast<const u32x4_t*>(s_codes[wave] + (32 * m + col) * kKv8RowBytes +
+                                                            (((4 * half + i) ^ col) & 7) * 16);
+        kf[m][2 * i] = operand(x[0], x[1], X);
+        kf[m][2 * i + 1] = operand(x[2], x[3], X);
+      }
+    }
+    const float before = w;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // and are read
+    if (k0 + kNext < c1) {
+      load_keys(k0 + kNext, pages);
+      pages = pages_of(k0 + 2 * kNext);
+    }
+    float sum[2][16] = {};
+    // As in the wide kernel: eight chunks, products and exponentials in turn.
+    auto round_of = [&](int i, f32x16_t (&z)[2], f32x16_t (&z_next)[2], auto plain, auto NEXT, auto ADD) {
+      constexpr bool kNextRows = decltype(NEXT)::value, kAdd = decltype(ADD)::value;
+      bf16x8_t q[8];
+      auto operand_of = [&](int d) {
+        return *reinterpret_cast<const bf16x8_t*>(s_rows + 32 * (i + 1) * kRowBytes + swizzled(col, 8 * half + d));
+      };
+      if constexpr (kNextRows) {
+#pragma unroll
+        for (int d = 0; d < 3; ++d) q[d] = operand_of(d);
+        z_next[0] = z_next[1] = f32x16_t{};
+      }
+      float lse2 = 0.f;
+      int sees = 0;
+      if constexpr (kAdd) {
+        lse2 = s_lse2[32 * i + col];
+        // the last key that the row sees, counted from the lane's first
+        if constexpr (!decltype(plain)::value) sees = old + (32 * i + col) / a.G - k0 - 4 * half;
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        if constexpr (kNextRows) {
+          if (d + 3 < 8) q[d + 3] = operand_of(d + 3);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) z_next[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[m][d], q[d], z_next[m], 0, 0, 0);
+        }
+        if constexpr (kAdd) add4(a, sum, z, d, lse2, sees, plain);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto run = [&](auto plain) {
+      using Yes = std::true_type;
+      using No = std::false_type;
+      f32x16_t za[2], zb[2];
+      round_of(-1, zb, za, plain, Yes{}, No{});
+      int i = 0;
+      for (; i + 2 < blocks; i += 2) {
+        round_of(i, za, zb, plain, Yes{}, Yes{});
+        round_of(i + 1, zb, za, plain, Yes{}, Yes{});
+      }
+      if (i + 1 < blocks) {
+        round_of(i, za, zb, plain, Yes{}, Yes{});
+        round_of(i + 1, zb, za, plain, No{}, Yes{});
+      } else {
+        round_of(i, za, zb, plain, No{}, Yes{});
+      }
+    };
+    if (any >= 0) {
+      if (k0 + kWideKeys <= old + 1) run(std::true_type{});   // every row sees all the wave's keys
+      else run(std::false_type{});
+    }
+    sums_of_keys(sum, s_sum[wave]);
+    __builtin_amdgcn_wave_barrier();
+    const int key = k0 + lane;
+    if (key < c1) {
+      const float v = s_sum[wave][lane];
+      w_out[key] = key < old ? before + v : v;
+      if (key >= old) c.positions[(size_t)bg * c.stride + key] = c.first_position[b] + (key - old);
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -440,14 +618,31 @@ hipError_t launch_kv8_attn_weights(const AttnWeightsCall& c, hipStream_t stream)
   const int64_t pairs = (int64_t)c.B * c.Hkv;
   const int64_t rows = (int64_t)c.N * a.G;
   if (rows > 64) {
-    // A workgroup of 256 keys passes 64 rows a round, one of 128 keys 128 rows; a round
-    // takes 1.2 to 1.3 us, the rest of a workgroup 4, and 256 of them run at once.  us a
-    // call, 256 / 128 keys: 4 x 4096 keys of 4 heads, 256 rows of 7 heads 41.2 / 49.9, 32
-    // of them 13.2 / 18.8; 4 x 2048, 256 rows 37.3 / 27.3, 32 13.2 / 10.0.
-    auto cost = [&](int keys, int round) {
-      const double groups = (double)(pairs * ((c.L_max + keys - 1) / keys));
-      return std::ceil(groups / 256) * (4 + 1.25 * (double)((rows + round - 1) / round));
-    };
+    // In us, 256 workgroups at a time.  One of 256 keys passes 64 rows a round, one of 128
+    // keys 128 rows; a round takes 1.2 to 1.3, the rest 4.  us a call, 256 / 128 keys: 4 x
+    // 4096 keys of 4 heads, 256 rows of 7 heads 41.2 / 49.9, 32 of them 13.2 / 18.8; 4 x
+    // 2048, 256 rows 37.3 / 27.3, 32 13.2 / 10.0.
+    auto times = [&](int keys) { return std::ceil((double)(pairs * ((c.L_max + keys - 1) / keys)) / 256); };
+    auto cost = [&](int keys, int round) { return 3 + times(keys) * (4 + 1.25 * (double)((rows + round - 1) / round)); };
+    // Up to 256 rows in LDS with blocks of 512 keys in turn.  us a call, so / as above: 16 x
+    // 8192 keys of 4 heads, 196 rows 38 / 72; 32 x 4096 of 8, 80 rows 45 / 116; 13 x 2000 of
+    // 16, 100 rows 27 / 54; 2 x 4096 of 4, 196 rows 11.8 / 10.2.
+    constexpr int kBlock = kMidWaves * kWideKeys;
+    int blocks = 0;   // of a workgroup, best
+    double least = std::min(cost(256, 64), cost(128, 128));
+    for (int p = 1; p <= kMidBlocks && rows <= kMidRows; ++p) {
+      const double t = 2.5 + times(p * kBlock) * (2.2 + p * (0.3 + 0.97 * (double)((rows + 31) / 32)));
+      if (t < least) {
+        least = t;
+        blocks = p;
+      }
+    }
+    if (blocks > 0) {
+      a.chunk = blocks * kBlock;
+      a.nsplit = (c.L_max + a.chunk - 1) / a.chunk;
+      hipLaunchKernelGGL(kv8_weights_mid_kernel, dim3((unsigned)(pairs * a.nsplit)), dim3(kMidThreads), 0, stream, a);
+      return hipGetLastError();
+    }
     auto wide = [&](auto KG, auto parts) {
       constexpr int kg = decltype(KG)::value, kp = decltype(parts)::value;
       a.chunk = kg * kWideKeys;

@@ -109,6 +109,13 @@ def test_weights_of_many_rows(T, Hq, Hkv, L):
     check_weights([L - T], [L], Hq, Hkv, T, 64)
 
 
+@pytest.mark.parametrize("T, Hq, B", [(80, 8, 3), (7, 80, 3), (256, 8, 2)])
+def test_weights_of_some_rows_over_long_contexts(T, Hq, B):
+    """Rows that stay in LDS while several blocks of keys pass."""
+    new = [9001, 8700, 4100][:B]
+    check_weights([n - T for n in new[:-1]] + [new[-1] - 1], new, Hq, 8, T, 64)
+
+
 def test_weights_with_large_logits():
     check_weights([400, 20], [403, 23], 4, 1, 3, 16, wide=8.0)
 
