@@ -68,20 +68,33 @@ __device__ __forceinline__ void store(V* p, V v) {
   else *p = v;
 }
 
-// Where the other half of a pair is: beside it (16 bytes a lane, both runs); rot_dim / 2
-// on (8 bytes a run); or, for a rotation of the whole head, half a head on: then lanes 8
-// apart read 16 bytes each and exchange a run, before and after.
-enum Pairs { kBeside, kApart, kHalfHead };
+// Where the other half of a pair is: kBeside it (16 bytes a lane, both runs); rot_dim / 2
+// on, kApart (8 bytes a run); or, where that is a power of two of lanes, so many on: then
+// those lanes read 16 bytes each and exchange a run, before and after (14298 tokens of 64
+// heads, 16 of 128 dimensions rotated 101 -> 87 us against 8 bytes a run).
+constexpr int kBeside = 0, kApart = -1;
 
-// What the lane 8 further on or back has.
-__device__ __forceinline__ uint2 of_lane_xor8(uint2 v) {
-  return make_uint2((uint32_t)__builtin_amdgcn_mov_dpp((int)v.x, 0x128, 0xf, 0xf, false),
-                    (uint32_t)__builtin_amdgcn_mov_dpp((int)v.y, 0x128, 0xf, 0xf, false));
+// What the lane X further on or back has.
+template <int X>
+__device__ __forceinline__ uint32_t of_lane_xor(uint32_t v) {
+  static_assert(X == 1 || X == 2 || X == 4 || X == 8, "within a head's lanes");
+  auto dpp = [](uint32_t x, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xf, 0xf, false);
+  };
+  if constexpr (X == 1) return dpp(v, std::integral_constant<int, 0xb1>{});        // quad_perm 1 0 3 2
+  else if constexpr (X == 2) return dpp(v, std::integral_constant<int, 0x4e>{});   // quad_perm 2 3 0 1
+  else if constexpr (X == 4)                                                       // row_half_mirror, quad_perm 3 2 1 0
+    return dpp(dpp(v, std::integral_constant<int, 0x141>{}), std::integral_constant<int, 0x1b>{});
+  else return dpp(v, std::integral_constant<int, 0x128>{});                        // row_ror:8
+}
+template <int X>
+__device__ __forceinline__ uint2 of_lane_xor(uint2 v) {
+  return make_uint2(of_lane_xor<X>(v.x), of_lane_xor<X>(v.y));
 }
 
 // STREAM: for many rows; they are loaded and stored with the non-temporal hint, and
 // not before it is known that the token counts.
-template <Pairs PAIRS, int H, bool STREAM>
+template <int PAIRS, int H, bool STREAM>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(const NormRopeCall c, int parts) {
   // B * T * parts fits 31 bits by the host's check
   const uint32_t job = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -92,8 +105,8 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(const NormRopeCa
   const int part = threadIdx.x % kLanes, group = lane_id() / kLanes;
   // the lane's two runs
   const bool rotated = part < c.rot_dim / 8;
-  const bool low = part < kLanes / 2;
-  const int run0 = PAIRS == kBeside || !rotated ? 8 * part : PAIRS == kApart ? 4 * part : low ? 8 * part : 8 * part - 60;
+  const bool low = !(part & PAIRS);
+  const int run0 = PAIRS == kBeside || !rotated ? 8 * part : PAIRS == kApart ? 4 * part : low ? 8 * part : 8 * (part - PAIRS) + 4;
   const int run1 = PAIRS == kBeside || !rotated ? run0 + 4 : run0 + c.rot_dim / 2;
   const int freq0 = PAIRS == kBeside ? 4 * part : run0;
 
@@ -149,10 +162,10 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(const NormRopeCa
   for (int i = 0; i < H; ++i) {
     const int h = first + kGroups * i + group, side = h >= c.Hq;
     if (h >= heads) return;   // the 16 lanes of a head leave together
-    if constexpr (PAIRS == kHalfHead) {
-      const uint2 other = of_lane_xor8(low ? x[i][1] : x[i][0]);
-      if (low) x[i][1] = other;
-      else x[i][0] = other;
+    if constexpr (PAIRS > 0) {
+      const uint2 other = of_lane_xor<PAIRS>(low ? x[i][1] : x[i][0]);
+      if (rotated && low) x[i][1] = other;
+      if (rotated && !low) x[i][0] = other;
     }
     float y[8];
     unpack4(x[i][0], y);
@@ -176,10 +189,10 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(const NormRopeCa
     }
     uint16_t* const to = c.out[side] + ((size_t)tok * (side ? c.Hkv : c.Hq) + (side ? h - c.Hq : h)) * ADAPLD_HEAD_DIM;
     uint2 r0 = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3])), r1 = make_uint2(pack2(y[4], y[5]), pack2(y[6], y[7]));
-    if constexpr (PAIRS == kHalfHead) {
-      const uint2 other = of_lane_xor8(low ? r1 : r0);
-      if (low) r1 = other;
-      else r0 = other;
+    if constexpr (PAIRS > 0) {
+      const uint2 other = of_lane_xor<PAIRS>(low ? r1 : r0);
+      if (rotated && low) r1 = other;
+      if (rotated && !low) r0 = other;
     }
     if constexpr (PAIRS != kApart) {
       store<STREAM>(reinterpret_cast<u32x4_t*>(to + 8 * part), (u32x4_t){r0.x, r0.y, r1.x, r1.y});
@@ -200,12 +213,17 @@ hipError_t launch_qk_norm_rope(const NormRopeCall& c, hipStream_t stream) {
     constexpr bool STREAM = decltype(st)::value;
     const int parts = (heads + kGroups * H - 1) / (kGroups * H);
     const dim3 grid((unsigned)((tokens * parts + kWaves - 1) / kWaves));
-    if (c.interleaved)
-      hipLaunchKernelGGL((qk_norm_rope_kernel<kBeside, H, STREAM>), grid, dim3(kThreads), 0, stream, c, parts);
-    else if (c.rot_dim == ADAPLD_HEAD_DIM)
-      hipLaunchKernelGGL((qk_norm_rope_kernel<kHalfHead, H, STREAM>), grid, dim3(kThreads), 0, stream, c, parts);
-    else
-      hipLaunchKernelGGL((qk_norm_rope_kernel<kApart, H, STREAM>), grid, dim3(kThreads), 0, stream, c, parts);
+    auto launch = [&](auto pairs) {
+      hipLaunchKernelGGL((qk_norm_rope_kernel<decltype(pairs)::value, H, STREAM>), grid, dim3(kThreads), 0, stream, c, parts);
+    };
+    if (c.interleaved) return launch(std::integral_constant<int, kBeside>{});
+    switch (c.rot_dim) {
+      case 16: return launch(std::integral_constant<int, 1>{});
+      case 32: return launch(std::integral_constant<int, 2>{});
+      case 64: return launch(std::integral_constant<int, 4>{});
+      case 128: return launch(std::integral_constant<int, 8>{});
+      default: return launch(std::integral_constant<int, kApart>{});
+    }
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;

@@ -47,7 +47,7 @@ def weight(rng):
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
-@pytest.mark.parametrize("rot", [0, 16, 48, 64, 80, 112, 128])
+@pytest.mark.parametrize("rot", [0, 16, 32, 48, 64, 80, 96, 112, 128])
 @pytest.mark.parametrize("B, T, Hq, Hkv", [(1, 1, 1, 1), (2, 5, 7, 1), (3, 9, 4, 2), (1, 33, 16, 16)])
 def test_against_float64(B, T, Hq, Hkv, rot, interleaved):
     rng = np.random.default_rng(rot + B)
