@@ -10,9 +10,9 @@
 // each, until all equal ones stay; a thread holds its slots' weights and positions in
 // registers throughout, up to 16384 slots.
 //
-// Where it stands: 128 kv heads, 2065 tokens to 2048, 13 us: launch and loads 3.4,
-// protected tokens 1.3, a digit 1.2, the ranks 2.7, the moves 3.6, one after the other,
-// half of the CUs busy.  8192 tokens at most to 2048: selection 14 and moves 24 (some 91
+// Where it stands: 128 kv heads, 2065 tokens to 2048, 12 us: launch and loads 3, a digit
+// 1.2, the ranks 2, the moves 3.5, one after the other, half of the CUs busy; 75 tokens to
+// 32 of 8 heads 9.  8192 tokens at most to 2048: selection 14 and moves 24 (some 91
 // MB, 3.7 TB/s in the latter; without the rows' reads 17, without their writes 18.5,
 // without the scales 19).  One, two or four blocks a wave, and a head's blocks on one XCD,
 // made no difference.
