@@ -116,11 +116,19 @@ def test_weights_of_some_rows_over_long_contexts(T, Hq, B):
     check_weights([n - T for n in new[:-1]] + [new[-1] - 1], new, Hq, 8, T, 64)
 
 
+def test_weights_of_many_accepted_rows():
+    """Queries in any order, some twice, some that are none; fewer rows than the bound."""
+    rng = np.random.default_rng(4)
+    rows = rng.integers(-1, 32, (3, 24)).tolist()
+    rows[0][3], rows[1][:] = 2 ** 31 - 1, [5] * 24
+    check_weights([400, 90, 0], [424, 100, 7], 16, 4, 31, 32, rows=rows)
+
+
 def test_weights_with_large_logits():
     check_weights([400, 20], [403, 23], 4, 1, 3, 16, wide=8.0)
 
 
-@pytest.mark.parametrize("T, Hq, Hkv", [(5, 4, 2), (20, 8, 1), (70, 4, 2)])
+@pytest.mark.parametrize("T, Hq, Hkv", [(5, 4, 2), (22, 4, 1), (20, 8, 1), (70, 4, 2)])
 def test_weights_ignore_what_is_no_row(T, Hq, Hkv):
     """NaN in the queries and log-sum-exps that no row picks, in keys behind the length
     and in weights behind the old one changes nothing."""
@@ -141,7 +149,7 @@ def test_weights_ignore_what_is_no_row(T, Hq, Hkv):
     assert torch.equal(call(), want)
 
 
-@pytest.mark.parametrize("T, Hq, Hkv", [(4, 4, 4), (5, 4, 2), (20, 8, 1), (70, 4, 2), (256, 2, 2)])
+@pytest.mark.parametrize("T, Hq, Hkv", [(4, 4, 4), (5, 4, 2), (24, 4, 1), (20, 8, 1), (70, 4, 2), (256, 2, 2)])
 def test_weights_ignore_rows_without_keys(T, Hq, Hkv):
     """Heads whose log-sum-exp is -inf, or no number, give nothing, whatever their queries
     hold; a sequence may have no others."""
