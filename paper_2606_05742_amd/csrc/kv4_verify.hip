@@ -22,6 +22,7 @@ namespace {
 // A part is a group of 32 dimensions: 16 bytes of codes and a scale of its own.
 struct Kv4Format {
   static constexpr int kLoads = 1, kCodeBytes = kKv4RowBytes;
+  static constexpr int kSmallFrom = 0;
   // A model's layers each bring their own cache, so a call finds its codes in
   // HBM; where one wave reads each of them, large ones are streamed past the
   // caches.  us a call over rotating caches, plain / non-temporal: single tokens,

@@ -20,6 +20,12 @@ namespace {
 // brings: the same for all its lanes.
 struct Kv8Format {
   static constexpr int kLoads = 2, kCodeBytes = kKv8RowBytes;
+  // Where there are more workgroups than CUs, two share one.  us a call, 4 / 8 waves: 64 x
+  // 4096 keys of 8 heads, single tokens 93.9 / 97.2; 48 x 4096 76.4 / 81.7; 16 x 300 of 32
+  // heads 12.9 / 15.5; 64 x 517 of 8, 8 nodes 21.0 / 25.8; 45 x 130 of 32, 56 rows 54.1 /
+  // 67.0.  With no more they are the same or slower: 1 x 517 of 32 10.1 / 9.3, 32 x 4096, 64
+  // rows 86.6 / 81.7.
+  static constexpr int kSmallFrom = 256;
   // Two loads share a line, which the non-temporal hint lets go between them: us a call,
   // plain / with it, single tokens, 32 x 8192 keys of 8 heads 93.6 / 103.9, 4 x 30000 51.5
   // / 58.1; 8 nodes, 16 x 4096 36.3 / 38.9.

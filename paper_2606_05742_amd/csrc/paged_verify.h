@@ -18,6 +18,7 @@
 //                          j = 0..3 of the part is
 //   dequant(c, j, X)       that group as 8 bf16 values, scale X
 //   load_scale(...)        the part's scale byte
+//   kSmallFrom             workgroups beyond which they have 4 waves up to 64 rows; 0: never
 //   kStreamBytes           bytes of codes from which on a cache that one wave reads is
 //                          loaded with the non-temporal hint; 0: never
 #pragma once
@@ -867,12 +868,14 @@ struct Rows32 {
   }
 };
 
-// STREAM: the codes are loaded with the non-temporal hint.
-template <class F, class ROWS, int RB, bool STREAM>
-__global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs a) {
-  constexpr int kSlices = kWaves / RB;   // waves that share a row block's keys
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kWaves * 2 * kVBuffer];
-  __shared__ float2 s_ml[kWaves][ROWS::kRows];
+// STREAM: the codes are loaded with the non-temporal hint.  W: the waves of a workgroup,
+// kWaves, or 4, of which two workgroups share a CU.
+template <class F, class ROWS, int RB, bool STREAM, int W>
+__global__ __launch_bounds__(W * kWave, 2) void paged_narrow_kernel(const PagedArgs a) {
+  constexpr int kSlices = W / RB;   // waves that share a row block's keys
+  static_assert(kSlices >= 2, "two steps of the tree");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[W * 2 * kVBuffer];
+  __shared__ float2 s_ml[W][ROWS::kRows];
   const VerifyPagedCall& c = a.c;
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
   const int b = bg / c.Hkv, g = bg - b * c.Hkv;
@@ -1046,9 +1049,9 @@ __global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs 
       // with the loads of half the waves left for the rest: 32 x 8192, single tokens,
       // 42 us against 48.  So the younger goes first in every other step (47.5 ->
       // 46.8 us a call; chains of 16 nodes, 32 x 4096, 55.2 -> 54.3).
-      if (wave >= kWaves / 2) __builtin_amdgcn_s_setprio(1);
+      if (W == kWaves && wave >= kWaves / 2) __builtin_amdgcn_s_setprio(1);
       ctx_pair(s, r[1], 0);
-      __builtin_amdgcn_s_setprio(0);
+      if (W == kWaves) __builtin_amdgcn_s_setprio(0);
       ctx_pair(s + kSlices, r[0], 1);
     }
     for (int buf = 0; s < n_ctx; s += kSlices, buf ^= 1) {   // at most two steps
@@ -1067,7 +1070,7 @@ __global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs 
   // its waves' common max.
   constexpr int kMergeRows = 2 * kVBuffer / (kD * 4);   // rows of a wave's part
   static_assert(ROWS::kRows <= kMergeRows, "a wave's rows fit its own V buffers");
-  float4* const xo = reinterpret_cast<float4*>(smem);   // [kWaves][kMergeRows][32]
+  float4* const xo = reinterpret_cast<float4*>(smem);   // [W][kMergeRows][32]
   {
     const float l = x.total();
     const int r = ROWS::row();
@@ -1078,8 +1081,8 @@ __global__ __launch_bounds__(kThreads) void paged_narrow_kernel(const PagedArgs 
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < RB * ROWS::kRows / 16; ++i) {
-    const int out_row = 16 * i + (tid >> 5), ch = tid & 31;
+  for (int i = 0; i < RB * ROWS::kRows / (2 * W); ++i) {
+    const int out_row = 2 * W * i + (tid >> 5), ch = tid & 31;
     if (out_row >= rows) break;
     const int rb = out_row / ROWS::kRows, r = out_row % ROWS::kRows;
     float2 ml[kSlices];
@@ -1241,8 +1244,15 @@ hipError_t launch_paged(const VerifyPagedCall& c, const VerifyPagedPlan& p, hipS
   const int units = c.B * c.Hkv * p.nsplit;
   const dim3 grid((unsigned)((units + 7) / 8 * 8 * p.rowgroups));
   auto narrow = [&](auto rows, auto rb, auto st) {
-    hipLaunchKernelGGL((paged_narrow_kernel<F, decltype(rows), decltype(rb)::value, decltype(st)::value>),
-                       dim3((unsigned)units), dim3(kThreads), 0, stream, a);
+    auto go = [&](auto waves) {
+      constexpr int W = decltype(waves)::value;
+      hipLaunchKernelGGL((paged_narrow_kernel<F, decltype(rows), decltype(rb)::value, decltype(st)::value, W>),
+                         dim3((unsigned)units), dim3(W * kWave), 0, stream, a);
+    };
+    if constexpr (F::kSmallFrom > 0) {
+      if (units > F::kSmallFrom) return go(std::integral_constant<int, 4>{});
+    }
+    go(std::integral_constant<int, kWaves>{});
   };
   using One = std::integral_constant<int, 1>;
   using Two = std::integral_constant<int, 2>;

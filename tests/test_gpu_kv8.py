@@ -261,8 +261,30 @@ def test_verify_like_the_dense_cache():
 def test_long_splits(T, Hq, Hkv, L):
     """More steps of one wave than a register holds page ids for, against float64."""
     B = 32 if T < 52 else 16
-    c = Case8([L - 17 * b for b in range(B)], Hq, Hkv, T, [T] * B, 64, L, 89, tree="chain" if T > 1 else None)
+    check_heads(Case8([L - 17 * b for b in range(B)], Hq, Hkv, T, [T] * B, 64, L, 89, tree="chain" if T > 1 else None))
+
+
+@pytest.mark.parametrize("T", [1, 8, 16])
+def test_long_contexts_of_many_sequences(T):
+    """The same for workgroups of four waves."""
+    check_heads(Case8([9001 - 17 * b for b in range(33)], 32, 8, T, [T] * 33, 64, 9001, 97, tree="chain" if T > 1 else None))
+
+
+@pytest.mark.parametrize("T, Hq, tree", [(1, 8, None), (1, 60, None), (4, 16, "random"), (7, 16, "random"),
+                                         (15, 16, "random"), (16, 16, "chain")])
+def test_many_short_sequences(T, Hq, tree):
+    """More workgroups than CUs, which then have four waves."""
+    lens = [(37 * b) % 91 for b in range(66)] + [0, 257, 511, 640]
+    c = Case8(lens, Hq, 4, T, [T - b % min(T, 3) for b in range(70)], 16, 640, 53, tree=tree)
     out, lse = c.run()
+    c.check(out, lse)
+
+
+def check_heads(c):
+    """Some heads of a case against float64."""
+    out, lse = c.run()
+    B, T, Hq, _ = c.q.shape
+    Hkv, L = c.kq.shape[1], c.L_max
     G = Hq // Hkv
     for b, g in ((0, 0), (0, Hkv - 1), (B - 1, 3)):
         n = c.lens[b]
