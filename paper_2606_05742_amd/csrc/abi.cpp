@@ -606,7 +606,7 @@ int adapld_qk_norm_rope(const uint16_t* q, const uint16_t* k, int64_t q_batch, i
                         (const void*)q_out, (const void*)k_out})
     if (misaligned16(p)) return ADAPLD_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(freqs) & 7u) != 0) return ADAPLD_ERR_INVALID_ARG;
-  // at least 4 heads of a token a wave, and 16 where there are more rows than 2^18
+  // at least 4 heads of a token a wave, and 16 where there are many rows
   if (D != ADAPLD_HEAD_DIM || (double)B * T * ((double)Hq + Hkv) > kKv4MaxRows ||
       (double)B * T * (((int64_t)Hq + Hkv + 15) / 16) > kMaxWaves)
     return ADAPLD_ERR_UNSUPPORTED;

@@ -232,9 +232,9 @@ hipError_t launch_qk_norm_rope(const NormRopeCall& c, hipStream_t stream) {
   // us a call, 4 / 8 / 16 heads a wave, the largest streamed: 1 token of 40 heads 2.7 / 3.0
   // / 3.9; 832 7.2 / 6.8 / 7.6; 2800 14.8 / 12.6 / 13.5; 24028 of 32 112 / 90 / 79, streamed
   // - / 78 / 68 (pairs beside each other 98 / 83 / 76, - / 73 / 65: 4.8 TB/s, where a copy
-  // moves 5.1).
+  // moves 5.1).  8 heads plain / 16 streamed: 190080 rows 23.7 / 24.4, 240000 33.3 / 31.2.
   if (rows <= 8192) go(One{}, std::false_type{});
-  else if (rows <= 1 << 18) go(Two{}, std::false_type{});
+  else if (rows <= 3 << 16) go(Two{}, std::false_type{});
   else go(Four{}, std::true_type{});
   return hipGetLastError();
 }
