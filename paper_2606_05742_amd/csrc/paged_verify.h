@@ -616,8 +616,9 @@ __global__ __launch_bounds__(kThreads, 1) void paged_verify_kernel(const PagedAr
 // ------------------------------------------------------------- up to 64 rows
 //
 // With few rows (single tokens, one copied chain) the call is one pass over the
-// cache, so waves share no keys: of the 8 waves, 8 / RB take the 32-key steps of
-// the split in turn for each of RB row blocks, alone, without a barrier.  16
+// cache, so waves share no keys: of the W waves (8, or 4 where a format says so),
+// W / RB take the 32-key steps of the split in turn for each of RB row blocks, alone,
+// without a barrier.  16
 // rows run on 16x16x32 products, 32 and 64 in blocks of 32 on 32x32x16 ones.
 //
 // Lane (quad, col) brings part `quad` of keys col and 16 + col.  K codes become A
