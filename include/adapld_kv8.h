@@ -172,8 +172,9 @@ int adapld_tree_verify_attn_kv8(const uint16_t* q, const uint8_t* k_codes, const
  *   L_max       an upper bound of the lengths, at most max_pages * page_size and
  *               at most stride
  *   weights_out fp32 [B, Hkv, stride] (out); weights itself, or no overlap
- * Sums are fp32, in an order that the sizes fix.  Of the heads that give, q, the keys
- * and scale * q.k * log2(e) are finite.
+ * Sums are fp32, in an order that the sizes fix.  For the rows and heads that give, q,
+ * the keys that they see and scale * q.k * log2(e) are finite; a key that only others
+ * see may be a NaN, and gets nothing.
  *
  * Errors: NULL_ARG; INVALID_ARG for B < 0, Hq % Hkv != 0, non-positive sizes, N > T_max
  * without rows, L_max > max_pages * page_size or stride, a page_size other than the

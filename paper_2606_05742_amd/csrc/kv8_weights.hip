@@ -142,6 +142,7 @@ __global__ __launch_bounds__(kNarrowThreads, RB == 1 ? 4 : RB == 2 ? 3 : 2) void
 
   const float my_lse2 = lane < n * a.G ? mine.lse2 : INFINITY;
   const int my_place = my_lse2 < INFINITY ? mine.place : -1;
+  const bool none = !__any(my_lse2 < INFINITY);   // then nothing is known of the keys
   bf16x8_t q[RB][4];
   float lse2[RB][4];
 #pragma unroll
@@ -179,8 +180,12 @@ __global__ __launch_bounds__(kNarrowThreads, RB == 1 ? 4 : RB == 2 ? 3 : 2) void
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           float e = __builtin_amdgcn_exp2f(fmaf(z[rb][t], a.sl2, -lse2[rb][t]));
-          if (!plain)   // a new row sees no later one
-            e = k0 + 16 * i + col <= old + __shfl(mine.i, 16 * rb + 4 * quad + t, kWave) ? e : 0.f;
+          // A new row sees no later one, and one that gives nothing none of the new ones: where
+          // no other row sees them they may be NaN.  All rows see the older ones.
+          if (!plain) {
+            const int last_seen = old + __shfl(mine.i, 16 * rb + 4 * quad + t, kWave);   // by all lanes
+            e = lse2[rb][t] < INFINITY && k0 + 16 * i + col <= last_seen ? e : 0.f;
+          }
           p[t] += e;
         }
       sum[i] = (p[0] + p[1]) + (p[2] + p[3]);
@@ -188,7 +193,7 @@ __global__ __launch_bounds__(kNarrowThreads, RB == 1 ? 4 : RB == 2 ? 3 : 2) void
     load(s + 3 * kNarrowWaves, x);
     // lanes 0..15 and 16..31 take the sums of either half
     const float v0 = add_lane_xor32(add_lane_xor16(sum[0])), v1 = add_lane_xor32(add_lane_xor16(sum[1]));
-    const float v = n == 0 ? 0.f : quad & 1 ? v1 : v0;   // without rows nothing is known of the keys
+    const float v = none ? 0.f : quad & 1 ? v1 : v0;
     const int key = k0 + lane;
     if (lane < kStep && key < c1) {
       w_out[key] = key < old ? w + v : v;
@@ -268,6 +273,9 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
   __shared__ __attribute__((aligned(1024))) uint8_t s_rows[kStages][kRows * kRowBytes];
   __shared__ int s_at[kMaxRows];       // query of a row, in rows of q behind the sequence's first; -1: it gives nothing
   __shared__ float s_lse2[kMaxRows];
+  // The last key that a row sees; -1 where it gives nothing: new keys that no other row sees
+  // may be NaN.
+  __shared__ int s_last[kMaxRows];
   __shared__ int s_any;
   const AttnWeightsCall& c = a.c;
   const int bg = blockIdx.x / a.nsplit, split = blockIdx.x - bg * a.nsplit;
@@ -316,6 +324,7 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
         const bool gives = first + r < rows && x[i].lse2 < INFINITY;
         s_at[r] = gives ? x[i].place : -1;
         s_lse2[r] = gives ? x[i].lse2 : INFINITY;
+        s_last[r] = gives ? old + x[i].i : -1;
         if (gives) s_any = x[i].place;
       }
     }
@@ -377,7 +386,7 @@ __global__ __launch_bounds__(KG * kParts * kWave, 2) void kv8_weights_wide_kerne
       if constexpr (kAdd) {
         lse2 = s_lse2[r];
         // the last key that the row sees, counted from the lane's first
-        if constexpr (!decltype(plain)::value) sees = old + (first + r) / a.G - k0 - 4 * half;
+        if constexpr (!decltype(plain)::value) sees = s_last[r] - k0 - 4 * half;
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -457,6 +466,7 @@ __global__ __launch_bounds__(kMidThreads, 2) void kv8_weights_mid_kernel(const W
   __shared__ __attribute__((aligned(1024))) uint8_t s_codes[kMidWaves][kWideKeys * kKv8RowBytes];
   __shared__ int s_at[kMidRows];       // as in the wide kernel
   __shared__ float s_lse2[kMidRows];
+  __shared__ int s_last[kMidRows];
   __shared__ float s_sum[kMidWaves][kWideKeys];
   __shared__ int s_any;
   const AttnWeightsCall& c = a.c;
@@ -506,6 +516,7 @@ __global__ __launch_bounds__(kMidThreads, 2) void kv8_weights_mid_kernel(const W
     const bool gives = tid < rows && mine.lse2 < INFINITY;
     s_at[tid] = gives ? mine.place : -1;
     s_lse2[tid] = gives ? mine.lse2 : INFINITY;
+    s_last[tid] = gives ? old + mine.i : -1;
     if (gives) s_any = mine.place;
   }
   __syncthreads();
@@ -559,8 +570,8 @@ __global__ __launch_bounds__(kMidThreads, 2) void kv8_weights_mid_kernel(const W
       int sees = 0;
       if constexpr (kAdd) {
         lse2 = s_lse2[32 * i + col];
-        // the last key that the row sees, counted from the lane's first
-        if constexpr (!decltype(plain)::value) sees = old + (32 * i + col) / a.G - k0 - 4 * half;
+        // as in the wide kernel
+        if constexpr (!decltype(plain)::value) sees = s_last[32 * i + col] - k0 - 4 * half;
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

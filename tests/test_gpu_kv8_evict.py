@@ -174,6 +174,33 @@ def test_weights_ignore_rows_without_keys(T, Hq, Hkv):
     assert torch.equal(call(), want)
 
 
+@pytest.mark.parametrize("T, Hq, Hkv, B, L", [
+    (4, 4, 4, 2, 300), (8, 4, 1, 2, 300), (50, 4, 4, 2, 300),    # up to 16, 32 and 64 stacked rows
+    (24, 4, 1, 2, 300),                                          # rows that stay in LDS
+    (20, 8, 1, 2, 300), (256, 2, 2, 2, 300),                     # the ring: 128 keys a workgroup
+    (70, 16, 4, 8, 1990)])                                       # and 256
+def test_weights_without_rows_that_see_a_nan(T, Hq, Hkv, B, L):
+    """A NaN among the keys matters to the rows that give and see it, and to no others: it
+    may lie in a kv head none of whose rows gives anything (sequence 0), or be a new key
+    that only rows which give nothing see (sequence 1)."""
+    rng = np.random.default_rng(T)
+    G, page, old = Hq // Hkv, 16, L - T
+    cache, table, _ = filled([L] * B, page, Hkv, rng)
+    q = bf16(rng.standard_normal((B, T, Hq, 128))).cuda()
+    lse = torch.full((B, Hq, T), 6.0, device="cuda")
+    lse[0, :G, ::2], lse[0, :G, 1::2] = -math.inf, math.nan
+    lse[1, -G:, 1:] = math.nan
+    w, p = torch.rand((B, Hkv, L), device="cuda"), torch.zeros((B, Hkv, L), dtype=torch.int32, device="cuda")
+    call = lambda: adapld.kv8_attn_weights(cache, q, lse, i32([old] * B), i32([L] * B), i32([0] * B), w, p,  # noqa: E731
+                                           weights_out=torch.zeros_like(w))[0]
+    want = call()
+    assert torch.isfinite(want).all() and torch.equal(want[0, 0, :old], w[0, 0, :old])
+    assert (want[0, 0, old:] == 0).all() and (want[1, -1, old + 1:] == 0).all() and want[1, -1, old] > 0
+    for b, g, j in ((0, 0, 5), (0, 0, L - 1), (1, Hkv - 1, old + 1), (1, Hkv - 1, L - 1)):
+        cache.k_codes[int(table[b][j // page]), g, j % page, 77] = 0x7f
+    assert torch.equal(call(), want)
+
+
 def test_weights_long_and_clamped():
     """Longer than one workgroup takes, several sequences; lengths outside are clamped."""
     rng = np.random.default_rng(5)
