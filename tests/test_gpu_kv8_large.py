@@ -1,12 +1,17 @@
-"""The 8-bit cache's larger calls on the GPU: prompts whose rows are streamed into it.
-Stored bytes are exact.
+"""The 8-bit cache's larger calls on the GPU: prompts whose rows are streamed into it, and
+evictions in one launch from more slots than threads hold.  Every byte is exact.
 """
 import math
 
 import numpy as np
 import pytest
+import torch
 
-from test_gpu_kv8 import check_append, rows_of
+import oracle
+import paper_2606_05742_amd as adapld
+from test_gpu_kv4 import i32
+from test_gpu_kv8 import arrays, check_append, make_cache, rows_of
+from test_gpu_kv8_evict import check_evict
 
 pytestmark = pytest.mark.gpu
 
@@ -36,3 +41,40 @@ def test_append_many_picked_rows():
     rows = rng.integers(-1, n_src + 1, (B, N)).tolist()
     rows[0][7], rows[1][8] = 2 ** 31 - 1, -2 ** 31
     check_append(k, v, [0, 9, 500], [4000, 2900, 3100], 32, rows=rows, table_of=[3040, 2900, 3072])
+
+
+# ----------------------------------- at most 64 rows move, more than 8192 slots a kv head
+
+KINDS = {"distinct": None, "few values": lambda r, s: r.integers(0, 3, s) / 2, "all equal": lambda r, s: np.full(s, 0.5)}
+
+
+@pytest.mark.parametrize("weights", sorted(KINDS))
+@pytest.mark.parametrize("lens, budget, recent", [([9000, 8961], 8960, 17), ([16384, 16383, 5], 16320, 0),
+                                                  ([16417, 16390], 16384, 256), ([20000, 64, 16500], 64, 9),
+                                                  ([33000], 32944, 20)])
+def test_evict_in_one_launch_from_many_slots(lens, budget, recent, weights):
+    check_evict(lens, budget, recent, 64, 1, weights=KINDS[weights])
+
+
+@pytest.mark.parametrize("lens, budget", [([300, 280], 272), ([9000, 8961], 8960), ([16417, 16390], 16384), ([20000, 16500], 64)])
+def test_evict_in_one_launch_in_place(lens, budget):
+    """Weights and positions in place, the lengths apart, which a loop gets by default."""
+    rng = np.random.default_rng(budget)
+    B, Hkv, page, recent = len(lens), 2, 64, 30
+    cache, table = make_cache(lens, page, Hkv, rng)
+    k, v = rows_of(rng, B, max(lens), Hkv, 12)
+    adapld.kv8_append(cache, k.cuda(), v.cuda(), i32([0] * B), i32(lens))
+    stride = max(lens) + 3
+    w = np.floor(rng.random((B, Hkv, stride)) * 5000).astype(np.float32)
+    p = np.stack([[rng.permutation(2 * stride)[:stride] for _ in range(Hkv)] for _ in range(B)]).astype(np.int32)
+    want = arrays(cache)
+    wo, po, lo = oracle.kv8_evict(w, p, lens, [2 * stride] * B, budget, recent, table, page, want)
+    tw, tp = torch.from_numpy(w).cuda(), torch.from_numpy(p).cuda()
+    gw, gp, gl = adapld.kv8_evict(cache, tw, tp, i32(lens), i32([2 * stride] * B), budget, recent, L_max=max(lens))
+    assert gw is tw and gp is tp and gl.tolist() == lo
+    for got, x in zip(arrays(cache), want):
+        assert np.array_equal(got, x)
+    for b in range(B):
+        for g in range(Hkv):
+            assert gw[b, g, :lo[b]].tolist() == [float(x) for x in wo[b * Hkv + g]] and gp[b, g, :lo[b]].tolist() == po[b * Hkv + g]
+            assert np.array_equal(gw[b, g, lo[b]:].cpu().numpy(), w[b, g, lo[b]:])
