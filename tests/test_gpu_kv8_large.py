@@ -1,5 +1,7 @@
-"""The 8-bit cache's larger calls on the GPU: prompts whose rows are streamed into it, and
-evictions in one launch from more slots than threads hold.  Every byte is exact.
+"""The 8-bit cache's larger calls on the GPU: prompts whose rows are streamed into it,
+evictions in one launch from more slots than threads hold, the attention of a chunk of a
+prompt.  Rows and evictions are exact, byte for byte; the attention's bounds are those of
+test_gpu_kv4.py.
 """
 import math
 
@@ -10,7 +12,7 @@ import torch
 import oracle
 import paper_2606_05742_amd as adapld
 from test_gpu_kv4 import i32
-from test_gpu_kv8 import arrays, check_append, make_cache, rows_of
+from test_gpu_kv8 import Case8, arrays, check_append, check_heads, make_cache, rows_of
 from test_gpu_kv8_evict import check_evict
 
 pytestmark = pytest.mark.gpu
@@ -78,3 +80,11 @@ def test_evict_in_one_launch_in_place(lens, budget):
         for g in range(Hkv):
             assert gw[b, g, :lo[b]].tolist() == [float(x) for x in wo[b * Hkv + g]] and gp[b, g, :lo[b]].tolist() == po[b * Hkv + g]
             assert np.array_equal(gw[b, g, lo[b]:].cpu().numpy(), w[b, g, lo[b]:])
+
+
+# --------------------------------------------- the attention of a prompt's chunk
+
+@pytest.mark.parametrize("Hq, T", [(32, 256), (64, 255), (4, 200)])
+def test_verify_a_chunk_of_a_prompt(Hq, T):
+    """Causal rows over a long cache: 2048, 4080 and 200 stacked rows a kv head."""
+    check_heads(Case8([5003, 1500], Hq, 4, T, [T, T], 64, 5003, Hq, tree="chain"))
