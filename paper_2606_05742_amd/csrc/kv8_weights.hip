@@ -4,8 +4,10 @@
 // For one sequence and kv head the n * G new query rows are stacked as row = i * G +
 // head.  The codes become bf16 operands in registers (exact), the logits fp32 sums of
 // matrix products, and a weight 2^(s scale log2(e) - lse log2(e)).  One wave (or one
-// workgroup's waves in a fixed order) sums up all that a key gets, so the order of a
-// sum does not depend on the launch.
+// workgroup's waves in a fixed order) sums up all that a key gets: no atomics, and the order
+// of a sum is fixed by the call's sizes.  Those choose one of the kernels below, which take a
+// key's rows in different orders, so L_max, B, N and the heads can change a sum's last bits;
+// what the other sequences of a batch hold does not.
 //
 // Where it stands: single tokens, 32 x 8192 keys of 8 heads, read 286 MB in 54 us, 5.3
 // TB/s.  196 rows (28 new ones, 28 heads over 4), 16 x 8192 keys 38 us, 0.69 PFLOP/s; 1792

@@ -117,3 +117,22 @@ def test_parts_of_the_rows_give_nothing(Hkv, B, L):
     others, all of them, or one head here and there."""
     silent = lambda b, i, h: (i < 128, i >= 128, True, (7 * i + 5 * h + b) % 3 > 0)[b % 4]  # noqa: E731
     check_rows([L - 5 * b for b in range(B)], [256] * B, 16 * Hkv, Hkv, 256, 32, silent=silent)
+
+
+@pytest.mark.parametrize("T, Hq, Hkv, L", [(1, 8, 2, 700), (16, 8, 2, 700), (40, 8, 2, 3000), (100, 8, 2, 700), (256, 28, 4, 1000)])
+def test_batch_mates_do_not_matter(T, Hq, Hkv, L):
+    """A sequence's bits stay where the others get shorter or add no rows."""
+    rng = np.random.default_rng(T)
+    new = [L - 7, L, L // 2 + T]
+    cache, _ = make_cache(new, 32, Hkv, rng)
+    k, v = (bf16(rng.standard_normal((3, L, Hkv, 128))).cuda() for _ in range(2))
+    adapld.kv8_append(cache, k, v, i32([0] * 3), i32(new))
+    q = bf16(rng.standard_normal((3, T, Hq, 128))).cuda()
+    lse = torch.from_numpy(rng.random((3, Hq, T)).astype(np.float32) * 3 + 5).cuda()
+    w, p = torch.rand((3, Hkv, L), device="cuda"), torch.zeros((3, Hkv, L), dtype=torch.int32, device="cuda")
+    call = lambda old, new: adapld.kv8_attn_weights(cache, q, lse, i32(old), i32(new), i32([0] * 3), w, p,  # noqa: E731
+                                                    weights_out=torch.zeros_like(w))[0]
+    want = call([n - T for n in new], new)
+    for b in range(3):
+        got = call([n - T if x == b else 3 for x, n in enumerate(new)], [n if x == b else 3 + x for x, n in enumerate(new)])
+        assert torch.equal(got[b], want[b])
