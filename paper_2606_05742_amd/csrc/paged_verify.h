@@ -4,12 +4,13 @@
 //
 // For one sequence and kv head the T*G query rows (node u, query head g*G + i) are
 // stacked as row = u*G + i, so the G heads that share a kv head share every byte
-// of the cache.  A workgroup of 8 waves takes a number of rows and one split of
-// the context; the last split also takes the tree's keys, which are bf16.  Two
+// of the cache.  A workgroup (8 waves, up to 64 rows also 4) takes a number of rows and one
+// split of the context; the last split also takes the tree's keys, which are bf16.  Two
 // kernels share the work by the number of rows: up to 64 rows a pass of
 // independent waves (paged_narrow_kernel), above a pipeline over tiles of 64 keys
 // (paged_verify_kernel).  Both convert the codes to bf16 (exact) and multiply on
-// bf16 matrix products with fp32 sums.
+// bf16 matrix products with fp32 sums.  Times and cycles in this file were taken with the
+// 4-bit cache's rows; those of the 8-bit cache stand in kv8_verify.hip.
 //
 // A format F says how a lane brings its part, 32 of the 128 dimensions of a key:
 //   kLoads, kCodeBytes     16-byte loads of a part, bytes of a key's codes
@@ -236,8 +237,9 @@ __device__ __forceinline__ void v_offsets(int (&vofs)[2][kD / 32]) {
 // 32-key halves of each tile, with R = 4 two waves share one and take a half
 // each.  Tiles of 64 keys are converted once per workgroup, by all its waves, into
 // a ring of 4 bf16 stages in LDS (128 KiB): while tile t is computed, tile t + 1 is
-// written and the codes of t + 2 and t + 3 are in flight in registers (10 of
-// them, against 128 KiB of LDS for bf16 tiles).  One barrier a tile publishes the
+// written and the codes of t + 2 and t + 3 are in flight in registers (4 *
+// kLoads + 1 a tile and lane: 10 of them with 4-bit rows, 18 with 8-bit ones, against 128 KiB
+// of LDS for bf16 tiles).  One barrier a tile publishes the
 // next tile and frees the one before.  The loop is software-pipelined over half
 // tiles: the products P V of half h - 1 and S of half h + 1 are issued beside the
 // exponentials of half h, with every LDS address a lane offset plus an immediate
