@@ -12,10 +12,11 @@
 //
 // Where it stands: 128 kv heads, 2065 tokens to 2048, 12 us: launch and loads 3, a digit
 // 1.2, the ranks 2, the moves 3.5, one after the other, half of the CUs busy; 75 tokens to
-// 32 of 8 heads 9.  8192 tokens at most to 2048: selection 14 and moves 24 (some 91
-// MB, 3.7 TB/s in the latter; without the rows' reads 17, without their writes 18.5,
-// without the scales 19).  One, two or four blocks a wave, and a head's blocks on one XCD,
-// made no difference.
+// 32 of 8 heads 9.  With more slots, 17 of which go, in one launch too: 8209 23, and beyond
+// the registers, with the weights read again for each step, 16401 43, 32785 70.  8192 tokens
+// at most to 2048: selection 14 and moves 24 (some 91 MB, 3.7 TB/s in the latter; without the
+// rows' reads 17, without their writes 18.5, without the scales 19).  One, two or four blocks
+// a wave, and a head's blocks on one XCD, made no difference.
 #include <type_traits>
 
 #include "adapld_internal.h"

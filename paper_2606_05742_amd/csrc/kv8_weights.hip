@@ -11,8 +11,8 @@
 //
 // Where it stands: single tokens, 32 x 8192 keys of 8 heads, read 286 MB in 54 us, 5.3
 // TB/s.  196 rows (28 new ones, 28 heads over 4), 16 x 8192 keys 38 us, 0.69 PFLOP/s; 1792
-// rows, 4 x 4096 keys 41 us, 0.73 PFLOP/s, the exponentials beside the products; 4 x 6007
-// at most, two thirds of it tokens, 64 us, in part-filled rounds of workgroups over the
+// rows, 4 x 4096 keys 40 us, 0.75 PFLOP/s, the exponentials beside the products; 4 x 6007
+// at most, two thirds of it tokens, 63 us, in part-filled rounds of workgroups over the
 // CUs.
 #include <algorithm>
 #include <cmath>
